@@ -286,6 +286,50 @@ int hg_kv_append_fp8(hg_ctx* ctx, const void* Knew, const void* Vnew, void* Ks8,
                      const int32_t* offsets, int32_t* lengths, int capacity, int B, int Hkv, int D);
 
 /*
+ * From a prompt to its first decode step (Sec. 2.2: the prompt's keys and values are what the cache holds first; Sec. 3.5: suffix lengths change from
+ * step to step).  The calls above answer decode queries, the same number for every sequence; the four below take a batch in which every
+ * sequence brings its own number of new tokens, some none and some thousands: their places in the paged cache, their rows written there, and
+ * their attention.  The tokens of all sequences lie packed one after another: sequence b owns tokens [q_off[b], q_off[b+1]) of Q, of the new K/V rows
+ * and of the results, q_off being DEVICE int32[B+1], non-decreasing; tokens that no sequence owns are nobody's, and their results are left as they
+ * are.  `rows` is a host upper bound on the tokens (the rows of the tensors): offsets are clamped to it.  HG_OPT_NUM_QUERIES is ignored.
+ *   Q rows may lie further apart than Hq * D elements, new K and V rows further apart than Hkv * D (views of a projection's output): q_stride, kv_stride and stride
+ * count elements from a row to the next, multiples of 8; tensors begin on 16-byte boundaries.  O [rows, Hq, D] and LSE [rows, Hq] (may be NULL)
+ * are packed.  A shared prefix is added as in a decode step: hg_prefix_attn or hg_prefix_attn_grouped over the tokens as sequences of one query (seq_off
+ * counting tokens), fp32 results, hg_merge.
+ *
+ * hg_prompt_attn: causal self-attention over whole prompts.  K, V: bf16 [rows, Hkv, D]; token t of a sequence attends to its tokens 0 .. t.  Tokens of a
+ * sequence from max_len (a host upper bound) on are not computed.
+ * hg_chunk_attn_paged: the n = q_off[b+1] - q_off[b] new tokens of a sequence are the last n of its lengths[b] rows in the paged cache, already written
+ * there; token t attends to rows [0, lengths[b] - (n-1-t)).  n = 1 is decode; a token that sees no row gets O = 0, LSE = -inf.  Rows above
+ * max_len are ignored (min(lengths[b], max_len) takes the place of lengths[b]); tokens of a sequence from max_new (a host upper bound) on are not computed.  The
+ * pool may hold 2^31 - 1 rows, bf16 or codes (weights are rounded to bf16 over either); pool rows that no sequence owns may hold anything, NaN included.
+ * In both, a key that a token does not see may hold anything, but the value rows of one sequence must be finite: they are multiplied with weights of zero.
+ * Both use the workspace, where there is one, to split long key ranges over more workgroups, and run without it.
+ *
+ * hg_page_slots: places for the new tokens.  lengths, counts: DEVICE int32[B], rows that sequence b has in the cache and new tokens that it brings
+ * (negative ones count as 0).  Row j of the sequence lives in page page_table[b * table_stride + j / page_size]; the pages that rows lengths[b] ..
+ * lengths[b] + counts[b] - 1 need beyond those in use are taken from free_pages (DEVICE int32[n_free]) in order, sequence after sequence, and entered.
+ * Out: q_off, the running sum of counts; slots (DEVICE int32[rows]), the pool row of each packed token, -1 behind the last one; new_lengths =
+ * lengths + counts; pages_used (DEVICE int32[1]), how many pages of the list were wanted.  More than n_free: the list was too short; the missing pages are entered as -1,
+ * their tokens have slot -1, and new_lengths counts only rows with a place.  Rows from table_stride * page_size on have none either.  Nothing but
+ * the new entries of page_table changes, so a call may be made again with a longer list.  new_lengths and q_off must not be lengths or counts.
+ *
+ * hg_kv_write_paged: pool row slots[i] = new row i, as bf16 or as codes (as in hg_kv_append_fp8); slots outside the pool are skipped.  No two tokens may
+ * have the same slot.  kv->page_table is not read.
+ */
+int hg_prompt_attn(hg_ctx* ctx, const void* Q, const void* K, const void* V, int64_t q_stride, int64_t kv_stride,
+                   const int32_t* q_off, int rows, int max_len, int B, int Hq, int Hkv, int D, float scale,
+                   void* O, int o_dtype, float* LSE);
+int hg_chunk_attn_paged(hg_ctx* ctx, const void* Q, int64_t q_stride, const int32_t* q_off, int rows,
+                        const hg_paged_kv* kv, const int32_t* lengths, int max_new, int max_len,
+                        int B, int Hq, int Hkv, int D, float scale, void* O, int o_dtype, float* LSE);
+int hg_page_slots(hg_ctx* ctx, const int32_t* lengths, const int32_t* counts, const int32_t* free_pages, int n_free,
+                  int page_size, int B, int rows, int32_t* page_table, int table_stride,
+                  int32_t* q_off, int32_t* slots, int32_t* new_lengths, int32_t* pages_used);
+int hg_kv_write_paged(hg_ctx* ctx, const void* Knew, const void* Vnew, int64_t stride, const int32_t* slots, int rows,
+                      const hg_paged_kv* kv, int Hkv, int D);
+
+/*
  * Non-decomposed comparison (the behaviour Sec. 1 and Sec. 2.3 attribute to per-sequence decode kernels):
  * same arguments and result as hg_hydragen_attn, but every sequence walks its whole key list
  * (shared blocks, then suffix) by itself, so shared rows are re-read once per sequence.

@@ -40,6 +40,7 @@ EXPORTS = (
     "hg_prefix_attn_grouped", "hg_suffix_attn", "hg_merge", "hg_hydragen_attn", "hg_naive_attn", "hg_read_stage_timings",
     "hg_strerror", "hg_suffix_attn_paged", "hg_hydragen_attn_paged", "hg_kv_append", "hg_kv_append_paged",
     "hg_debug_wide_plan", "hg_debug_wide_ranges", "hg_debug_wide_team", "hg_debug_item_runs", "hg_debug_suffix_plan", "hg_debug_fused_plan", "hg_debug_single_work", "hg_suffix_attn_fp8", "hg_hydragen_attn_fp8", "hg_kv_append_fp8",
+    "hg_prompt_attn", "hg_chunk_attn_paged", "hg_page_slots", "hg_kv_write_paged",
     "hg_hydragen_attn_static", "hg_debug_mfma_loop", "hg_debug_stream_read", "hg_debug_xcd_of_workgroups",
 )
 
@@ -118,6 +119,15 @@ def lib() -> ctypes.CDLL:
         L.hg_kv_append_fp8.restype = ci
         L.hg_kv_append_paged.argtypes = [vp, vp, vp, ctypes.POINTER(hg_paged_kv), vp, ci, ci, ci, ci]
         L.hg_kv_append_paged.restype = ci
+        i64 = ctypes.c_int64
+        L.hg_prompt_attn.argtypes = [vp, vp, vp, vp, i64, i64, vp, ci, ci, ci, ci, ci, ci, cf, vp, ci, vp]
+        L.hg_prompt_attn.restype = ci
+        L.hg_chunk_attn_paged.argtypes = [vp, vp, i64, vp, ci, ctypes.POINTER(hg_paged_kv), vp, ci, ci, ci, ci, ci, ci, cf, vp, ci, vp]
+        L.hg_chunk_attn_paged.restype = ci
+        L.hg_page_slots.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, vp, ci, vp, vp, vp, vp]
+        L.hg_page_slots.restype = ci
+        L.hg_kv_write_paged.argtypes = [vp, vp, vp, i64, vp, ci, ctypes.POINTER(hg_paged_kv), ci, ci]
+        L.hg_kv_write_paged.restype = ci
         L.hg_debug_wide_plan.argtypes = [ci] * 8 + [ctypes.POINTER(ci)]
         L.hg_debug_wide_plan.restype = ci
         L.hg_debug_wide_ranges.argtypes = [ci] * 8 + [ctypes.POINTER(ci), ctypes.POINTER(ci)]
@@ -540,6 +550,73 @@ def hg_kv_append_paged(ctx: Context, Knew, Vnew, kv: PagedKV, lengths, capacity:
     st = kv.c_struct()
     _check(lib().hg_kv_append_paged(ctx.h, _p(Knew), _p(Vnew), ctypes.byref(st), _p(lengths), capacity, B, Hkv, D),
            "hg_kv_append_paged")
+
+
+def _rows_of(t: torch.Tensor, dtype, name: str):
+    """(tokens, heads, D, elements from a token to the next) of a tensor whose tokens may lie further apart than they are long"""
+    if not t.is_cuda or t.dtype != dtype or t.ndim != 3:
+        raise TypeError(f"{name}: need a device tensor [tokens, heads, D] of {dtype}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    T, H, D = t.shape
+    step = t.stride(0) if T > 1 else H * D
+    if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D) or step < H * D or step % 8 or t.data_ptr() % 16:
+        raise ValueError(f"{name}: a token's heads must lie packed, tokens a multiple of 8 elements apart and 16-byte aligned: strides {t.stride()}")
+    return T, H, D, step
+
+
+def _packed_out(O, LSE, lead, D):
+    _want(O, O.dtype, lead + (D,), "O")
+    if LSE is not None:
+        _want(LSE, torch.float32, lead, "LSE")
+
+
+def hg_prompt_attn(ctx: Context, Q, K, V, q_off, max_len: int, O, LSE=None, scale: float = 0.0) -> None:
+    """Causal self-attention of packed prompts: Q [T, Hq, D], K and V [T, Hkv, D] (rows may lie further apart), q_off int32 [B + 1]."""
+    T, Hq, D, q_step = _rows_of(Q, torch.bfloat16, "Q")
+    Tk, Hkv, Dk, kv_step = _rows_of(K, torch.bfloat16, "K")
+    if (Tk, Dk) != (T, D) or _rows_of(V, torch.bfloat16, "V") != (T, Hkv, D, kv_step):
+        raise ValueError(f"K {tuple(K.shape)} and V {tuple(V.shape)} must have Q's tokens {tuple(Q.shape)} and each other's strides")
+    _want(q_off, torch.int32, (q_off.numel(),), "q_off")
+    _packed_out(O, LSE, (T, Hq), D)
+    _check(lib().hg_prompt_attn(ctx.h, _p(Q), _p(K), _p(V), q_step, kv_step, _p(q_off), T, max_len, q_off.numel() - 1, Hq, Hkv, D, scale,
+                                _p(O), _dtype_code(O), _p(LSE)), "hg_prompt_attn")
+
+
+def hg_chunk_attn_paged(ctx: Context, Q, q_off, kv: PagedKV, lengths, max_new: int, max_len: int, O, LSE=None, scale: float = 0.0) -> None:
+    """Attention of every sequence's new tokens, the last rows of its paged cache: Q [T, Hq, D], q_off int32 [B + 1], lengths int32 [B]."""
+    T, Hq, D, q_step = _rows_of(Q, torch.bfloat16, "Q")
+    B = q_off.numel() - 1
+    Hkv = _want_paged(kv, B, D)
+    _want(q_off, torch.int32, (B + 1,), "q_off"); _want(lengths, torch.int32, (B,), "lengths")
+    _packed_out(O, LSE, (T, Hq), D)
+    st = kv.c_struct()
+    _check(lib().hg_chunk_attn_paged(ctx.h, _p(Q), q_step, _p(q_off), T, ctypes.byref(st), _p(lengths), max_new, max_len, B, Hq, Hkv, D, scale,
+                                     _p(O), _dtype_code(O), _p(LSE)), "hg_chunk_attn_paged")
+
+
+def hg_page_slots(ctx: Context, lengths, counts, free_pages, page_size: int, page_table, q_off, slots, new_lengths, pages_used) -> None:
+    """Places for counts[b] new tokens of every sequence: fills in page_table, q_off [B + 1], slots [T], new_lengths [B] and pages_used [1]."""
+    B = lengths.numel()
+    for t, shape, name in ((lengths, (B,), "lengths"), (counts, (B,), "counts"), (free_pages, (free_pages.numel(),), "free_pages"),
+                           (q_off, (B + 1,), "q_off"), (slots, (slots.numel(),), "slots"), (new_lengths, (B,), "new_lengths"),
+                           (pages_used, (1,), "pages_used")):
+        _want(t, torch.int32, shape, name)
+    _want(page_table, torch.int32, name="page_table")
+    if page_table.ndim != 2 or page_table.shape[0] != B:
+        raise ValueError(f"page_table: need [B, stride], got {tuple(page_table.shape)}")
+    _check(lib().hg_page_slots(ctx.h, _p(lengths), _p(counts), _p(free_pages), free_pages.numel(), page_size, B, slots.numel(), _p(page_table),
+                               page_table.shape[1], _p(q_off), _p(slots), _p(new_lengths), _p(pages_used)), "hg_page_slots")
+
+
+def hg_kv_write_paged(ctx: Context, Knew, Vnew, slots, kv: PagedKV) -> None:
+    """Pool row slots[i] = new row i: Knew and Vnew bf16 [T, Hkv, D] (rows may lie further apart), slots int32 [T]; -1: nowhere."""
+    T, Hkv, D, step = _rows_of(Knew, torch.bfloat16, "Knew")
+    if _rows_of(Vnew, torch.bfloat16, "Vnew") != (T, Hkv, D, step):
+        raise ValueError(f"Vnew {tuple(Vnew.shape)} must have Knew's shape {tuple(Knew.shape)} and strides")
+    _want(slots, torch.int32, (T,), "slots")
+    dt = torch.uint8 if kv.kv_format == HG_KV_E4M3 else torch.bfloat16
+    _want(kv.K, dt, (kv.K.shape[0], Hkv, D), "paged K"); _want(kv.V, dt, kv.K.shape, "paged V")
+    st = kv.c_struct()
+    _check(lib().hg_kv_write_paged(ctx.h, _p(Knew), _p(Vnew), step, _p(slots), T, ctypes.byref(st), Hkv, D), "hg_kv_write_paged")
 
 
 def hg_debug_wide_plan(n_blocks: int, max_rows: int, max_seqs: int, Hkv: int, rows_per_seq: int, max_parts: int, slots_per_xcd: int,

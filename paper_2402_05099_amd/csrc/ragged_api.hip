@@ -1,0 +1,164 @@
+// Host side of the calls between a prompt and its first decode step: argument checks and the choice of kernels for hg_prompt_attn,
+// hg_chunk_attn_paged, hg_page_slots and hg_kv_write_paged.  As in api.hip: no device allocation, no host synchronisation, no copies.
+#include <math.h>
+#include <algorithm>
+
+#include "context.h"
+#include "hydragen.h"
+#include "ragged.h"
+
+namespace {
+
+using namespace hg;
+
+int rc_of(hipError_t e) { return e == hipSuccess ? HG_OK : HG_ERR_HIP; }
+
+bool positive_scale(float s) { return s > 0.f && s <= 3.0e38f; }
+
+// log2 of the rows per page; -1: not a power of two in [16, 1024]
+int page_shift(int page_size) {
+    for (int s = 4; s <= 10; ++s)
+        if (1 << s == page_size) return s;
+    return -1;
+}
+
+// Shapes and row distances that both attention calls have.
+int check_ragged(const hg_ctx* c, const void* Q, int64_t q_stride, const int32_t* q_off, int rows, int max_new, int B, int Hq, int Hkv, int D,
+                 const void* O, int o_dtype) {
+    if (!c || (o_dtype != HG_F32 && o_dtype != HG_BF16) || rows < 0 || max_new < 0 || B < 0 || Hq <= 0 || Hkv <= 0) return HG_ERR_INVALID_ARG;
+    if (D != 64 && D != 128) return HG_ERR_UNSUPPORTED;
+    if (Hq % Hkv != 0) return HG_ERR_UNSUPPORTED;
+    if ((int64_t)rows * Hq >= (1LL << 31) || B >= (1 << 24) || ((int64_t)rows * (Hq / Hkv) + 256LL * B) * Hkv >= (1LL << 31)) return HG_ERR_UNSUPPORTED;
+    if (rows > 0 && B > 0 && max_new > 0) {
+        if (!Q || !q_off || !O) return HG_ERR_INVALID_ARG;
+        if (q_stride < (int64_t)Hq * D || q_stride % 8 != 0 || reinterpret_cast<uintptr_t>(Q) % 16 != 0) return HG_ERR_INVALID_ARG;
+    }
+    return HG_OK;
+}
+
+// What is the same for both attention calls, from checked arguments.
+RaggedArgs ragged_args(const void* Q, int64_t q_stride, const int32_t* q_off, int rows, int max_new, int B, int Hq, int Hkv, int D, float scale,
+                       void* O, int o_dtype, float* LSE) {
+    RaggedArgs a{};
+    a.Q = static_cast<const uint16_t*>(Q);
+    a.q_stride = 2 * q_stride;
+    a.q_off = q_off;
+    a.rows = rows;
+    a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.G = Hq / Hkv;
+    a.max_new = max_new;
+    a.by_group = divider((unsigned)a.G);
+    a.by_heads = divider((unsigned)Hkv);
+    a.scale = scale > 0.f ? scale : 1.0f / sqrtf((float)D);
+    a.v_scale = 1.f;
+    a.out.O = O;
+    a.out.LSE = LSE;
+    a.out.bf16 = o_dtype == HG_BF16;
+    a.nsplit = 1;
+    a.chunk = 0x3fffffff;
+    return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+int hg_prompt_attn(hg_ctx* c, const void* Q, const void* K, const void* V, int64_t q_stride, int64_t kv_stride, const int32_t* seq_off, int rows,
+                   int max_len, int B, int Hq, int Hkv, int D, float scale, void* O, int o_dtype, float* LSE) {
+    const int rc = check_ragged(c, Q, q_stride, seq_off, rows, max_len, B, Hq, Hkv, D, O, o_dtype);
+    if (rc) return rc;
+    if (rows == 0 || B == 0 || max_len == 0) return HG_OK;
+    if (!K || !V || kv_stride < (int64_t)Hkv * D || kv_stride % 8 != 0 ||
+        (reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V)) % 16 != 0) return HG_ERR_INVALID_ARG;
+    if (hipSetDevice(c->device) != hipSuccess) return HG_ERR_HIP;
+    RaggedArgs a = ragged_args(Q, q_stride, seq_off, rows, max_len, B, Hq, Hkv, D, scale, O, o_dtype, LSE);
+    a.K = static_cast<const unsigned char*>(K);
+    a.V = static_cast<const unsigned char*>(V);
+    a.kv_stride = 2 * kv_stride;
+    a.max_len = max_len;
+    return rc_of(launch_ragged_tiles(a, D, false, c->stream));
+}
+
+int hg_chunk_attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_t* q_off, int rows, const hg_paged_kv* kv, const int32_t* lengths,
+                        int max_new, int max_len, int B, int Hq, int Hkv, int D, float scale, void* O, int o_dtype, float* LSE) {
+    const int rc = check_ragged(c, Q, q_stride, q_off, rows, max_new, B, Hq, Hkv, D, O, o_dtype);
+    if (rc) return rc;
+    if (!kv || max_len < 0) return HG_ERR_INVALID_ARG;
+    const bool codes = kv->kv_format == HG_KV_E4M3;
+    if (!codes && kv->kv_format != HG_KV_BF16) return HG_ERR_INVALID_ARG;
+    if (codes && (!positive_scale(kv->k_scale) || !positive_scale(kv->v_scale))) return HG_ERR_INVALID_ARG;
+    const int shift = page_shift(kv->page_size);
+    if (shift < 0 || kv->n_pages < 0 || kv->table_stride < 0) return HG_ERR_INVALID_ARG;
+    if ((int64_t)kv->n_pages * kv->page_size >= (1LL << 31) || (int64_t)kv->table_stride * kv->page_size >= (1LL << 31)) return HG_ERR_UNSUPPORTED;
+    if (rows == 0 || B == 0 || max_new == 0) return HG_OK;
+    if (!lengths || !kv->K || !kv->V || !kv->page_table || kv->n_pages < 1 || (int64_t)kv->table_stride * kv->page_size < std::max(max_len, 1) ||
+        (reinterpret_cast<uintptr_t>(kv->K) | reinterpret_cast<uintptr_t>(kv->V)) % 16 != 0) return HG_ERR_INVALID_ARG;
+    if (hipSetDevice(c->device) != hipSuccess) return HG_ERR_HIP;
+    RaggedArgs a = ragged_args(Q, q_stride, q_off, rows, max_new, B, Hq, Hkv, D, scale, O, o_dtype, LSE);
+    a.K = static_cast<const unsigned char*>(kv->K);
+    a.V = static_cast<const unsigned char*>(kv->V);
+    a.kv_stride = (int64_t)Hkv * D * (codes ? 1 : 2);
+    a.lengths = lengths;
+    a.pg.table = kv->page_table;
+    a.pg.shift = shift;
+    a.pg.stride = kv->table_stride;
+    a.pg.n_pages = kv->n_pages;
+    a.max_len = max_len;
+    if (codes) {
+        a.scale *= kv->k_scale;
+        a.v_scale = kv->v_scale;
+    }
+    return rc_of(launch_ragged_tiles(a, D, codes, c->stream));
+}
+
+int hg_page_slots(hg_ctx* c, const int32_t* lengths, const int32_t* counts, const int32_t* free_pages, int n_free, int page_size, int B, int rows,
+                  int32_t* page_table, int table_stride, int32_t* q_off, int32_t* slots, int32_t* new_lengths, int32_t* pages_used) {
+    const int shift = page_shift(page_size);
+    if (!c || shift < 0 || n_free < 0 || B < 0 || rows < 0 || table_stride < 0 || !q_off || !pages_used) return HG_ERR_INVALID_ARG;
+    if ((int64_t)table_stride * page_size >= (1LL << 31)) return HG_ERR_UNSUPPORTED;
+    if (B > 0 && (!lengths || !counts || !new_lengths || (table_stride > 0 && !page_table))) return HG_ERR_INVALID_ARG;
+    if ((rows > 0 && !slots) || (n_free > 0 && !free_pages)) return HG_ERR_INVALID_ARG;
+    // every workgroup reads the lengths and the counts: none may write over them
+    if (B > 0 && (new_lengths == lengths || new_lengths == counts || q_off == lengths || q_off == counts)) return HG_ERR_INVALID_ARG;
+    if (hipSetDevice(c->device) != hipSuccess) return HG_ERR_HIP;
+    SlotArgs a{};
+    a.lengths = lengths; a.counts = counts; a.free_pages = free_pages; a.n_free = n_free;
+    a.table = page_table; a.stride = table_stride; a.shift = shift;
+    a.B = B; a.rows = rows;
+    a.q_off = q_off; a.slots = slots; a.new_lengths = new_lengths; a.pages_used = pages_used;
+    return rc_of(launch_page_slots(a, c->stream));
+}
+
+int hg_kv_write_paged(hg_ctx* c, const void* Knew, const void* Vnew, int64_t stride, const int32_t* slots, int rows, const hg_paged_kv* kv, int Hkv,
+                      int D) {
+    if (!c || !kv || rows < 0 || Hkv <= 0) return HG_ERR_INVALID_ARG;
+    if (D != 64 && D != 128) return HG_ERR_UNSUPPORTED;
+    const bool codes = kv->kv_format == HG_KV_E4M3;
+    if (!codes && kv->kv_format != HG_KV_BF16) return HG_ERR_INVALID_ARG;
+    if (codes && (!positive_scale(kv->k_scale) || !positive_scale(kv->v_scale))) return HG_ERR_INVALID_ARG;
+    if (page_shift(kv->page_size) < 0 || kv->n_pages < 0) return HG_ERR_INVALID_ARG;
+    if ((int64_t)kv->n_pages * kv->page_size >= (1LL << 31) || (int64_t)rows * Hkv * D >= (1LL << 33)) return HG_ERR_UNSUPPORTED;
+    if (rows == 0) return HG_OK;
+    if (!Knew || !Vnew || !slots || stride < (int64_t)Hkv * D || stride % 8 != 0 ||
+        (reinterpret_cast<uintptr_t>(Knew) | reinterpret_cast<uintptr_t>(Vnew)) % 16 != 0) return HG_ERR_INVALID_ARG;
+    if (kv->n_pages > 0 && (!kv->K || !kv->V || (reinterpret_cast<uintptr_t>(kv->K) | reinterpret_cast<uintptr_t>(kv->V)) % 16 != 0))
+        return HG_ERR_INVALID_ARG;
+    if (kv->n_pages == 0) return HG_OK;      // no row has a place
+    if (hipSetDevice(c->device) != hipSuccess) return HG_ERR_HIP;
+    WriteArgs a{};
+    a.Knew = static_cast<const uint16_t*>(Knew);
+    a.Vnew = static_cast<const uint16_t*>(Vnew);
+    a.stride = stride;
+    a.slots = slots;
+    a.K = static_cast<uint16_t*>(kv->K);
+    a.V = static_cast<uint16_t*>(kv->V);
+    a.pool_rows = (int64_t)kv->n_pages * kv->page_size;
+    a.rows = rows;
+    a.vec = Hkv * D / 8;
+    a.by_vec = divider((unsigned)a.vec);
+    a.codes = codes;
+    a.k_scale = kv->k_scale;
+    a.v_scale = kv->v_scale;
+    return rc_of(launch_kv_write(a, c->stream));
+}
+
+}  // extern "C"
