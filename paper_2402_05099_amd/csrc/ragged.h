@@ -25,10 +25,23 @@ struct RaggedArgs {
     float scale;              // of the scores, the K scale of codes included
     float v_scale;            // of the values (1 for bf16 rows)
     OutDev out;               // packed rows t * Hq + h; part index = split
-    int nsplit, chunk;        // key ranges a tile is split into, and their length (a multiple of 64)
+    int nsplit, chunk;        // key ranges a tile is split into, and their length (a multiple of 128)
+
+    // Sequences of at most few_rows query rows to a KV head (paged cache): ragged_rows.hip.  The tiles' kernel takes the others.
+    int few_rows;             // 0: none
+    int few_tokens;           // tokens that such a sequence has at most
+    int tile_rows, tiles;     // rows of a tile, 16 or 32, and tiles of few_tokens tokens
+    int wavefronts;           // of a workgroup: 4 or 8
+    Divider by_seq;           // division by tiles * nsplit
+    float* part_O;            // nsplit > 1: partial results [nsplit][part_rows][D], [nsplit][part_rows], part_rows = B * few_tokens * Hq
+    float* part_L;
+    int64_t part_rows;
+    Divider by_q_heads, by_tokens;      // division by Hq and by few_tokens
 };
+constexpr int kFewRows = 64;
 
 // ---- launchers (ragged.hip) ----
+hipError_t launch_ragged_rows(const RaggedArgs& a, int D, bool codes, hipStream_t s);       // (ragged_rows.hip)
 hipError_t launch_ragged_tiles(const RaggedArgs& a, int D, bool codes, hipStream_t s);
 
 // ---- block tables, slots and the write into a paged cache (pages.hip) ----

@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256) void ragged_tiles_kernel(RaggedArgs a) {
     if (!ragged_tile<kRows>(a, number, b, tile)) return;
     const RaggedSeq sq = ragged_seq(a, b);
     const int nrows = sq.take * a.G, row0 = tile * kRows;
-    if (row0 >= nrows) return;
+    if (row0 >= nrows || nrows <= a.few_rows) return;
 
     const int tid = threadIdx.x, l = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -58,6 +58,35 @@ RaggedArgs ragged_args(const void* Q, int64_t q_stride, const int32_t* q_off, in
     return a;
 }
 
+// The sequences of at most kFewRows query rows to a KV head: how their keys are split, and the launch.  a.few_rows is set for the kernel that takes the others.
+int few_rows(const hg_ctx* c, RaggedArgs& all, int D, bool codes) {
+    RaggedArgs a = all;
+    a.few_rows = all.few_rows = kFewRows;
+    a.few_tokens = std::min(a.max_new, std::max(kFewRows / a.G, 1));
+    const int most = std::min(a.few_tokens * a.G, kFewRows);
+    if (a.G > kFewRows) return HG_OK;      // even a single token has more
+    a.tile_rows = most <= 16 ? 16 : 32;
+    a.tiles = (most + a.tile_rows - 1) / a.tile_rows;
+    // enough workgroups to fill the chip twice, so that contexts of different lengths even out; no shorter ranges than 512 keys
+    const int64_t wgs = (int64_t)a.B * a.tiles * a.Hkv;
+    a.part_rows = (int64_t)a.B * a.few_tokens * a.Hq;
+    const int64_t room = c->ws ? (int64_t)(c->ws_bytes / ((size_t)a.part_rows * (D + 1) * sizeof(float))) : 0;
+    const int64_t want = std::min<int64_t>({(1024 + wgs - 1) / wgs, (a.max_len + 511) / 512, room, 256});
+    a.nsplit = a.part_rows < (1LL << 31) && want > 1 ? (int)want : 1;
+    if (a.nsplit > 1) {
+        a.chunk = ((a.max_len + a.nsplit - 1) / a.nsplit + 127) / 128 * 128;
+        a.nsplit = (a.max_len + a.chunk - 1) / a.chunk;
+    }
+    if (a.nsplit == 1) a.chunk = 0x3fffffff;
+    a.wavefronts = wgs * a.nsplit <= 256 ? 8 : 4;
+    a.by_seq = divider((unsigned)(a.tiles * a.nsplit));
+    a.by_q_heads = divider((unsigned)a.Hq);
+    a.by_tokens = divider((unsigned)a.few_tokens);
+    a.part_O = reinterpret_cast<float*>(c->ws);
+    a.part_L = a.part_O + (int64_t)a.nsplit * a.part_rows * D;
+    return rc_of(launch_ragged_rows(a, D, codes, c->stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -107,6 +136,9 @@ int hg_chunk_attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_
         a.scale *= kv->k_scale;
         a.v_scale = kv->v_scale;
     }
+    if ((int64_t)Hkv * D * 64 >= (1LL << 31)) return HG_ERR_UNSUPPORTED;
+    int rc2 = few_rows(c, a, D, codes);
+    if (rc2 || (int64_t)std::min(max_new, rows) * a.G <= kFewRows) return rc2;
     return rc_of(launch_ragged_tiles(a, D, codes, c->stream));
 }
 
