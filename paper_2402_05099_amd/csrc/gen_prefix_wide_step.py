@@ -12,21 +12,25 @@ instead of running the two kinds back to back.  The exponentials need no result 
 none of them, so they go evenly into all the gaps, and the row sum is there before the weights are multiplied with anything: it
 says whether they have to be taken again against a larger maximum, which spares every step the search for it.
 
-usage: gen_prefix_wide_step.py [D [out.inc [vector-ALU cycles per gap]]]     (no arguments: both files)
+The ragged form (ragged_wide_step.inc, ragged_wide_step_d64.inc, for ragged_wide_impl.h) has the same order with two differences: its copies are the kernel's
+own (issue_k, issue_v and, between them, work_k and work_v, which are empty but over 8-bit rows), and the sum of the rounded weights is taken beside that of the unrounded ones.
+
+usage: gen_prefix_wide_step.py [D [out.inc [vector-ALU cycles per gap]]]     (no arguments: all files)
 """
 import os
 import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 DEFAULT_OUT = {128: os.path.join(HERE, "prefix_wide_step.inc"), 64: os.path.join(HERE, "prefix_wide_step_d64.inc")}
+RAGGED_OUT = {128: os.path.join(HERE, "ragged_wide_step.inc"), 64: os.path.join(HERE, "ragged_wide_step_d64.inc")}
 DEFAULT_CAP = {128: 22.0, 64: 44.0}     # a 32x32x16 MFMA occupies the matrix pipe for 32 cycles
 XYZW = "xyzw"
 # measured issue cost of one wave64 instruction, cycles
 C_FMA, C_EXP, C_CVT, C_ADD = 5.2, 8.8, 5.2, 4.9
 
 
-def build(D=128, CAP=None):
-    CAP = DEFAULT_CAP[D] if CAP is None else CAP
+def build(D=128, CAP=None, ragged=False):
+    CAP = (DEFAULT_CAP[D] * (1.12 if ragged else 1.0)) if CAP is None else CAP
     wide = D == 128
     # score tile(s) of a stage as the kernel names them
     cur_t = ["Scur"] if wide else ["Scur.a", "Scur.b"]
@@ -53,10 +57,16 @@ def build(D=128, CAP=None):
         mf.append([value(i), [], [v_load(i - 4, "slot1")]])
     # the copy that keeps the ring AHEAD stages ahead (the copy cursor may already be in a later piece): scalar address
     # arithmetic in gap 0, the two copy instructions in gaps 1 and 3
-    mf[0][1].extend(["const int64_t cp_off = (int64_t)min(cur.ks + cur.t * KT, cur.kwin) * rstride_b;",
-                     "const unsigned cp_dst = ldsw + (unsigned)((slot + AHEAD) & (NS - 1)) * STB;"])
-    mf[1][1].append("copy16(cur.Kg + cp_off, cur.voffK, cp_dst);")
-    mf[3][1].append("copy16(cur.Vg + cp_off, cur.voffV, cp_dst + VRING);")
+    if ragged:
+        mf[0][1].append("issue_k(j, slot);")
+        mf[2][1].append("issue_v(j, slot);")
+        mf[6][1].append("work_k(j, slot);")
+        mf[9][1].append("work_v(j, slot);")
+    else:
+        mf[0][1].extend(["const int64_t cp_off = (int64_t)min(cur.ks + cur.t * KT, cur.kwin) * rstride_b;",
+                         "const unsigned cp_dst = ldsw + (unsigned)((slot + AHEAD) & (NS - 1)) * STB;"])
+        mf[1][1].append("copy16(cur.Kg + cp_off, cur.voffK, cp_dst);")
+        mf[3][1].append("copy16(cur.Vg + cp_off, cur.voffV, cp_dst + VRING);")
 
     work = []     # (cycles, statement)
     n = 0
@@ -76,6 +86,8 @@ def build(D=128, CAP=None):
             work.append((C_EXP, f"const float eb{k} = __builtin_amdgcn_exp2f(xb{k});"))
         for p, k in enumerate(ids):
             work.append((C_CVT, f"pn[{h}].{XYZW[p]} = pack_bf16_pair(ea{k}, eb{k});"))
+            if ragged:      # (the pair goes through a variable of its own, see sum_of_pair)
+                work.append((C_ADD, f"rsum = sum_of_pair(pn[{h}].{XYZW[p]}, {'0.f' if k == 0 else 'rsum'});"))
             if k == 0:
                 pending += ["ea0", "eb0"]
             elif k == 1:
@@ -93,7 +105,7 @@ def build(D=128, CAP=None):
         out.append(f"// gap {g}")
         out.append(stmt)
         out.extend(pre)
-        if g == 0:
+        if g == 0 and not ragged:
             out.append("if (kMasked) mask_stage(Scur, j + 1);")
         budget += CAP
         while wi < len(work) and budget > 0:
@@ -111,9 +123,15 @@ def write(D, out=None, cap=None):
         f.write(f"// Generated by gen_prefix_wide_step.py (one pipeline step of prefix_wide_impl.h, D = {D}); do not edit by hand.\n" + build(D, cap))
 
 
+def write_ragged(D):
+    with open(RAGGED_OUT[D], "w") as f:
+        f.write(f"// Generated by gen_prefix_wide_step.py (one pipeline step of ragged_wide_impl.h, D = {D}); do not edit by hand.\n" + build(D, ragged=True))
+
+
 if __name__ == "__main__":
     if len(sys.argv) > 1:
         write(int(sys.argv[1]), sys.argv[2] if len(sys.argv) > 2 else None, float(sys.argv[3]) if len(sys.argv) > 3 else None)
     else:
-        write(128)
-        write(64)
+        for D in (128, 64):
+            write(D)
+            write_ragged(D)

@@ -24,12 +24,12 @@ struct RaggedArgs {
     Divider by_group, by_heads;      // division by G and by Hkv
     float scale;              // of the scores, the K scale of codes included
     float v_scale;            // of the values (1 for bf16 rows)
-    OutDev out;               // packed rows t * Hq + h; part index = split
-    int nsplit, chunk;        // key ranges a tile is split into, and their length (a multiple of 128)
+    OutDev out;               // packed rows t * Hq + h
 
     // Sequences of at most few_rows query rows to a KV head (paged cache): ragged_rows.hip.  The tiles' kernel takes the others.
     int few_rows;             // 0: none
     int few_tokens;           // tokens that such a sequence has at most
+    int nsplit, chunk;        // key ranges a tile is split into, and their length (a multiple of 128)
     int tile_rows, tiles;     // rows of a tile, 16 or 32, and tiles of few_tokens tokens
     int wavefronts;           // of a workgroup: 4 or 8
     Divider by_seq;           // division by tiles * nsplit
@@ -37,12 +37,22 @@ struct RaggedArgs {
     float* part_L;
     int64_t part_rows;
     Divider by_q_heads, by_tokens;      // division by Hq and by few_tokens
+
+    // The others, and prompts: ragged_wide_impl.h, tiles of kTile rows.
+    int tiles_all;            // numbers of tiles (ragged_tile)
+    Divider by_heads8;        // division by Hkv / 8 where Hkv is a multiple of 8
+    int tile_nsplit, tile_chunk;        // key ranges of a tile and their length (a multiple of 64)
+    float* tile_part_O;       // tile_nsplit > 1: partial results [tile_nsplit][rows * Hq][D], [tile_nsplit][rows * Hq]
+    float* tile_part_L;
 };
+constexpr int kTile = 128;
 constexpr int kFewRows = 64;
 
-// ---- launchers (ragged.hip) ----
-hipError_t launch_ragged_rows(const RaggedArgs& a, int D, bool codes, hipStream_t s);       // (ragged_rows.hip)
-hipError_t launch_ragged_tiles(const RaggedArgs& a, int D, bool codes, hipStream_t s);
+// ---- launchers ----
+hipError_t launch_ragged_rows(const RaggedArgs& a, int D, bool codes, hipStream_t s);       // ragged_rows.hip: sequences of few rows, with their join
+hipError_t launch_ragged_wide(const RaggedArgs& a, bool codes, hipStream_t s);              // ragged_wide.hip, D = 128: the others' tiles
+hipError_t launch_ragged_wide_d64(const RaggedArgs& a, bool codes, hipStream_t s);          // ragged_wide_d64.hip
+hipError_t launch_ragged_join(const RaggedArgs& a, int D, hipStream_t s);                   // ragged_rows.hip: the parts of the others' rows
 
 // ---- block tables, slots and the write into a paged cache (pages.hip) ----
 struct SlotArgs {

@@ -11,6 +11,8 @@ namespace {
 
 using namespace hg;
 
+constexpr int kAllKeys = 0x3fffffff;      // longer than any key range
+
 int rc_of(hipError_t e) { return e == hipSuccess ? HG_OK : HG_ERR_HIP; }
 
 bool positive_scale(float s) { return s > 0.f && s <= 3.0e38f; }
@@ -53,38 +55,65 @@ RaggedArgs ragged_args(const void* Q, int64_t q_stride, const int32_t* q_off, in
     a.out.O = O;
     a.out.LSE = LSE;
     a.out.bf16 = o_dtype == HG_BF16;
-    a.nsplit = 1;
-    a.chunk = 0x3fffffff;
+    a.nsplit = a.tile_nsplit = 1;
+    a.chunk = a.tile_chunk = kAllKeys;
+    a.tiles_all = (int)ragged_tiles(rows, a.G, B, kTile);
+    a.by_heads8 = divider((unsigned)std::max(Hkv / 8, 1));
     return a;
 }
 
+// Workspace that is left: partial results are taken from it in turn.
+struct Room {
+    float* p;
+    size_t floats;
+    float* take(size_t n) {
+        float* const at = p;
+        p += n;
+        floats -= n;
+        return at;
+    }
+};
+Room room_of(const hg_ctx* c) { return Room{reinterpret_cast<float*>(c->ws), c->ws ? c->ws_bytes / sizeof(float) : 0}; }
+
+// Ranges of at least `least` keys, a multiple of `step` long, for `want` of them, and where their parts go.
+void split_keys(int64_t want, int max_len, int least, int step, int64_t rows, int D, Room& room, int& nsplit, int& chunk, float*& O, float*& L) {
+    const size_t per = (size_t)rows * (D + 1);
+    const int64_t most = std::min<int64_t>({want, (max_len + least - 1) / least, (int64_t)(per ? room.floats / per : 0), 256});
+    if (most <= 1 || rows >= (1LL << 31)) return;
+    chunk = (int)(((max_len + most - 1) / most + step - 1) / step * step);
+    nsplit = (max_len + chunk - 1) / chunk;
+    O = room.take((size_t)nsplit * rows * D);
+    L = room.take((size_t)nsplit * rows);
+}
+
 // The sequences of at most kFewRows query rows to a KV head: how their keys are split, and the launch.  a.few_rows is set for the kernel that takes the others.
-int few_rows(const hg_ctx* c, RaggedArgs& all, int D, bool codes) {
-    RaggedArgs a = all;
-    a.few_rows = all.few_rows = kFewRows;
-    a.few_tokens = std::min(a.max_new, std::max(kFewRows / a.G, 1));
-    const int most = std::min(a.few_tokens * a.G, kFewRows);
+int run_few_rows(const hg_ctx* c, RaggedArgs& a, int D, bool codes, Room& room) {
+    a.few_rows = kFewRows;
     if (a.G > kFewRows) return HG_OK;      // even a single token has more
+    a.few_tokens = std::min(a.max_new, kFewRows / a.G);
+    const int most = a.few_tokens * a.G;
     a.tile_rows = most <= 16 ? 16 : 32;
     a.tiles = (most + a.tile_rows - 1) / a.tile_rows;
     // enough workgroups to fill the chip twice, so that contexts of different lengths even out; no shorter ranges than 512 keys
     const int64_t wgs = (int64_t)a.B * a.tiles * a.Hkv;
     a.part_rows = (int64_t)a.B * a.few_tokens * a.Hq;
-    const int64_t room = c->ws ? (int64_t)(c->ws_bytes / ((size_t)a.part_rows * (D + 1) * sizeof(float))) : 0;
-    const int64_t want = std::min<int64_t>({(1024 + wgs - 1) / wgs, (a.max_len + 511) / 512, room, 256});
-    a.nsplit = a.part_rows < (1LL << 31) && want > 1 ? (int)want : 1;
-    if (a.nsplit > 1) {
-        a.chunk = ((a.max_len + a.nsplit - 1) / a.nsplit + 127) / 128 * 128;
-        a.nsplit = (a.max_len + a.chunk - 1) / a.chunk;
-    }
-    if (a.nsplit == 1) a.chunk = 0x3fffffff;
+    split_keys((1024 + wgs - 1) / wgs, a.max_len, 512, 128, a.part_rows, D, room, a.nsplit, a.chunk, a.part_O, a.part_L);
     a.wavefronts = wgs * a.nsplit <= 256 ? 8 : 4;
     a.by_seq = divider((unsigned)(a.tiles * a.nsplit));
     a.by_q_heads = divider((unsigned)a.Hq);
     a.by_tokens = divider((unsigned)a.few_tokens);
-    a.part_O = reinterpret_cast<float*>(c->ws);
-    a.part_L = a.part_O + (int64_t)a.nsplit * a.part_rows * D;
     return rc_of(launch_ragged_rows(a, D, codes, c->stream));
+}
+
+// The others, and prompts.
+int run_tiles(const hg_ctx* c, RaggedArgs& a, int D, bool codes, Room& room) {
+    // two workgroups to a CU; tiles of sequences with more than few_rows rows, from the host's bounds
+    const int64_t tiles = ((int64_t)a.rows * a.G + kTile - 1) / kTile + std::min<int64_t>(a.B, (int64_t)a.rows * a.G / (a.few_rows + 1));
+    const int64_t wgs = std::max<int64_t>(1, tiles * a.Hkv);
+    split_keys(wgs >= 512 ? 1 : (1024 + wgs - 1) / wgs, a.max_len, 512, 64, (int64_t)a.rows * a.Hq, D, room, a.tile_nsplit, a.tile_chunk, a.tile_part_O, a.tile_part_L);
+    const int rc = rc_of(D == 128 ? launch_ragged_wide(a, codes, c->stream) : launch_ragged_wide_d64(a, codes, c->stream));
+    if (rc || a.tile_nsplit == 1) return rc;
+    return rc_of(launch_ragged_join(a, D, c->stream));
 }
 
 }  // namespace
@@ -98,13 +127,15 @@ int hg_prompt_attn(hg_ctx* c, const void* Q, const void* K, const void* V, int64
     if (rows == 0 || B == 0 || max_len == 0) return HG_OK;
     if (!K || !V || kv_stride < (int64_t)Hkv * D || kv_stride % 8 != 0 ||
         (reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V)) % 16 != 0) return HG_ERR_INVALID_ARG;
+    if (kv_stride >= (1LL << 26)) return HG_ERR_UNSUPPORTED;      // (a copy's rows lie within 32 bits of each other)
     if (hipSetDevice(c->device) != hipSuccess) return HG_ERR_HIP;
     RaggedArgs a = ragged_args(Q, q_stride, seq_off, rows, max_len, B, Hq, Hkv, D, scale, O, o_dtype, LSE);
     a.K = static_cast<const unsigned char*>(K);
     a.V = static_cast<const unsigned char*>(V);
     a.kv_stride = 2 * kv_stride;
     a.max_len = max_len;
-    return rc_of(launch_ragged_tiles(a, D, false, c->stream));
+    Room room = room_of(c);
+    return run_tiles(c, a, D, false, room);
 }
 
 int hg_chunk_attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_t* q_off, int rows, const hg_paged_kv* kv, const int32_t* lengths,
@@ -117,7 +148,9 @@ int hg_chunk_attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_
     if (codes && (!positive_scale(kv->k_scale) || !positive_scale(kv->v_scale))) return HG_ERR_INVALID_ARG;
     const int shift = page_shift(kv->page_size);
     if (shift < 0 || kv->n_pages < 0 || kv->table_stride < 0) return HG_ERR_INVALID_ARG;
-    if ((int64_t)kv->n_pages * kv->page_size >= (1LL << 31) || (int64_t)kv->table_stride * kv->page_size >= (1LL << 31)) return HG_ERR_UNSUPPORTED;
+    if ((int64_t)kv->n_pages * kv->page_size >= (1LL << 31) || (int64_t)kv->table_stride * kv->page_size >= (1LL << 31) || max_len >= kAllKeys ||
+        (int64_t)Hkv * D * 32 >= (1LL << 31))
+        return HG_ERR_UNSUPPORTED;
     if (rows == 0 || B == 0 || max_new == 0) return HG_OK;
     if (!lengths || !kv->K || !kv->V || !kv->page_table || kv->n_pages < 1 || (int64_t)kv->table_stride * kv->page_size < std::max(max_len, 1) ||
         (reinterpret_cast<uintptr_t>(kv->K) | reinterpret_cast<uintptr_t>(kv->V)) % 16 != 0) return HG_ERR_INVALID_ARG;
@@ -136,10 +169,10 @@ int hg_chunk_attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_
         a.scale *= kv->k_scale;
         a.v_scale = kv->v_scale;
     }
-    if ((int64_t)Hkv * D * 64 >= (1LL << 31)) return HG_ERR_UNSUPPORTED;
-    int rc2 = few_rows(c, a, D, codes);
+    Room room = room_of(c);
+    const int rc2 = run_few_rows(c, a, D, codes, room);
     if (rc2 || (int64_t)std::min(max_new, rows) * a.G <= kFewRows) return rc2;
-    return rc_of(launch_ragged_tiles(a, D, codes, c->stream));
+    return run_tiles(c, a, D, codes, room);
 }
 
 int hg_page_slots(hg_ctx* c, const int32_t* lengths, const int32_t* counts, const int32_t* free_pages, int n_free, int page_size, int B, int rows,

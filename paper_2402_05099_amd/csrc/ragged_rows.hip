@@ -31,6 +31,20 @@ struct RowsGeo {
     static constexpr int bytes(int nw) { return nw * (SLOT + 2 * TR * 4); }
 };
 
+// Columns 8 c8 .. + 7 of a row's result
+template <int D>
+__device__ __forceinline__ void store_row8(const OutDev& out, int64_t row, int c8, const float (&o)[8], float lse) {
+    if (out.bf16) {
+        *reinterpret_cast<uintx4*>(static_cast<uint16_t*>(out.O) + row * D + 8 * c8) =
+            uintx4{pack_pair(o[0], o[1]), pack_pair(o[2], o[3]), pack_pair(o[4], o[5]), pack_pair(o[6], o[7])};
+    } else {
+        float* const O = static_cast<float*>(out.O) + row * D + 8 * c8;
+        *reinterpret_cast<float4*>(O) = make_float4(o[0], o[1], o[2], o[3]);
+        *reinterpret_cast<float4*>(O + 4) = make_float4(o[4], o[5], o[6], o[7]);
+    }
+    if (out.LSE && c8 == 0) out.LSE[row] = lse;
+}
+
 }  // namespace
 
 template <int D, bool CODES, int TR, int NW>
@@ -222,33 +236,13 @@ __global__ __launch_bounds__(64 * NW) void ragged_rows_kernel(RaggedArgs a) {
             if (c8 == 0) a.part_L[(int64_t)sp * a.part_rows + at] = lse;
             continue;
         }
-        if (a.out.bf16) {
-            *reinterpret_cast<uintx4*>(static_cast<uint16_t*>(a.out.O) + at * D + 8 * c8) =
-                uintx4{pack_pair(o[0], o[1]), pack_pair(o[2], o[3]), pack_pair(o[4], o[5]), pack_pair(o[6], o[7])};
-        } else {
-            float* const O = static_cast<float*>(a.out.O) + at * D + 8 * c8;
-            *reinterpret_cast<float4*>(O) = make_float4(o[0], o[1], o[2], o[3]);
-            *reinterpret_cast<float4*>(O + 4) = make_float4(o[4], o[5], o[6], o[7]);
-        }
-        if (a.out.LSE && c8 == 0) a.out.LSE[at] = lse;
+        store_row8<D>(a.out, at, c8, o, lse);
     }
 }
 
-// Joins the parts of the rows that ragged_rows_kernel computed (Eq. 5): D / 8 lanes per row, a workgroup of 256 threads takes 2048 / D rows of the
-// places for few_tokens tokens of every sequence.  Part p holds the keys from p * chunk on, so those of a row are its first ceil(seen / chunk).
+// One row's parts joined by Eq. 5: D / 8 lanes of eight columns.  Part p of row `at` is O[p * part_rows + at], L[p * part_rows + at].
 template <int D>
-__global__ __launch_bounds__(256) void ragged_merge_kernel(RaggedArgs a) {
-    constexpr int LPR = D / 8;
-    const int64_t at = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
-    if (at >= a.part_rows) return;
-    const int c8 = threadIdx.x % LPR;
-    const int bt = (int)a.by_q_heads.of((unsigned)at), h = (int)at - bt * a.Hq;
-    const int b = (int)a.by_tokens.of((unsigned)bt), tok = bt - b * a.few_tokens;
-    const int q0 = min(max(a.q_off[b], 0), a.rows);
-    const int n = min(max(a.q_off[b + 1], q0), a.rows) - q0, take = min(n, a.max_new);
-    if (tok >= take || take * a.G > a.few_rows) return;
-    const int seen = max(min(a.lengths[b], a.max_len), 0) - (n - 1 - tok);
-    const int parts = seen > 0 ? min((seen + a.chunk - 1) / a.chunk, a.nsplit) : 0;
+__device__ __forceinline__ void join_row(const float* O, const float* L, int64_t part_rows, int64_t at, int parts, int c8, const OutDev& out, int64_t row) {
     float m = -INFINITY, den = 0.f, o[8] = {};
     constexpr int U = 4;
     for (int p0 = 0; p0 < parts; p0 += U) {
@@ -256,17 +250,17 @@ __global__ __launch_bounds__(256) void ragged_merge_kernel(RaggedArgs a) {
         float4 x[U][2];
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            const int p = min(p0 + k, parts - 1);
-            li[k] = a.part_L[(int64_t)p * a.part_rows + at];
-            const float4* const O = reinterpret_cast<const float4*>(a.part_O + ((int64_t)p * a.part_rows + at) * D + 8 * c8);
-            x[k][0] = O[0];
-            x[k][1] = O[1];
+            const int64_t i = (int64_t)min(p0 + k, parts - 1) * part_rows + at;
+            li[k] = L[i];
+            const float4* const src = reinterpret_cast<const float4*>(O + i * D + 8 * c8);
+            x[k][0] = src[0];
+            x[k][1] = src[1];
             if (p0 + k >= parts) li[k] = -INFINITY;
         }
         float gm = m;
 #pragma unroll
         for (int k = 0; k < U; ++k) gm = fmaxf(gm, li[k]);
-        if (gm == -INFINITY) continue;
+        if (gm == -INFINITY) continue;      // (parts without a key have O = 0 and LSE = -inf)
         const float old = __builtin_amdgcn_exp2f((m - gm) * kLog2e);
         m = gm;
         den *= old;
@@ -283,16 +277,47 @@ __global__ __launch_bounds__(256) void ragged_merge_kernel(RaggedArgs a) {
     const float inv = den > 0.f ? 1.0f / den : 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] *= inv;
-    const int64_t row = (int64_t)(q0 + tok) * a.Hq + h;
-    if (a.out.bf16) {
-        *reinterpret_cast<uintx4*>(static_cast<uint16_t*>(a.out.O) + row * D + 8 * c8) =
-            uintx4{pack_pair(o[0], o[1]), pack_pair(o[2], o[3]), pack_pair(o[4], o[5]), pack_pair(o[6], o[7])};
-    } else {
-        float* const O = static_cast<float*>(a.out.O) + row * D + 8 * c8;
-        *reinterpret_cast<float4*>(O) = make_float4(o[0], o[1], o[2], o[3]);
-        *reinterpret_cast<float4*>(O + 4) = make_float4(o[4], o[5], o[6], o[7]);
+    store_row8<D>(out, row, c8, o, den > 0.f ? m + __logf(den) : -INFINITY);
+}
+
+// The rows that ragged_rows_kernel computed: a workgroup takes 2048 / D rows of the places for few_tokens tokens of every sequence.  Part p holds
+// the keys from p * chunk on, so those of a row are its first ceil(seen / chunk).
+template <int D>
+__global__ __launch_bounds__(256) void ragged_merge_kernel(RaggedArgs a) {
+    constexpr int LPR = D / 8;
+    const int64_t at = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+    if (at >= a.part_rows) return;
+    const int bt = (int)a.by_q_heads.of((unsigned)at), h = (int)at - bt * a.Hq;
+    const int b = (int)a.by_tokens.of((unsigned)bt), tok = bt - b * a.few_tokens;
+    const RaggedSeq sq = ragged_seq(a, b);
+    if (tok >= sq.take || sq.take * a.G > a.few_rows) return;
+    const int seen = sq.seen(tok);
+    join_row<D>(a.part_O, a.part_L, a.part_rows, at, seen > 0 ? min((seen + a.chunk - 1) / a.chunk, a.nsplit) : 0, threadIdx.x % LPR, a.out,
+                (int64_t)(sq.q0 + tok) * a.Hq + h);
+}
+
+// The others' rows, and prompts': a workgroup takes one token's rows from blockIdx.y * 2048 / D on.
+template <int D>
+__global__ __launch_bounds__(256) void ragged_join_kernel(RaggedArgs a) {
+    constexpr int LPR = D / 8;
+    const int token = blockIdx.x;
+    // the sequence that owns the token: the last that begins at or before it (tiles of one row, but for the room between the sequences)
+    int lo = 0, n = a.B;
+    const int lane = threadIdx.x & 63;
+    while (true) {
+        const int step = (n + 63) / 64, i = lo + lane * step;
+        const int c = __builtin_popcountll(__ballot(lane * step < n && a.q_off[i] <= token));
+        if (c == 0) return;
+        lo += (c - 1) * step;
+        n = min(step, n - (c - 1) * step);
+        if (n == 1) break;
     }
-    if (a.out.LSE && c8 == 0) a.out.LSE[row] = den > 0.f ? m + __logf(den) : -INFINITY;
+    const RaggedSeq sq = ragged_seq(a, __builtin_amdgcn_readfirstlane(lo));
+    const int tok = token - sq.q0, h = (int)blockIdx.y * (256 / LPR) + (int)threadIdx.x / LPR;
+    if (tok < 0 || tok >= sq.take || sq.take * a.G <= a.few_rows || h >= a.Hq) return;
+    const int seen = sq.seen(tok);
+    join_row<D>(a.tile_part_O, a.tile_part_L, (int64_t)a.rows * a.Hq, (int64_t)token * a.Hq + h,
+                seen > 0 ? min((seen + a.tile_chunk - 1) / a.tile_chunk, a.tile_nsplit) : 0, threadIdx.x % LPR, a.out, (int64_t)token * a.Hq + h);
 }
 
 template <int D, bool CODES, int TR, int NW>
@@ -327,6 +352,14 @@ hipError_t launch_ragged_rows(const RaggedArgs& a, int D, bool codes, hipStream_
     const unsigned g = (unsigned)((a.part_rows + 2048 / D - 1) / (2048 / D));
     if (D == 128) ragged_merge_kernel<128><<<g, 256, 0, s>>>(a);
     else ragged_merge_kernel<64><<<g, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_ragged_join(const RaggedArgs& a, int D, hipStream_t s) {
+    const dim3 grid((unsigned)a.rows, (unsigned)((a.Hq * D / 8 + 255) / 256));
+    if (grid.y > 65535) return hipErrorInvalidValue;
+    if (D == 128) ragged_join_kernel<128><<<grid, 256, 0, s>>>(a);
+    else ragged_join_kernel<64><<<grid, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -1,0 +1,595 @@
+// Causal attention of packed tokens on the matrix cores, 128 query rows to a workgroup: the body shared by ragged_wide.hip (D = 128) and
+// ragged_wide_d64.hip (D = 64), which define HG_RW_D.  Sequences of more than a.few_rows query rows to a KV head: prompts, long chunks.
+//
+// Mathematics and pipeline are those of prefix_wide_impl.h (transposed products with v_mfma_f32_32x32x16_bf16, a lane owns one query row, weights
+// against a maximum that is only raised when their sum says so, one step = scores of stage j + 2, weights of stage j + 1 and P V of stage j, written out by
+// gen_prefix_wide_step.py).  What differs, and why:
+//   * A workgroup is four wavefronts x 32 rows with 80 KiB of LDS, two to a CU, so that one's start (its tile is looked up, Q and
+//     the first stages arrive) and end lie under the other's products: a causal tile is short, 16 stages for a prompt of 1000 tokens.  A
+//     tile of 128 rows also has half the triangle of one of 256 that is multiplied for nothing, and a wavefront stops at its own last key.
+//   * K and V have rings of their own: in step j the K of stages j + 3 .. j + 5 and the V of j + 2 and j + 3 are in flight.  One barrier per step.
+//   * A row's own tokens bound its keys: steps that reach that bound, or the end of the keys, mask the scores and copy with care (`kCareful`).
+//   * Paged rows: a wavefront copies rows of one page per stage; the pages of its next 64 stages lie in the lanes of a register.
+//   * Codes are copied to a staging ring of the wavefront's own, and become bf16 on the way from there into the K and V rings: the
+//     pipeline behind is the same, and every code is expanded once per workgroup, not once per wavefront.
+//   * The output is divided by the sum of the rounded weights (LSE has the sum of the unrounded ones): where one key has nearly all the weight its rounding
+//     would otherwise show in O as a whole, since the largest weight is anywhere up to kMostWeight and not a power of two.
+#include <type_traits>
+
+#include "prefix_common.h"
+#include "ragged.h"
+
+#pragma clang diagnostic ignored "-Winline-asm"
+
+namespace hg {
+
+namespace {
+
+constexpr int D = HG_RW_D;
+constexpr int KT = D == 128 ? 32 : 64;  // keys per stage: 8 KiB of K and 8 KiB of V as bf16
+constexpr int KB = KT / 32;             // 32-key score tiles per stage
+constexpr int NW = 4;                   // wavefronts per workgroup
+constexpr int NS = 4;                   // steps of a group; V slots
+constexpr int KS = D / 16;              // MFMA k-steps of the score product
+constexpr int DB = D / 32;              // 32-row blocks of O^T
+constexpr int NKF = 4, NVF = 4;         // K and V fragment registers
+constexpr int CPR = D / 8;              // 16-byte chunks per bf16 row
+constexpr int RPI = 64 / CPR;           // rows one copy instruction covers
+constexpr int RPW = KT / NW;            // rows of a stage that one wavefront copies
+constexpr int CPW = RPW / RPI;          // ... in this many instructions per tensor
+constexpr int ROWB = D * 2;             // bytes per row
+constexpr int STB = KT * ROWB;          // bytes per stage and tensor
+constexpr int kTileRows = 32 * NW;
+static_assert(kTileRows == kTile, "");
+constexpr float kMostWeight = 256.f;    // as in prefix_wide_impl.h
+constexpr float kRoom = 16.f;
+static_assert(CPW == 2 && RPW <= 16, "a wavefront's rows of a stage lie in one page");
+
+enum { kDense = 0, kPaged = 1, kCodes = 2 };
+// LDS: K ring, V ring, and for codes the wavefronts' staging rings
+constexpr int k_slots(int mode) { return mode == kCodes ? 2 : 4; }
+constexpr int kCodeSlots = 4, kCodeBytes = 2 * RPW * D;      // per wavefront and stage: its rows of K, then of V
+constexpr int lds_bytes(int mode) { return (k_slots(mode) + NS) * STB + (mode == kCodes ? NW * kCodeSlots * kCodeBytes : 0); }
+static_assert(lds_bytes(kCodes) <= 81920 && lds_bytes(kDense) <= 81920, "two workgroups to a CU");
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+
+// XOR swizzles of the 16-byte chunks of LDS row `row`, as in prefix_wide_impl.h
+__device__ __forceinline__ int kswz(int row) { return D == 128 ? row % 16 : (row >> 1) & 7; }
+__device__ __forceinline__ int vswz(int row) { return D == 128 ? 4 * (row % 4) : 4 * ((row >> 1) & 1); }
+
+#if HG_RW_D == 128
+typedef floatx16 STile;
+#else
+struct STile { floatx16 a, b; };
+#endif
+
+__device__ __forceinline__ void mfma_first(floatx16& S, const uintx4& a, const bf16x8& b) {
+    floatx16 z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+    S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), b, z, 0, 0, 0);
+}
+__device__ __forceinline__ void mfma_acc(floatx16& S, const uintx4& a, const bf16x8& b) {
+    S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), b, S, 0, 0, 0);
+}
+__device__ __forceinline__ void mfma_acc(floatx16& O, const shortx8& a, const uintx4& b) {
+    O = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), O, 0, 0, 0);
+}
+__device__ __forceinline__ unsigned pack_bf16_pair(float lo, float hi) {
+    floatx2 f = {lo, hi};
+    return __builtin_bit_cast(unsigned, __builtin_convertvector(f, bf16x2));
+}
+__device__ __forceinline__ float sum_of_pair(unsigned pair, float acc) {      // acc + the pair's two values
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3f803f80u), acc, false);
+}
+template <int N>
+__device__ __forceinline__ void wait_vm() {      // at most N vector memory operations outstanding
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+}
+
+extern __shared__ __attribute__((aligned(1024))) unsigned char rw_smem[];
+
+}  // namespace
+
+template <int MODE>
+__global__ __launch_bounds__(64 * NW, 2) void HG_RW_KERNEL(RaggedArgs a) {
+    constexpr bool PAGED = MODE != kDense, CODES = MODE == kCodes;
+    constexpr int ES = CODES ? 1 : 2, NKS = k_slots(MODE), VRING = NKS * STB, CRING = VRING + NS * STB;
+    constexpr int KOPS = CODES ? 1 : CPW;                            // copy instructions per stage, tensor and wavefront
+    // How far ahead of step j the copies run, and what the step needs: K of stage j + 2, V of stage j + 1.  Codes: the stages that step j expands
+    // (K of j + 3, V of j + 2) were requested kCodeSlots - 1 steps before.
+    constexpr int KA = CODES ? 3 + kCodeSlots - 1 : 5, VA = CODES ? 2 + kCodeSlots - 1 : 3;
+    unsigned char* const smem = rw_smem;
+
+    // ---- which tile, which keys ----
+    int b, tile, kvh, sp;
+    {
+        const unsigned per_split = gridDim.x / (unsigned)a.tile_nsplit;
+        sp = (int)(blockIdx.x / per_split);
+        const unsigned u = blockIdx.x - (unsigned)sp * per_split;
+        // Workgroups whose ids are equal modulo 8 run on one XCD: the tiles of a KV head go to one of them, or to as few as there are heads for, so
+        // that its rows are in that XCD's L2.  The last tiles, which see the most keys, go first.
+        int number;
+        if (a.Hkv % 8 == 0) {
+            const unsigned v = u >> 3;
+            number = (int)a.by_heads8.of(v);
+            kvh = (int)((v - (unsigned)number * (unsigned)(a.Hkv / 8)) * 8u + (u & 7u));
+        } else {
+            number = (int)a.by_heads.of(u);
+            kvh = (int)(u - (unsigned)number * (unsigned)a.Hkv);
+        }
+        number = a.tiles_all - 1 - number;
+        if (!ragged_tile<kTileRows>(a, number, b, tile)) return;
+    }
+    const RaggedSeq sq = ragged_seq(a, b);
+    const int nrows = __builtin_amdgcn_readfirstlane(sq.take * a.G), row0 = tile * kTileRows;
+    if (row0 >= nrows || nrows <= a.few_rows) return;
+    const int q0 = __builtin_amdgcn_readfirstlane(sq.q0);
+    const int before = __builtin_amdgcn_readfirstlane(sq.len - (sq.n - 1));      // keys that the sequence's first token sees
+    const int tid = threadIdx.x, l = tid & 63, lq = l & 31, hl = l >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const auto token_of = [&](int r) { return (int)a.by_group.of((unsigned)r); };
+    const int k0 = sp * a.tile_chunk;
+    const int ke = __builtin_amdgcn_readfirstlane(min(before + token_of(min(row0 + kTileRows, nrows) - 1), k0 + a.tile_chunk));      // keys [k0, ke)
+    const int nst = ke > k0 ? (ke - k0 + KT - 1) / KT : 0, nfull = ke > k0 ? (ke - k0) / KT : 0;
+    if (sp > 0 && nst == 0) return;      // (the join looks at no part that starts behind a row's keys)
+    // this wavefront's rows, and this lane's
+    const int wrow0 = row0 + 32 * w;
+    const bool any = wrow0 < nrows;
+    const int w_least = __builtin_amdgcn_readfirstlane(any ? min(before + token_of(wrow0), ke) : 0);                              // every row of the wavefront sees the keys below
+    const int w_most = __builtin_amdgcn_readfirstlane(any ? min(before + token_of(min(wrow0 + 32, nrows) - 1), ke) : 0);          // ... and none those from here on
+    const int mine = w_most > k0 ? (w_most - k0 + KT - 1) / KT : 0;      // stages that this wavefront multiplies
+    const int r = wrow0 + lq;
+    const bool rv = r < nrows;
+    const int tok = token_of(rv ? r : row0), head = (rv ? r : row0) - tok * a.G + kvh * a.G;
+    const int seen = rv ? min(before + tok, ke) : 0;
+
+    // ---- HBM -> LDS copies: wavefront w copies rows w RPW .. of a stage; the swizzle is applied on the global side ----
+    const int64_t kv_stride = a.kv_stride;
+    const int lrow = CODES ? l / (D / 16) : l / CPR, lch = CODES ? l % (D / 16) : l % CPR;
+    unsigned voffK[KOPS], voffV;
+#pragma unroll
+    for (int i = 0; i < KOPS; ++i)
+        voffK[i] = (unsigned)lrow * (unsigned)kv_stride + (CODES ? (unsigned)lch : (unsigned)(lch ^ kswz(w * RPW + i * RPI + lrow))) * 16u;
+    voffV = (unsigned)lrow * (unsigned)kv_stride + (CODES ? (unsigned)lch : (unsigned)(lch ^ vswz(lrow))) * 16u;      // (rows RPI and RPW apart share their V swizzle)
+    const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)HG_LDS(smem));
+    const unsigned lds_rows = lds0 + (unsigned)(w * RPW * ROWB);
+    const unsigned char* const Kh = a.K + (int64_t)kvh * (D * ES);
+    const unsigned char* const Vh = a.V + (int64_t)kvh * (D * ES);
+    const auto scalar = [](const unsigned char* p) {
+        const uint64_t v = reinterpret_cast<uint64_t>(p);
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+        return reinterpret_cast<const unsigned char*>(((uint64_t)hi << 32) | lo);
+    };
+    const auto copy16 = [&](const unsigned char* base, unsigned voff, unsigned dst) {
+        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(dst) : "memory", "m0");
+    };
+    int pages = 0, page_base = 0;      // lane i: page of this wavefront's rows of stage page_base + i
+    const auto look_up = [&](int s0) {
+        page_base = s0;
+        const int e = min((int)((unsigned)(k0 + (s0 + l) * KT + w * RPW) >> a.pg.shift), a.pg.stride - 1);
+        pages = min(max(a.pg.table[(int64_t)b * a.pg.stride + e], 0), a.pg.n_pages - 1);
+    };
+    const auto row_offset = [&](int s) -> int64_t {      // byte offset of the first of this wavefront's rows of stage s
+        const int j = k0 + s * KT + w * RPW;
+        if constexpr (PAGED) {
+            const int page = __builtin_amdgcn_readlane(pages, (s - page_base) & 63);
+            return (((int64_t)page << a.pg.shift) + (j & ((1 << a.pg.shift) - 1))) * kv_stride;
+        } else {
+            return (int64_t)(q0 + j) * kv_stride;
+        }
+    };
+    // One tensor's rows of stage s to place `at` of its ring (s modulo its slots).  tail: rows may lie behind the last one of the tensor
+    // (packed rows); those are read as the last: they are nobody's keys here.
+    const auto copy_stage = [&](int s, int at, bool is_k, auto tail) {
+        const unsigned char* const tensor = is_k ? Kh : Vh;
+        unsigned dst;
+        if constexpr (CODES) dst = lds0 + (unsigned)(CRING + w * (kCodeSlots * kCodeBytes) + (at % kCodeSlots) * kCodeBytes + (is_k ? 0 : RPW * D));
+        else dst = lds_rows + (unsigned)((is_k ? 0 : VRING) + (at % (is_k ? NKS : NS)) * STB);
+        if constexpr (decltype(tail)::value && !PAGED) {
+#pragma unroll
+            for (int i = 0; i < KOPS; ++i) {
+                const int j = q0 + k0 + s * KT + w * RPW + i * RPI, base = min(j, a.rows - 1);
+                const int back = lrow - (min(j + lrow, a.rows - 1) - base);      // by how many rows this lane's comes before the one it would copy, at most lrow
+                copy16(scalar(tensor + (int64_t)base * kv_stride), (is_k ? voffK[i] : voffV) - (unsigned)back * (unsigned)kv_stride, dst + (unsigned)i * 1024u);
+            }
+        } else {
+            const unsigned char* const first = scalar(tensor + row_offset(s));
+#pragma unroll
+            for (int i = 0; i < KOPS; ++i) copy16(scalar(first + (int64_t)(i * RPI) * kv_stride), is_k ? voffK[i] : voffV, dst + (unsigned)i * 1024u);
+        }
+    };
+    // codes: this wavefront's rows of stage s out of the staging ring, as bf16 into the K or V ring
+    const auto expand = [&](int s, bool is_k) {
+        if constexpr (CODES) {
+            const unsigned char* const from = smem + CRING + w * (kCodeSlots * kCodeBytes) + (s % kCodeSlots) * kCodeBytes + (is_k ? 0 : RPW * D);
+            unsigned char* const to = smem + (is_k ? 0 : VRING) + (s % (is_k ? NKS : NS)) * STB;
+            const uintx4 c = *reinterpret_cast<const uintx4*>(from + l * 16);
+            const int row = w * RPW + lrow;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uintx4 v;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    v[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * h + i], 1.0f, false));
+                    v[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * h + i], 1.0f, true));
+                }
+                const int ch = 2 * lch + h;
+                *reinterpret_cast<uintx4*>(to + row * ROWB + ((ch ^ (is_k ? kswz(row) : vswz(row))) * 16)) = v;
+            }
+        }
+    };
+
+    // ---- LDS fragment reads, as in prefix_wide_impl.h ----
+    unsigned kaddr[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) kaddr[s] = (unsigned)(lq * ROWB + (((2 * s + hl) ^ kswz(lq)) * 16));
+    unsigned vaddr[DB];
+    {
+        const int i16 = l & 15, g1 = (l >> 4) & 1;
+        const int keyq = 4 * hl + (i16 >> 2);
+        const int fv = vswz(keyq);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+            const int chunk = 4 * db + 2 * g1 + ((i16 & 3) >> 1);
+            vaddr[db] = (unsigned)(VRING + keyq * ROWB + ((chunk ^ fv) * 16) + (i16 & 1) * 8);
+        }
+    }
+    const auto lds_k = [&](int slot, int f) -> uintx4 {
+        return *reinterpret_cast<const uintx4*>(smem + (slot % NKS) * STB + (f / KS) * 32 * ROWB + kaddr[f % KS]);
+    };
+    const auto lds_v = [&](int slot, int tt, int db) -> shortx8 {
+        const unsigned char* vp = smem + slot * STB + vaddr[db] + tt * 16 * ROWB;
+        const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)HG_LDS(vp));
+        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)HG_LDS(vp + 8 * ROWB));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+
+    // ---- online softmax state ----
+    floatx16 Oacc[DB];
+    float lsum, lround;         // this lane's share of the row's sum: of the unrounded weights, of the rounded ones
+    float mc;                   // what the exponents are taken against, log2 units
+    const float c2 = a.scale * kLog2e;
+    const auto weights = [&](const STile& S, uintx4 (&p)[KT / 16], float& rsum) -> float {
+        float sa = 0.f, sb = 0.f;
+        rsum = 0.f;
+#pragma unroll
+        for (int h = 0; h < KT / 16; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = 8 * (h & 1) + 2 * i;
+#if HG_RW_D == 128
+                const float x0 = S[e], x1 = S[e + 1];
+#else
+                const float x0 = h < 2 ? S.a[e] : S.b[e], x1 = h < 2 ? S.a[e + 1] : S.b[e + 1];
+#endif
+                const float ea = __builtin_amdgcn_exp2f(fmaf(x0, c2, -mc)), eb = __builtin_amdgcn_exp2f(fmaf(x1, c2, -mc));
+                const unsigned pair = pack_bf16_pair(ea, eb);
+                p[h][i] = pair;
+                rsum = sum_of_pair(pair, rsum);
+                sa += ea;
+                sb += eb;
+            }
+        return sa + sb;
+    };
+    const auto tile_max = [&](const STile& S) -> float {
+#if HG_RW_D == 128
+        float t = fmaxf(S[0], S[1]);
+#pragma unroll
+        for (int i = 2; i < 16; i += 2) t = fmaxf(fmaxf(t, S[i]), S[i + 1]);
+#else
+        float t = fmaxf(S.a[0], S.b[0]);
+#pragma unroll
+        for (int i = 1; i < 16; ++i) t = fmaxf(fmaxf(t, S.a[i]), S.b[i]);
+#endif
+        return half_max(t);
+    };
+    const auto mask_stage = [&](STile& S, int s) {      // keys of stage s that this lane's row does not see
+        const int hi = seen - (k0 + s * KT) - 4 * hl;   // row i of this lane is 8 (i / 4) + i % 4 + 4 hl (+ 32 in the second tile)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int ri = 8 * (i >> 2) + (i & 3);
+#if HG_RW_D == 128
+            if (ri >= hi) S[i] = -INFINITY;
+#else
+            if (ri >= hi) S.a[i] = -INFINITY;
+            if (ri + 32 >= hi) S.b[i] = -INFINITY;
+#endif
+        }
+    };
+
+    // ---- start: the first stages, Q, the stages behind them ----
+    const std::true_type TAIL{};
+    if constexpr (PAGED) look_up(0);
+    if constexpr (CODES) {
+        static_assert(kCodeSlots == 4, "");
+#pragma unroll
+        for (int s = 0; s < kCodeSlots; ++s) {
+            if (s < nst) copy_stage(s, s, true, TAIL);
+            if (s < nst) copy_stage(s, s, false, TAIL);
+        }
+    } else {
+        if (0 < nst) { copy_stage(0, 0, true, TAIL); copy_stage(0, 0, false, TAIL); }
+        if (1 < nst) copy_stage(1, 1, true, TAIL);
+    }
+    bf16x8 qf[KS];
+    {
+        const unsigned char* const qp = reinterpret_cast<const unsigned char*>(a.Q) + (int64_t)(q0 + tok) * a.q_stride + head * ROWB + 16 * hl;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uintx4*>(qp + 32 * s));
+#pragma unroll
+        for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[s]));
+    }
+    wait_vm<0>();
+    // Rows of the last stage from ke on may hold anything, and 0 * NaN would be NaN: whoever has copied them clears them once they have landed
+    const int partial = nst > nfull ? nst - 1 : -1;
+    const auto clear_rows = [&](int s) {
+#pragma unroll
+        for (int i = 0; i < CPW; ++i) {
+            const int row = w * RPW + i * RPI + l / CPR;
+            if (k0 + s * KT + row >= ke) *reinterpret_cast<uintx4*>(smem + VRING + (s % NS) * STB + row * ROWB + (l % CPR) * 16) = uintx4{0u, 0u, 0u, 0u};
+        }
+    };
+    const auto meet = [&]() {      // barrier of the workgroup, which no memory operation is moved over
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    const auto lds_done = [&]() { __builtin_amdgcn_s_waitcnt(0xC07F); };      // lgkmcnt(0)
+    if constexpr (CODES) {
+        // K of stages 0 .. 1 and V of stages 0 .. 1 by hand: there are only two K slots, so stage 2 waits for the scores of stage 0 (below)
+        if (0 < nst) { expand(0, true); expand(0, false); }
+        if (1 < nst) { expand(1, true); expand(1, false); }
+        if (partial == 0) clear_rows(0);
+        if (partial == 1) clear_rows(1);
+        if (4 < nst) { copy_stage(4, 4, true, TAIL); copy_stage(4, 4, false, TAIL); }
+        if (5 < nst) copy_stage(5, 5, true, TAIL);
+    } else {
+        if (partial == 0) clear_rows(0);
+        // (in this order: step 0 waits for all but the last K and the last V)
+        if (2 < nst) copy_stage(2, 2, true, TAIL);
+        if (1 < nst) copy_stage(1, 1, false, TAIL);
+        if (3 < nst) copy_stage(3, 3, true, TAIL);
+        if (2 < nst) copy_stage(2, 2, false, TAIL);
+        // K of stage 4 has the slot of stage 0, whose scores are taken first
+    }
+    lds_done();
+    meet();
+
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) Oacc[i][k] = 0.f;
+    lsum = lround = 0.f;
+    mc = 0.f;
+    uintx4 kf[NKF];
+    shortx8 vf[NVF];
+    STile SA, SB;
+    uintx4 PA[KT / 16], PB[KT / 16];
+    const auto scores = [&](int slot, STile& S) {
+        uintx4 kk[KB * KS];
+#pragma unroll
+        for (int q = 0; q < KB * KS; ++q) kk[q] = lds_k(slot, q);
+#if HG_RW_D == 128
+        mfma_first(S, kk[0], qf[0]);
+#pragma unroll
+        for (int q = 1; q < KS; ++q) mfma_acc(S, kk[q], qf[q]);
+        asm volatile("s_nop 11" : "+v"(S));
+        __builtin_amdgcn_sched_barrier(0);
+#else
+        mfma_first(S.a, kk[0], qf[0]);
+        mfma_first(S.b, kk[KS], qf[0]);
+#pragma unroll
+        for (int q = 1; q < KS; ++q) {
+            mfma_acc(S.a, kk[q], qf[q]);
+            mfma_acc(S.b, kk[KS + q], qf[q]);
+        }
+        asm volatile("s_nop 11" : "+v"(S.a), "+v"(S.b));
+#endif
+    };
+    if (mine > 0) {
+        scores(0, SB);
+        scores(1, SA);
+    }
+    if constexpr (CODES) {
+        // K of stage 2 takes the slot of stage 0 when everyone has its scores
+        meet();
+        if (2 < nst) { expand(2, true); }
+    } else {
+        meet();
+        if (4 < nst) copy_stage(4, 4, true, TAIL);
+    }
+    if (mine > 0) {
+        if (k0 + KT > w_least) mask_stage(SB, 0);
+        // (a finite number for a row with nothing but -inf, see prefix_wide_impl.h)
+        mc = fmaxf(tile_max(SB) * c2, -3.4028234e38f);
+        lsum = weights(SB, PA, lround);
+#pragma unroll
+        for (int i = 0; i < NVF; ++i) vf[i] = lds_v(0, i / DB, i % DB);
+    }
+
+    // ---- steps ----
+    // what step j starts with: everyone's copies for it have landed, everyone has finished step j - 1
+    const auto add_sum = [&](const STile& S, float ssum, float rsum, uintx4 (&pn)[KT / 16]) {
+        if (__builtin_expect(__any(!(ssum <= kMostWeight)), 0)) {
+            float top = tile_max(S) * c2;
+            if (__builtin_popcountll(__ballot(top > mc + 2.0f)) >= 48) top += kRoom;
+            const float mc_new = fmaxf(mc, top);
+            const float alpha = __builtin_amdgcn_exp2f(mc - mc_new);
+            mc = mc_new;
+            lsum *= alpha;
+            lround *= alpha;
+#pragma unroll
+            for (int i = 0; i < DB; ++i) {
+                Oacc[i] *= alpha;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            ssum = weights(S, pn, rsum);
+        }
+        lsum += ssum;
+        lround += rsum;
+    };
+    // The wait before step j: its K and V have landed while the younger copies may be in flight (those of the step before, careful ones only where there were any)
+    const auto wait_plain = [&]() {
+        if constexpr (CODES) wait_vm<2 * (kCodeSlots - 2)>();
+        else wait_vm<2 * CPW>();
+    };
+    const auto wait_careful = [&](int j) {
+        if constexpr (CODES) {
+            wait_vm<0>();
+        } else {
+            if (j + KA - 1 < nst) wait_vm<2 * CPW>();
+            else if (j + VA - 1 < nst) wait_vm<CPW>();
+            else wait_vm<0>();
+        }
+    };
+    const auto before_step = [&](int j) {      // the careful form; the partial stage's V rows are first read in the step before its own
+        wait_careful(j);
+        if constexpr (!CODES) {
+            if (j + 1 == partial) clear_rows(partial);
+        }
+        lds_done();
+        meet();
+    };
+    const auto careful_copies = [&](int j) {
+        if (j + KA < nst) copy_stage(j + KA, j + KA, true, TAIL);
+        if (j + VA < nst) copy_stage(j + VA, j + VA, false, TAIL);
+    };
+    const auto careful_expand = [&](int j) {
+        if constexpr (CODES) {
+            if (j + 3 < nst) expand(j + 3, true);
+            if (j + 2 < nst) expand(j + 2, false);
+            if (j + 2 == partial) clear_rows(partial);
+        }
+    };
+    const auto step = [&](int j, auto slotc, auto careful) {
+        constexpr int slot = decltype(slotc)::value;
+        constexpr bool kCareful = decltype(careful)::value;
+        STile &Scur = slot % 2 == 0 ? SA : SB, &Snext = slot % 2 == 0 ? SB : SA;
+        uintx4 (&pb)[KT / 16] = slot % 2 == 0 ? PA : PB, (&pn)[KT / 16] = slot % 2 == 0 ? PB : PA;
+        constexpr int slot1 = (slot + 1) % NS, slot2 = (slot + 2) % NS;
+        if constexpr (kCareful) {
+            before_step(j);
+            if (k0 + (j + 2) * KT > w_least) mask_stage(Scur, j + 1);
+            careful_copies(j);
+            careful_expand(j);
+        } else {
+            wait_plain();
+            if constexpr (CODES) lds_done();
+            meet();
+        }
+        float ssum, rsum;
+        {
+            const auto issue_k = [&](int j, int slot) { if constexpr (!kCareful) copy_stage(j + KA, slot + KA, true, std::false_type{}); };
+            const auto issue_v = [&](int j, int slot) { if constexpr (!kCareful) copy_stage(j + VA, slot + VA, false, std::false_type{}); };
+            const auto work_k = [&](int, int slot) { if constexpr (!kCareful) expand(slot + 3, true); };
+            const auto work_v = [&](int, int slot) { if constexpr (!kCareful) expand(slot + 2, false); };
+#if HG_RW_D == 128
+#include "ragged_wide_step.inc"
+#else
+#include "ragged_wide_step_d64.inc"
+#endif
+        }
+        add_sum(Scur, ssum, rsum, pn);
+    };
+    int j = 0;
+    // groups of plain steps: every copy they make is of a full stage, every weight they take of a stage that all rows see
+    const int plain = min(nfull - KA, (w_least - k0) / KT - 1);
+    for (; j + NS <= plain; j += NS) {
+        if constexpr (PAGED) {
+            if (j + NS + KA > page_base + 64) look_up(j);
+        }
+        step(j, std::integral_constant<int, 0>{}, std::false_type{});
+        step(j + 1, std::integral_constant<int, 1>{}, std::false_type{});
+        step(j + 2, std::integral_constant<int, 2>{}, std::false_type{});
+        step(j + 3, std::integral_constant<int, 3>{}, std::false_type{});
+    }
+    for (; j < mine; j += NS) {
+        if constexpr (PAGED) {
+            if (j + NS + KA > page_base + 64) look_up(j);
+        }
+        step(j, std::integral_constant<int, 0>{}, std::true_type{});
+        if (j + 1 < mine) {
+            step(j + 1, std::integral_constant<int, 1>{}, std::true_type{});
+            if (j + 2 < mine) {
+                step(j + 2, std::integral_constant<int, 2>{}, std::true_type{});
+                if (j + 3 < mine) step(j + 3, std::integral_constant<int, 3>{}, std::true_type{});
+            }
+        }
+    }
+    // stages that only the others multiply: this wavefront keeps its share of the copies going
+    for (j = mine; j < nst; ++j) {
+        if constexpr (PAGED) {
+            if (j + 1 + KA > page_base + 64) look_up(j);
+        }
+        before_step(j);
+        careful_copies(j);
+        careful_expand(j);
+    }
+
+    // ---- results: through LDS as whole lines, 32 columns of a wavefront's 32 rows at a time (the ring is free once everyone is here) ----
+    wait_vm<0>();
+    meet();
+    if (!any) return;
+    const float ltot = half_sum(lsum), lr = half_sum(lround);
+    const float inv = lr > 0.f ? a.v_scale / lr : 0.f;
+    const bool in_parts = a.tile_nsplit > 1;
+    const int64_t row_at = (int64_t)(q0 + tok) * a.Hq + head;
+    if (rv && hl == 0) {
+        const float lse = ltot > 0.f ? (mc + __log2f(ltot)) * kLn2 : -INFINITY;
+        if (in_parts) a.tile_part_L[(int64_t)sp * a.rows * a.Hq + row_at] = lse;
+        else if (a.out.LSE) a.out.LSE[row_at] = lse;
+    }
+    unsigned char* const stg = smem + w * 4096;
+    const int my_row = rv ? (int)row_at : -1;
+    int row_of[4];
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) row_of[kk] = __shfl(my_row, 8 * kk + (l >> 3));
+    float* const Of = in_parts ? a.tile_part_O + (int64_t)sp * a.rows * a.Hq * D : static_cast<float*>(a.out.O);
+    uint16_t* const Ob = static_cast<uint16_t*>(a.out.O);
+    const bool out_bf16 = a.out.bf16 && !in_parts;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+            *reinterpret_cast<float4*>(stg + lq * 128 + (((2 * q4 + hl) ^ (lq & 7)) * 16)) =
+                make_float4(Oacc[db][4 * q4] * inv, Oacc[db][4 * q4 + 1] * inv, Oacc[db][4 * q4 + 2] * inv, Oacc[db][4 * q4 + 3] * inv);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+            const int rr = 8 * kk + (l >> 3), c = l & 7;
+            const float4 v = *reinterpret_cast<const float4*>(stg + rr * 128 + ((c ^ (rr & 7)) * 16));
+            if (row_of[kk] >= 0) {
+                const int64_t at = (int64_t)row_of[kk] * D + 32 * db + 4 * c;
+                if (out_bf16) *reinterpret_cast<uint2*>(Ob + at) = make_uint2(pack_bf16_pair(v.x, v.y), pack_bf16_pair(v.z, v.w));
+                else *reinterpret_cast<float4*>(Of + at) = v;
+            }
+        }
+    }
+}
+
+template <int MODE>
+static hipError_t launch_mode(const RaggedArgs& a, unsigned grid, hipStream_t s) {
+    static bool attr_set[64] = {};
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev < 0 || dev >= 64 || !attr_set[dev]) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&HG_RW_KERNEL<MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes(MODE));
+        if (e != hipSuccess) return e;
+        if (dev >= 0 && dev < 64) attr_set[dev] = true;
+    }
+    HG_RW_KERNEL<MODE><<<grid, 64 * NW, lds_bytes(MODE), s>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t HG_RW_LAUNCH(const RaggedArgs& a, bool codes, hipStream_t s) {
+    const int64_t grid = (int64_t)a.tiles_all * a.Hkv * a.tile_nsplit;
+    if (grid >= (1LL << 31)) return hipErrorInvalidValue;
+    if (!a.pg.table) return launch_mode<kDense>(a, (unsigned)grid, s);
+    return codes ? launch_mode<kCodes>(a, (unsigned)grid, s) : launch_mode<kPaged>(a, (unsigned)grid, s);
+}
+
+}  // namespace hg
