@@ -1,5 +1,5 @@
-"""Thin ctypes binding of libhydragen.so: same names as include/hydragen.h, argument marshalling only.  The calls of a decode step
-(fused attention, cache update) are marshalled by a native extension (csrc/marshal.cpp); what it does not take comes
+"""Thin ctypes binding of libhydragen.so: same names as include/hydragen.h, argument marshalling only.  The calls of a decode step and those before it
+(fused attention, cache update, prompts and chunks, slots and the write into the pages) are marshalled by a native extension (csrc/marshal.cpp); what it does not take comes
 back here, to the same checks in Python.
 
 PyTorch is used for device memory and streams; every step of the attention path runs in the HIP kernels of
@@ -169,7 +169,7 @@ class _PythonOnly:
     def _none(*args):
         return None
 
-    attn = attn_fp8 = attn_paged = append = append_fp8 = append_paged = _none
+    attn = attn_fp8 = attn_paged = append = append_fp8 = append_paged = prompt = chunk = slots = write = _none
 
 
 def native():
@@ -188,7 +188,8 @@ def native():
             warnings.warn(f"decode-step calls are marshalled in Python: {e} (build it with `python -m paper_2402_05099_amd.build`)", RuntimeWarning)
             m = _PythonOnly
         else:
-            fns = (L.hg_hydragen_attn, L.hg_hydragen_attn_fp8, L.hg_hydragen_attn_paged, L.hg_kv_append, L.hg_kv_append_fp8, L.hg_kv_append_paged)
+            fns = (L.hg_hydragen_attn, L.hg_hydragen_attn_fp8, L.hg_hydragen_attn_paged, L.hg_kv_append, L.hg_kv_append_fp8, L.hg_kv_append_paged,
+                   L.hg_prompt_attn, L.hg_chunk_attn_paged, L.hg_page_slots, L.hg_kv_write_paged)
             m.setup([ctypes.cast(f, ctypes.c_void_p).value for f in fns], Level, PagedKV)
         _native = m
     return _native
@@ -571,6 +572,11 @@ def _packed_out(O, LSE, lead, D):
 
 def hg_prompt_attn(ctx: Context, Q, K, V, q_off, max_len: int, O, LSE=None, scale: float = 0.0) -> None:
     """Causal self-attention of packed prompts: Q [T, Hq, D], K and V [T, Hkv, D] (rows may lie further apart), q_off int32 [B + 1]."""
+    rc = (_native or native()).prompt(ctx, Q, K, V, q_off, max_len, O, LSE, scale)
+    if rc is not None:
+        if rc:
+            _check(rc, "hg_prompt_attn")
+        return
     T, Hq, D, q_step = _rows_of(Q, torch.bfloat16, "Q")
     Tk, Hkv, Dk, kv_step = _rows_of(K, torch.bfloat16, "K")
     if (Tk, Dk) != (T, D) or _rows_of(V, torch.bfloat16, "V") != (T, Hkv, D, kv_step):
@@ -583,6 +589,11 @@ def hg_prompt_attn(ctx: Context, Q, K, V, q_off, max_len: int, O, LSE=None, scal
 
 def hg_chunk_attn_paged(ctx: Context, Q, q_off, kv: PagedKV, lengths, max_new: int, max_len: int, O, LSE=None, scale: float = 0.0) -> None:
     """Attention of every sequence's new tokens, the last rows of its paged cache: Q [T, Hq, D], q_off int32 [B + 1], lengths int32 [B]."""
+    rc = (_native or native()).chunk(ctx, Q, q_off, kv, lengths, max_new, max_len, O, LSE, scale)
+    if rc is not None:
+        if rc:
+            _check(rc, "hg_chunk_attn_paged")
+        return
     T, Hq, D, q_step = _rows_of(Q, torch.bfloat16, "Q")
     B = q_off.numel() - 1
     Hkv = _want_paged(kv, B, D)
@@ -595,6 +606,11 @@ def hg_chunk_attn_paged(ctx: Context, Q, q_off, kv: PagedKV, lengths, max_new: i
 
 def hg_page_slots(ctx: Context, lengths, counts, free_pages, page_size: int, page_table, q_off, slots, new_lengths, pages_used) -> None:
     """Places for counts[b] new tokens of every sequence: fills in page_table, q_off [B + 1], slots [T], new_lengths [B] and pages_used [1]."""
+    rc = (_native or native()).slots(ctx, lengths, counts, free_pages, page_size, page_table, q_off, slots, new_lengths, pages_used)
+    if rc is not None:
+        if rc:
+            _check(rc, "hg_page_slots")
+        return
     B = lengths.numel()
     for t, shape, name in ((lengths, (B,), "lengths"), (counts, (B,), "counts"), (free_pages, (free_pages.numel(),), "free_pages"),
                            (q_off, (B + 1,), "q_off"), (slots, (slots.numel(),), "slots"), (new_lengths, (B,), "new_lengths"),
@@ -609,6 +625,11 @@ def hg_page_slots(ctx: Context, lengths, counts, free_pages, page_size: int, pag
 
 def hg_kv_write_paged(ctx: Context, Knew, Vnew, slots, kv: PagedKV) -> None:
     """Pool row slots[i] = new row i: Knew and Vnew bf16 [T, Hkv, D] (rows may lie further apart), slots int32 [T]; -1: nowhere."""
+    rc = (_native or native()).write(ctx, Knew, Vnew, slots, kv)
+    if rc is not None:
+        if rc:
+            _check(rc, "hg_kv_write_paged")
+        return
     T, Hkv, D, step = _rows_of(Knew, torch.bfloat16, "Knew")
     if _rows_of(Vnew, torch.bfloat16, "Vnew") != (T, Hkv, D, step):
         raise ValueError(f"Vnew {tuple(Vnew.shape)} must have Knew's shape {tuple(Knew.shape)} and strides")

@@ -1,4 +1,5 @@
-// The argument marshalling of the decode-step calls (fused attention, cache update) as a CPython extension: the checks of
+// The argument marshalling of the decode-step calls (fused attention, cache update) and of those that lead to it (prompts, chunks, slots, the write
+// into the pages) as a CPython extension: the checks of
 // binding.py on the tensors, their device pointers, and the call into libhydragen.so, whose functions it is handed as addresses.
 //
 // Why native: such a call is one to three kernel launches of a few microseconds each, and checking a dozen tensors
@@ -24,6 +25,10 @@ decltype(&hg_hydragen_attn_paged) f_attn_paged;
 decltype(&hg_kv_append) f_append;
 decltype(&hg_kv_append_fp8) f_append_fp8;
 decltype(&hg_kv_append_paged) f_append_paged;
+decltype(&hg_prompt_attn) f_prompt;
+decltype(&hg_chunk_attn_paged) f_chunk;
+decltype(&hg_page_slots) f_slots;
+decltype(&hg_kv_write_paged) f_write;
 PyObject *level_type, *paged_type;
 
 PyObject *s_h, *s_value, *s_nq, *s_K, *s_V, *s_n_blocks, *s_kv_off, *s_seq_off, *s_max_rows, *s_max_seqs, *s_page_table, *s_page_size,
@@ -80,12 +85,16 @@ const void* offsets_of(PyObject* level, PyObject* name) {
     return o.p == Py_None ? nullptr : tensor(o.p).data_ptr();
 }
 
-hg_ctx* context(PyObject* ctx, int nq) {
+hg_ctx* context(PyObject* ctx) {
     const Ref h(PyObject_GetAttr(ctx, s_h));
     const Ref value(PyObject_GetAttr(h.p, s_value));
     require(PyLong_CheckExact(value.p));
     void* const p = PyLong_AsVoidPtr(value.p);
     require(p != nullptr);
+    return static_cast<hg_ctx*>(p);
+}
+hg_ctx* context(PyObject* ctx, int nq) {
+    hg_ctx* const p = context(ctx);
     int have = 1;                        // the context's number of queries per sequence
     PyObject* const n = PyObject_GetAttr(ctx, s_nq);
     if (n) {
@@ -95,7 +104,7 @@ hg_ctx* context(PyObject* ctx, int nq) {
         PyErr_Clear();
     }
     require(have == nq);                 // (binding.py sets it)
-    return static_cast<hg_ctx*>(p);
+    return p;
 }
 
 // [B, H, D] or [B, nq, H, D], bf16
@@ -113,11 +122,38 @@ struct Rows {
     }
 };
 
+// [tokens, H, D], bf16, whose tokens may lie further apart than they are long
+struct Tokens {
+    const at::Tensor& t;
+    int64_t T, H, D, step;
+    explicit Tokens(PyObject* o) : t(tensor(o)) {
+        require(t.is_cuda() && t.scalar_type() == at::kBFloat16 && t.dim() == 3);
+        T = t.size(0);
+        H = t.size(1);
+        D = t.size(2);
+        step = T > 1 ? t.stride(0) : H * D;
+        require((D <= 1 || t.stride(2) == 1) && (H <= 1 || t.stride(1) == D) && step >= H * D && step % 8 == 0 && (uintptr_t)t.data_ptr() % 16 == 0);
+        require(T <= INT_MAX && H <= INT_MAX && D <= INT_MAX);
+    }
+    bool like(const Tokens& o) const { return T == o.T && H == o.H && D == o.D && step == o.step; }
+};
+struct Ints {      // int32 [n]
+    int32_t* p;
+    int n;
+    explicit Ints(PyObject* o) {
+        const at::Tensor& t = device_tensor(o, at::kInt);
+        require(t.dim() == 1 && t.size(0) <= INT_MAX);
+        p = static_cast<int32_t*>(t.data_ptr());
+        n = (int)t.size(0);
+    }
+};
+
 struct Outputs {
     void* O;
     int dtype;
     float* lse;
-    Outputs(PyObject* o, PyObject* l, const Rows& q) {
+    template <class Q>
+    Outputs(PyObject* o, PyObject* l, const Q& q) {
         const at::Tensor& t = tensor(o);
         require(t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16);
         device_tensor(o, t.scalar_type());
@@ -167,7 +203,7 @@ struct Cache {
     }
 };
 
-struct Paged {
+struct Paged {      // B < 0: the table is not looked at
     hg_paged_kv kv;
     int64_t Hkv;
     Paged(PyObject* o, int64_t B, int64_t D) {
@@ -178,7 +214,7 @@ struct Paged {
         const Cache rows(k.p, v.p, type);
         const at::Tensor& table = device_tensor(t.p, at::kInt);
         kv.page_size = int_attr(o, s_page_size);
-        require(kv.page_size > 0 && table.dim() == 2 && table.size(0) == B && rows.K.size(2) == D && rows.K.size(0) % kv.page_size == 0);
+        require(kv.page_size > 0 && table.dim() == 2 && (B < 0 || table.size(0) == B) && rows.K.size(2) == D && rows.K.size(0) % kv.page_size == 0);
         require(table.size(1) <= INT_MAX && rows.K.size(0) / kv.page_size <= INT_MAX);
         kv.K = rows.K.data_ptr();
         kv.V = rows.V.data_ptr();
@@ -317,16 +353,80 @@ PyObject* append_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// ([addresses of the six functions, in the order above], Level, PagedKV)
+// (ctx, Q, K, V, q_off, max_len, O, LSE, scale)
+PyObject* prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 9, [&]() {
+        const Tokens q(a[1]), k(a[2]), v(a[3]);
+        require(k.T == q.T && k.D == q.D && v.like(k));
+        const Ints off(a[4]);
+        require(off.n > 0);
+        const int max_len = to_int(a[5]);
+        const Outputs out(a[6], a[7], q);
+        const float scale = to_float(a[8]);
+        hg_ctx* const c = context(a[0]);
+        return without_gil([&]() {
+            return f_prompt(c, q.t.data_ptr(), k.t.data_ptr(), v.t.data_ptr(), q.step, k.step, off.p, (int)q.T, max_len, off.n - 1, (int)q.H, (int)k.H, (int)q.D,
+                            scale, out.O, out.dtype, out.lse);
+        });
+    });
+}
+// (ctx, Q, q_off, kv, lengths, max_new, max_len, O, LSE, scale)
+PyObject* chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 10, [&]() {
+        const Tokens q(a[1]);
+        const Ints off(a[2]);
+        require(off.n > 0);
+        const Paged kv(a[3], off.n - 1, q.D);
+        const void* len = vector_of(a[4], off.n - 1);
+        const int max_new = to_int(a[5]), max_len = to_int(a[6]);
+        const Outputs out(a[7], a[8], q);
+        const float scale = to_float(a[9]);
+        hg_ctx* const c = context(a[0]);
+        return without_gil([&]() {
+            return f_chunk(c, q.t.data_ptr(), q.step, off.p, (int)q.T, &kv.kv, (const int32_t*)len, max_new, max_len, off.n - 1, (int)q.H, (int)kv.Hkv, (int)q.D,
+                           scale, out.O, out.dtype, out.lse);
+        });
+    });
+}
+// (ctx, lengths, counts, free_pages, page_size, page_table, q_off, slots, new_lengths, pages_used)
+PyObject* slots(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 10, [&]() {
+        const Ints len(a[1]), counts(a[2]), free_pages(a[3]), off(a[6]), to(a[7]), grown(a[8]), used(a[9]);
+        const int page_size = to_int(a[4]);
+        const at::Tensor& table = device_tensor(a[5], at::kInt);
+        require(counts.n == len.n && grown.n == len.n && off.n == len.n + 1 && used.n == 1);
+        require(table.dim() == 2 && table.size(0) == len.n && table.size(1) <= INT_MAX);
+        hg_ctx* const c = context(a[0]);
+        return without_gil([&]() {
+            return f_slots(c, len.p, counts.p, free_pages.p, free_pages.n, page_size, len.n, to.n, (int32_t*)table.data_ptr(), (int)table.size(1), off.p, to.p, grown.p,
+                           used.p);
+        });
+    });
+}
+// (ctx, Knew, Vnew, slots, kv)
+PyObject* write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 5, [&]() {
+        const Tokens k(a[1]), v(a[2]);
+        require(v.like(k));
+        const void* to = vector_of(a[3], k.T);
+        const Paged kv(a[4], -1, k.D);
+        require(kv.Hkv == k.H);
+        hg_ctx* const c = context(a[0]);
+        return without_gil([&]() { return f_write(c, k.t.data_ptr(), v.t.data_ptr(), k.step, (const int32_t*)to, (int)k.T, &kv.kv, (int)k.H, (int)k.D); });
+    });
+}
+
+constexpr int kFunctions = 10;
+// ([addresses of the functions, in the order above], Level, PagedKV)
 PyObject* setup(PyObject*, PyObject* args) {
     PyObject *list, *lt, *pt;
     if (!PyArg_ParseTuple(args, "O!OO", &PyList_Type, &list, &lt, &pt)) return nullptr;
-    void* f[6];
-    if (PyList_GET_SIZE(list) != 6) {
-        PyErr_SetString(PyExc_ValueError, "six addresses are wanted");
+    void* f[kFunctions];
+    if (PyList_GET_SIZE(list) != kFunctions) {
+        PyErr_SetString(PyExc_ValueError, "ten addresses are wanted");
         return nullptr;
     }
-    for (int i = 0; i < 6; ++i) {
+    for (int i = 0; i < kFunctions; ++i) {
         f[i] = PyLong_AsVoidPtr(PyList_GET_ITEM(list, i));
         if (PyErr_Occurred()) return nullptr;
     }
@@ -336,6 +436,10 @@ PyObject* setup(PyObject*, PyObject* args) {
     f_append = (decltype(f_append))f[3];
     f_append_fp8 = (decltype(f_append_fp8))f[4];
     f_append_paged = (decltype(f_append_paged))f[5];
+    f_prompt = (decltype(f_prompt))f[6];
+    f_chunk = (decltype(f_chunk))f[7];
+    f_slots = (decltype(f_slots))f[8];
+    f_write = (decltype(f_write))f[9];
     Py_INCREF(lt);
     Py_INCREF(pt);
     level_type = lt;
@@ -345,7 +449,7 @@ PyObject* setup(PyObject*, PyObject* args) {
 
 #define HG_FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HG_FAST(attn), HG_FAST(attn_fp8), HG_FAST(attn_paged), HG_FAST(append), HG_FAST(append_fp8), HG_FAST(append_paged),
-                         {"setup", setup, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         HG_FAST(prompt), HG_FAST(chunk), HG_FAST(slots), HG_FAST(write), {"setup", setup, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -7,31 +7,46 @@
 namespace hg {
 
 namespace {
-constexpr int kThreads = 256;        // also: sequences that a workgroup looks at together
-constexpr int kTokens = 1024;        // tokens that a workgroup finds the slots of
+constexpr int kThreads = 256;
+constexpr int kPer = 4;                          // sequences that a thread looks at
+constexpr int kSeqs = kThreads * kPer;           // ... and a workgroup at a time
+constexpr int kTokens = 1024;                    // tokens that a workgroup finds the slots of
 }
 
 // With have = ceil(len / ps) pages in use and want = ceil(min(len + n, capacity) / ps) needed, sequence b's new pages are the entries
 // [first, first + want - have) of the list of free ones, first = the new pages of the sequences before it; token t of it becomes row
 // len + t.  Two prefix sums over the sequences (tokens, new pages) are all that ties the sequences to each other; every workgroup takes them
-// for itself, so that one launch does: 4 bytes twice per sequence out of L2 instead of a second launch.
+// for itself, so that one launch does: 8 bytes per sequence out of L2 instead of a second launch.  A new page begins with a new token, so the
+// page's entry in the table is written where that token's slot is found.
+// What bounds it is latency, a chain of loads and barriers; the largest call here, 512 sequences with 131 thousand tokens, takes as long as a small one and a half.
 __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a) {
-    __shared__ int s_q0[kThreads + 1], s_len[kThreads], s_have[kThreads], s_first[kThreads], s_sum[2][kThreads / 64];
+    __shared__ int s_q0[kSeqs], s_len[kSeqs], s_have[kSeqs], s_first[kSeqs], s_sum[2][kThreads / 64];
     const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;
     const int ps_mask = (1 << a.shift) - 1, cap = a.stride << a.shift;
-    const int tok0 = (int)blockIdx.x * kTokens, tok1 = min(tok0 + kTokens, a.rows);
+    // the last workgroup also enters the pages of the tokens that have no place in `slots`
+    const bool last = blockIdx.x == gridDim.x - 1;
+    const int tok0 = (int)blockIdx.x * kTokens, tok1 = last ? 0x7fffffff : tok0 + kTokens;
     int base_q = 0, base_p = 0;
-    for (int b0 = 0; b0 < a.B; b0 += kThreads) {
-        const int b = b0 + tid;
-        int len = 0, n = 0;
-        if (b < a.B) {
-            len = max(a.lengths[b], 0);
-            n = max(a.counts[b], 0);
+    for (int b0 = 0; b0 < a.B; b0 += kSeqs) {
+        const int b = b0 + kPer * tid;
+        int len[kPer], n[kPer], have[kPer], fresh[kPer], end[kPer];
+        int q = 0, p = 0;      // inclusive sums over this thread's sequences, then over all before
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            len[i] = b + i < a.B ? a.lengths[b + i] : 0;
+            n[i] = b + i < a.B ? a.counts[b + i] : 0;
         }
-        const int have = (int)(((int64_t)len + ps_mask) >> a.shift);
-        const int end = max((int)min((int64_t)len + n, (int64_t)cap), len);      // rows with a place in the table (what is there already stays)
-        const int fresh = max((int)(((int64_t)end + ps_mask) >> a.shift) - have, 0);
-        int q = n, p = fresh;      // inclusive sums
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            len[i] = max(len[i], 0);
+            n[i] = max(n[i], 0);
+            have[i] = (int)(((int64_t)len[i] + ps_mask) >> a.shift);
+            end[i] = max((int)min((int64_t)len[i] + n[i], (int64_t)cap), len[i]);      // rows with a place in the table (what is there already stays)
+            fresh[i] = max((int)(((int64_t)end[i] + ps_mask) >> a.shift) - have[i], 0);
+            q += n[i];
+            p += fresh[i];
+        }
+        const int own_q = q, own_p = p;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
             const int qo = __shfl_up(q, d), po = __shfl_up(p, d);
@@ -46,52 +61,51 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a) {
             all_q += s_sum[0][i];
             all_p += s_sum[1][i];
         }
-        const int q0 = base_q + q - n, first = base_p + p - fresh;
-        s_q0[tid] = q0;
-        s_len[tid] = len;
-        s_have[tid] = have;
-        s_first[tid] = first;
-        if (tid == 0) s_q0[kThreads] = base_q + all_q;
-        __syncthreads();
-        if ((b0 / kThreads) % (int)gridDim.x == (int)blockIdx.x) {      // these sequences' own results
-            if (b < a.B) {
-                a.q_off[b] = q0;
-                const int granted = min(max(a.n_free - first, 0), fresh);
-                a.new_lengths[b] = max(len, (int)min((int64_t)end, (int64_t)(have + granted) << a.shift));
+        int q0 = base_q + q - own_q, first = base_p + p - own_p;
+        const bool owner = (b0 / kSeqs) % (int)gridDim.x == (int)blockIdx.x;      // of these sequences' own results
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int at = kPer * tid + i;
+            s_q0[at] = q0;
+            s_len[at] = len[i];
+            s_have[at] = have[i];
+            s_first[at] = first;
+            if (owner && b + i < a.B) {
+                a.q_off[b + i] = q0;
+                const int granted = min(max(a.n_free - first, 0), fresh[i]);
+                a.new_lengths[b + i] = max(len[i], (int)min((int64_t)end[i], (int64_t)(have[i] + granted) << a.shift));
             }
-            if (b0 + kThreads >= a.B && tid == 0) {
-                a.q_off[a.B] = base_q + all_q;
-                *a.pages_used = base_p + all_p;
-            }
-            // table entries: a wavefront goes through its own sequences, a lane per entry
-            for (unsigned long long todo = __ballot(fresh > 0); todo; todo &= todo - 1) {
-                const int from = __builtin_ctzll(todo);
-                const int nf = __shfl(fresh, from), f0 = __shfl(first, from), h = __shfl(have, from);
-                int32_t* const row = a.table + (int64_t)(b0 + 64 * w + from) * a.stride + h;
-                for (int i = l; i < nf; i += 64) row[i] = f0 + i < a.n_free ? a.free_pages[f0 + i] : -1;
-            }
+            q0 += n[i];
+            first += fresh[i];
         }
-        // slots of the tokens of this workgroup that belong to these sequences
+        if (owner && b0 + kSeqs >= a.B && tid == 0) {
+            a.q_off[a.B] = base_q + all_q;
+            *a.pages_used = base_p + all_p;
+        }
+        __syncthreads();
+        // the tokens of this workgroup that belong to these sequences
         const int t_end = min(tok1, base_q + all_q);
         for (int i = max(tok0, base_q) + tid; i < t_end; i += kThreads) {
             int lo = 0;      // the last sequence that starts at or before i
 #pragma unroll
-            for (int d = kThreads / 2; d > 0; d /= 2)
+            for (int d = kSeqs / 2; d > 0; d /= 2)
                 if (s_q0[lo + d] <= i) lo += d;
-            const int j = s_len[lo] + (i - s_q0[lo]);
+            const int64_t j = (int64_t)s_len[lo] + (i - s_q0[lo]);
             int slot = -1;
-            if (j < cap && j >= 0) {
-                const int e = j >> a.shift;
+            if (j < cap) {
+                const int e = (int)j >> a.shift;
+                int32_t* const entry = a.table + (int64_t)(b0 + lo) * a.stride + e;
                 int page;
                 if (e < s_have[lo]) {
-                    page = a.table[(int64_t)(b0 + lo) * a.stride + e];
+                    page = *entry;
                 } else {
                     const int f = s_first[lo] + e - s_have[lo];
                     page = f < a.n_free ? a.free_pages[f] : -1;
+                    if (((int)j & ps_mask) == 0) *entry = page;
                 }
-                if (page >= 0) slot = (page << a.shift) + (j & ps_mask);
+                if (page >= 0) slot = (page << a.shift) + ((int)j & ps_mask);
             }
-            a.slots[i] = slot;
+            if (i < a.rows) a.slots[i] = slot;
         }
         base_q += all_q;
         base_p += all_p;
@@ -101,7 +115,7 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a) {
         a.q_off[0] = 0;
         *a.pages_used = 0;
     }
-    for (int i = max(tok0, base_q) + tid; i < tok1; i += kThreads) a.slots[i] = -1;      // behind the last token
+    for (int i = max(tok0, base_q) + tid; i < min(tok1, a.rows); i += kThreads) a.slots[i] = -1;      // behind the last token
 }
 
 hipError_t launch_page_slots(const SlotArgs& a, hipStream_t s) {

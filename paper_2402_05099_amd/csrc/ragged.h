@@ -30,7 +30,8 @@ struct RaggedArgs {
     int few_rows;             // 0: none
     int few_tokens;           // tokens that such a sequence has at most
     int nsplit, chunk;        // key ranges a tile is split into, and their length (a multiple of 128)
-    int tile_rows, tiles;     // rows of a tile, 16 or 32, and tiles of few_tokens tokens
+    int tiles;                // tiles of few_tokens tokens
+    int both_tiles;           // 0: no sequence has more than 16 rows
     int wavefronts;           // of a workgroup: 4 or 8
     Divider by_seq;           // division by tiles * nsplit
     float* part_O;            // nsplit > 1: partial results [nsplit][part_rows][D], [nsplit][part_rows], part_rows = B * few_tokens * Hq
@@ -48,11 +49,15 @@ struct RaggedArgs {
 constexpr int kTile = 128;
 constexpr int kFewRows = 64;
 
+// Workgroups that take the sequences of few rows
+inline int64_t rows_grid(const RaggedArgs& a) { return (int64_t)a.B * a.tiles * a.nsplit * a.Hkv; }
+
 // ---- launchers ----
-hipError_t launch_ragged_rows(const RaggedArgs& a, int D, bool codes, hipStream_t s);       // ragged_rows.hip: sequences of few rows, with their join
-hipError_t launch_ragged_wide(const RaggedArgs& a, bool codes, hipStream_t s);              // ragged_wide.hip, D = 128: the others' tiles
-hipError_t launch_ragged_wide_d64(const RaggedArgs& a, bool codes, hipStream_t s);          // ragged_wide_d64.hip
-hipError_t launch_ragged_join(const RaggedArgs& a, int D, hipStream_t s);                   // ragged_rows.hip: the parts of the others' rows
+hipError_t launch_ragged_rows(const RaggedArgs& a, int D, bool codes, hipStream_t s);       // ragged_rows.hip: sequences of few rows
+hipError_t launch_ragged_merge(const RaggedArgs& a, int D, hipStream_t s);                  // ... their parts (nsplit > 1)
+hipError_t launch_ragged_wide(const RaggedArgs& a, bool codes, bool with_rows, hipStream_t s);           // ragged_wide.hip, D = 128: the others' tiles; with_rows: sequences of few rows in the same launch
+hipError_t launch_ragged_wide_d64(const RaggedArgs& a, bool codes, bool with_rows, hipStream_t s);          // ragged_wide_d64.hip
+hipError_t launch_ragged_join(const RaggedArgs& a, int D, hipStream_t s);                   // the parts of the others' rows (tile_nsplit > 1)
 
 // ---- block tables, slots and the write into a paged cache (pages.hip) ----
 struct SlotArgs {

@@ -78,7 +78,7 @@ Room room_of(const hg_ctx* c) { return Room{reinterpret_cast<float*>(c->ws), c->
 // Ranges of at least `least` keys, a multiple of `step` long, for `want` of them, and where their parts go.
 void split_keys(int64_t want, int max_len, int least, int step, int64_t rows, int D, Room& room, int& nsplit, int& chunk, float*& O, float*& L) {
     const size_t per = (size_t)rows * (D + 1);
-    const int64_t most = std::min<int64_t>({want, (max_len + least - 1) / least, (int64_t)(per ? room.floats / per : 0), 256});
+    const int64_t most = std::min<int64_t>({want, max_len / least, (int64_t)(per ? room.floats / per : 0), 256});
     if (most <= 1 || rows >= (1LL << 31)) return;
     chunk = (int)(((max_len + most - 1) / most + step - 1) / step * step);
     nsplit = (max_len + chunk - 1) / chunk;
@@ -86,32 +86,35 @@ void split_keys(int64_t want, int max_len, int least, int step, int64_t rows, in
     L = room.take((size_t)nsplit * rows);
 }
 
-// The sequences of at most kFewRows query rows to a KV head: how their keys are split, and the launch.  a.few_rows is set for the kernel that takes the others.
-int run_few_rows(const hg_ctx* c, RaggedArgs& a, int D, bool codes, Room& room) {
+// The sequences of at most kFewRows query rows to a KV head: how their keys are split.  a.few_rows is set for the kernel that takes the others.
+void plan_few_rows(RaggedArgs& a, int D, Room& room) {
     a.few_rows = kFewRows;
-    if (a.G > kFewRows) return HG_OK;      // even a single token has more
-    a.few_tokens = std::min(a.max_new, kFewRows / a.G);
+    a.few_tokens = std::min(a.max_new, kFewRows / a.G);      // (0: even a single token has more)
+    if (a.few_tokens == 0) return;
     const int most = a.few_tokens * a.G;
-    a.tile_rows = most <= 16 ? 16 : 32;
-    a.tiles = (most + a.tile_rows - 1) / a.tile_rows;
-    // enough workgroups to fill the chip twice, so that contexts of different lengths even out; no shorter ranges than 512 keys
-    const int64_t wgs = (int64_t)a.B * a.tiles * a.Hkv;
+    a.both_tiles = most > 16;
+    a.tiles = (most + 31) / 32;
+    // Four times the workgroups that fit the chip, so that contexts of different lengths even out; no ranges of fewer than 512 keys, which the join would cost more than
+    // they save.
+    const int64_t wgs = (int64_t)a.B * a.Hkv;
     a.part_rows = (int64_t)a.B * a.few_tokens * a.Hq;
-    split_keys((1024 + wgs - 1) / wgs, a.max_len, 512, 128, a.part_rows, D, room, a.nsplit, a.chunk, a.part_O, a.part_L);
+    split_keys((2048 + wgs - 1) / wgs, a.max_len, 512, 128, a.part_rows, D, room, a.nsplit, a.chunk, a.part_O, a.part_L);
     a.wavefronts = wgs * a.nsplit <= 256 ? 8 : 4;
     a.by_seq = divider((unsigned)(a.tiles * a.nsplit));
     a.by_q_heads = divider((unsigned)a.Hq);
     a.by_tokens = divider((unsigned)a.few_tokens);
-    return rc_of(launch_ragged_rows(a, D, codes, c->stream));
 }
 
 // The others, and prompts.
-int run_tiles(const hg_ctx* c, RaggedArgs& a, int D, bool codes, Room& room) {
+void plan_tiles(RaggedArgs& a, int D, Room& room) {
     // two workgroups to a CU; tiles of sequences with more than few_rows rows, from the host's bounds
     const int64_t tiles = ((int64_t)a.rows * a.G + kTile - 1) / kTile + std::min<int64_t>(a.B, (int64_t)a.rows * a.G / (a.few_rows + 1));
     const int64_t wgs = std::max<int64_t>(1, tiles * a.Hkv);
     split_keys(wgs >= 512 ? 1 : (1024 + wgs - 1) / wgs, a.max_len, 512, 64, (int64_t)a.rows * a.Hq, D, room, a.tile_nsplit, a.tile_chunk, a.tile_part_O, a.tile_part_L);
-    const int rc = rc_of(D == 128 ? launch_ragged_wide(a, codes, c->stream) : launch_ragged_wide_d64(a, codes, c->stream));
+}
+
+int run_tiles(const hg_ctx* c, const RaggedArgs& a, int D, bool codes, bool with_rows) {
+    const int rc = rc_of(D == 128 ? launch_ragged_wide(a, codes, with_rows, c->stream) : launch_ragged_wide_d64(a, codes, with_rows, c->stream));
     if (rc || a.tile_nsplit == 1) return rc;
     return rc_of(launch_ragged_join(a, D, c->stream));
 }
@@ -135,7 +138,8 @@ int hg_prompt_attn(hg_ctx* c, const void* Q, const void* K, const void* V, int64
     a.kv_stride = 2 * kv_stride;
     a.max_len = max_len;
     Room room = room_of(c);
-    return run_tiles(c, a, D, false, room);
+    plan_tiles(a, D, room);
+    return run_tiles(c, a, D, false, false);
 }
 
 int hg_chunk_attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_t* q_off, int rows, const hg_paged_kv* kv, const int32_t* lengths,
@@ -170,9 +174,17 @@ int hg_chunk_attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_
         a.v_scale = kv->v_scale;
     }
     Room room = room_of(c);
-    const int rc2 = run_few_rows(c, a, D, codes, room);
-    if (rc2 || (int64_t)std::min(max_new, rows) * a.G <= kFewRows) return rc2;
-    return run_tiles(c, a, D, codes, room);
+    plan_few_rows(a, D, room);
+    const bool few = a.few_tokens > 0, others = (int64_t)std::min(max_new, rows) * a.G > kFewRows;
+    int done = HG_OK;
+    if (others) {
+        plan_tiles(a, D, room);
+        done = run_tiles(c, a, D, codes, few);
+    } else if (few) {
+        done = rc_of(launch_ragged_rows(a, D, codes, c->stream));
+    }
+    if (done == HG_OK && few && a.nsplit > 1) done = rc_of(launch_ragged_merge(a, D, c->stream));
+    return done;
 }
 
 int hg_page_slots(hg_ctx* c, const int32_t* lengths, const int32_t* counts, const int32_t* free_pages, int n_free, int page_size, int B, int rows,

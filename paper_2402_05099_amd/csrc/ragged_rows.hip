@@ -1,244 +1,14 @@
-// Attention of a paged cache's few newest tokens (decode steps, drafted tokens): sequences with at most kFewRows query rows to a KV head.
-// What bounds it is the cache that is read, once for every KV head whatever the rows, so the rows of a head's group and of all
-// new tokens form one tile of 16 or 32 rows (v_mfma_f32_16x16x32_bf16, v_mfma_f32_32x32x16_bf16; decode_mfma_core.h has the products and the softmax).
-//
-// A workgroup of NW wavefronts takes one tile and one range of its keys; its 32-key stages go to the wavefronts in turn, each with a K and a V slot
-// in LDS that is filled again by global_load_lds_dwordx4 as soon as its rows have been multiplied.  The wavefronts never wait for each other until their
-// (m, l, O) meet in LDS.  So a call of short contexts is one launch that needs no workspace, and one of long contexts splits the
-// keys over workgroups as well: partial results by Eq. 5, joined by ragged_merge_kernel.
+// Kernels over ragged_rows_impl.h, and the joins of partial results.
 #include <algorithm>
 
-#include "decode_mfma_core.h"
-#include "ragged.h"
-
-#pragma clang diagnostic ignored "-Winline-asm"
+#include "ragged_rows_impl.h"
 
 namespace hg {
 
-using namespace dm;
+using namespace rr;
 
-namespace {
-
-extern __shared__ __attribute__((aligned(1024))) unsigned char rr_smem[];
-
-template <int D, bool CODES, int TR>
-struct RowsGeo {
-    static constexpr int RPI = CODES ? 8 : Geo<D>::RPI;          // rows one copy instruction covers (codes of either D lie 128 bytes apart in LDS)
-    static constexpr int CPS = KT / RPI;                         // copy instructions per stage and tensor
-    static constexpr int TENSOR = CPS * 1024;                    // bytes of a stage's K or V in LDS
-    static constexpr int JOIN = TR * D * 4;                      // bytes of a wavefront's O where they meet
-    static constexpr int SLOT = 2 * TENSOR > JOIN ? 2 * TENSOR : JOIN;
-    static constexpr int bytes(int nw) { return nw * (SLOT + 2 * TR * 4); }
-};
-
-// Columns 8 c8 .. + 7 of a row's result
-template <int D>
-__device__ __forceinline__ void store_row8(const OutDev& out, int64_t row, int c8, const float (&o)[8], float lse) {
-    if (out.bf16) {
-        *reinterpret_cast<uintx4*>(static_cast<uint16_t*>(out.O) + row * D + 8 * c8) =
-            uintx4{pack_pair(o[0], o[1]), pack_pair(o[2], o[3]), pack_pair(o[4], o[5]), pack_pair(o[6], o[7])};
-    } else {
-        float* const O = static_cast<float*>(out.O) + row * D + 8 * c8;
-        *reinterpret_cast<float4*>(O) = make_float4(o[0], o[1], o[2], o[3]);
-        *reinterpret_cast<float4*>(O + 4) = make_float4(o[4], o[5], o[6], o[7]);
-    }
-    if (out.LSE && c8 == 0) out.LSE[row] = lse;
-}
-
-}  // namespace
-
-template <int D, bool CODES, int TR, int NW>
-__global__ __launch_bounds__(64 * NW) void ragged_rows_kernel(RaggedArgs a) {
-    using Tile = MfmaTile<D, CODES, TR>;
-    using G_ = Geo<D>;
-    using R_ = RowsGeo<D, CODES, TR>;
-    constexpr int RPI = R_::RPI, CPS = R_::CPS, ES = CODES ? 1 : 2;
-    const int l = threadIdx.x & 63;
-    const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-
-    // ---- which tile, which keys (everything uniform) ----
-    typedef const __attribute__((address_space(4))) int32_t* const_i32;
-    int u = blockIdx.x;
-    const int rest = (int)a.by_heads.of((unsigned)u), kvh = u - rest * a.Hkv;
-    const int tiles = a.tiles, per_seq = tiles * a.nsplit;
-    const int b = (int)a.by_seq.of((unsigned)rest), in_seq = rest - b * per_seq;
-    const int rt = in_seq % tiles, sp = in_seq / tiles;
-    const int q0 = min(max(((const_i32)(uintptr_t)a.q_off)[b], 0), a.rows);
-    const int n = min(max(((const_i32)(uintptr_t)a.q_off)[b + 1], q0), a.rows) - q0;
-    const int len = max(min(((const_i32)(uintptr_t)a.lengths)[b], a.max_len), 0);
-    const int nrows = min(n, a.max_new) * a.G;
-    if (nrows > a.few_rows || rt * TR >= nrows) return;
-    const auto seen_by = [&](int t) { return len - (n - 1 - t); };
-    const int t_first = (int)a.by_group.of((unsigned)(rt * TR)), t_last = (int)a.by_group.of((unsigned)(min(rt * TR + TR, nrows) - 1));
-    const int k0 = sp * a.chunk, ke = min(seen_by(t_last), k0 + a.chunk);      // keys [k0, ke)
-    if (sp > 0 && k0 >= ke) return;      // (the join looks at no part that starts behind a row's keys)
-    const int all_see = seen_by(t_first);       // every row of the tile sees the keys below
-    const int nst = ke > k0 ? (ke - k0 + KT - 1) / KT : 0;
-
-    // ---- this lane's query row ----
-    Tile t(a.scale, l);
-    t.tau_raw = 0.f;      // sums follow every maximum: the largest weight of a row is 1, which bf16 holds exactly (with scores of many nats it is nearly the only one)
-    const int r = rt * TR + t.row();
-    const bool rv = r < nrows;
-    const int tok = (int)a.by_group.of((unsigned)(rv ? r : 0)), g = (rv ? r : 0) - tok * a.G;
-    const int seen = rv ? seen_by(tok) : 0;
-    {
-        const unsigned char* const qp = reinterpret_cast<const unsigned char*>(a.Q) + (int64_t)(q0 + tok) * a.q_stride + (kvh * a.G + g) * (D * 2);
-        if constexpr (TR == 16) {
-#pragma unroll
-            for (int s = 0; s < Tile::KS16; ++s) t.qf16[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uintx4*>(qp + 64 * s + 16 * t.lg));
-        } else {
-#pragma unroll
-            for (int s = 0; s < Tile::KS; ++s) t.qf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uintx4*>(qp + 32 * s + 16 * t.hl));
-        }
-    }
-
-    // ---- copies: stage i of this wavefront is stage w + i NW of the range ----
-    unsigned char* const slot = rr_smem + w * R_::SLOT;
-    const unsigned dst = (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)HG_LDS(slot));
-    unsigned voffK[CPS], voffV[CPS];      // lane offsets within the rows of one copy instruction
-    {
-        constexpr int LPR = 64 / RPI;
-        const int lr = l / LPR, sl = l % LPR;
-#pragma unroll
-        for (int i = 0; i < CPS; ++i) {
-            const int row = i * RPI + lr;
-            int ck, cv;
-            if (CODES) {      // slots of 16 codes, swizzled as MfmaTile reads them; at D = 64 the other four of eight hold a row once more, which nothing reads
-                ck = (sl ^ ((row >> 1) & 7)) & (D / 16 - 1);
-                cv = (sl ^ (((row >> 1) & 1) | (((row >> (TR == 16 ? 4 : 3)) & 1) << 1))) & (D / 16 - 1);
-            } else {
-                ck = sl ^ G_::kswz(row);
-                cv = sl ^ G_::vswz(row);
-            }
-            voffK[i] = (unsigned)lr * (unsigned)a.kv_stride + (unsigned)ck * 16u;
-            voffV[i] = (unsigned)lr * (unsigned)a.kv_stride + (unsigned)cv * 16u;
-        }
-    }
-    // page of half a stage (16 rows): lane 2 i + h holds that of half h of this wavefront's stage i0 + i, 32 stages at a time
-    int pages = 0;
-    const int shift = a.pg.shift;
-    const auto look_up = [&](int i0) {
-        const int j = k0 + (w + (i0 + (l >> 1)) * NW) * KT + (l & 1) * 16;
-        const int e = min(j >> shift, a.pg.stride - 1);
-        pages = min(max(a.pg.table[(int64_t)b * a.pg.stride + e], 0), a.pg.n_pages - 1);
-    };
-    const auto base_of = [&](int i, int h) -> int64_t {      // byte offset of the first row of half h of stage i
-        const int page = __builtin_amdgcn_readlane(pages, (2 * i + h) & 63);
-        const int j = k0 + (w + i * NW) * KT + h * 16;
-        return (((int64_t)page << shift) + (j & ((1 << shift) - 1))) * a.kv_stride + (int64_t)kvh * (D * ES);
-    };
-    const auto scalar = [](const unsigned char* p) {
-        const uint64_t v = reinterpret_cast<uint64_t>(p);
-        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-        return reinterpret_cast<const unsigned char*>(((uint64_t)hi << 32) | lo);
-    };
-    const auto copy = [&](const unsigned char* tensor, const unsigned (&voff)[CPS], int i, unsigned to) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const unsigned char* const first = scalar(tensor + base_of(i, h));
-#pragma unroll
-            for (int k = 0; k < CPS / 2; ++k) {
-                const unsigned char* const base = first + (int64_t)(k * RPI) * a.kv_stride;
-                const int c = h * (CPS / 2) + k;
-                asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(voff[c]), "s"(scalar(base)), "s"(to + (unsigned)c * 1024u) : "memory", "m0");
-            }
-        }
-    };
-    const int mine = nst > w ? (nst - w + NW - 1) / NW : 0;
-    if (mine > 0) {
-        look_up(0);
-        copy(a.K, voffK, 0, dst);
-        copy(a.V, voffV, 0, dst + R_::TENSOR);
-    }
-    for (int i = 0; i < mine; ++i) {
-        const bool more = i + 1 < mine;
-        const int key0 = k0 + (w + i * NW) * KT;
-        typename Tile::Scores S;
-        uintx4 pb[2];
-        wait_vm<CPS>();      // K has landed; V may be in flight
-        asm volatile("" ::: "memory");
-        t.scores(slot, S);
-        if (more) {
-            if (((i + 1) & 31) == 0) look_up(i + 1);
-            copy(a.K, voffK, i + 1, dst);
-        }
-        if (key0 + KT > min(ke, all_see)) t.mask(S, 0, min(seen, ke) - key0);
-        t.softmax(S, pb);
-        if (more) wait_vm<CPS>();      // V has landed; the next K may be in flight
-        else wait_vm<0>();
-        asm volatile("" ::: "memory");
-        if (key0 + KT > ke) {      // rows past the range may hold anything, and 0 * NaN would be NaN
-#pragma unroll
-            for (int c = 0; c < CPS; ++c)
-                if (c * RPI + l / (64 / RPI) >= ke - key0) *reinterpret_cast<uintx4*>(slot + R_::TENSOR + c * 1024 + l * 16) = uintx4{0u, 0u, 0u, 0u};
-        }
-        t.values(slot + R_::TENSOR, pb);
-        if (more) copy(a.V, voffV, i + 1, dst + R_::TENSOR);
-    }
-
-    // ---- the wavefronts' (m, l, O) meet: O as [row][16-byte piece ^ row], statistics behind the slots ----
-    float lsum = t.lsum;
-    if constexpr (TR == 16) lsum += __shfl_xor(lsum, 16);
-    lsum = half_sum(lsum);
-    float* const stat = reinterpret_cast<float*>(rr_smem + NW * R_::SLOT);      // [NW][2][TR]
-    constexpr int PCS = D / 4;
-    const auto piece = [&](unsigned char* base, int row, int c) { return reinterpret_cast<float4*>(base + row * (D * 4) + ((c ^ (row & (PCS - 1))) * 16)); };
-    if constexpr (TR == 16) {
-#pragma unroll
-        for (int db = 0; db < Tile::DB16; ++db)
-            *piece(slot, t.ln, 4 * db + t.lg) = make_float4(t.Oacc16[db][0], t.Oacc16[db][1], t.Oacc16[db][2], t.Oacc16[db][3]);
-        if (t.lg == 0) { stat[(2 * w) * TR + t.ln] = t.m_used; stat[(2 * w + 1) * TR + t.ln] = lsum; }
-    } else {
-#pragma unroll
-        for (int db = 0; db < Tile::DB; ++db)
-#pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4)
-                *piece(slot, t.lq, 8 * db + 2 * q4 + t.hl) = make_float4(t.Oacc[db][4 * q4], t.Oacc[db][4 * q4 + 1], t.Oacc[db][4 * q4 + 2], t.Oacc[db][4 * q4 + 3]);
-        if (t.hl == 0) { stat[(2 * w) * TR + t.lq] = t.m_used; stat[(2 * w + 1) * TR + t.lq] = lsum; }
-    }
-    __syncthreads();
-    constexpr int LPR = D / 8;      // lanes per row, eight columns each
-    for (int row = (int)threadIdx.x / LPR; row < TR; row += 64 * NW / LPR) {
-        const int rr = rt * TR + row;
-        if (rr >= nrows) break;
-        const int c8 = (int)threadIdx.x % LPR;
-        float m = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) m = fmaxf(m, stat[(2 * i) * TR + row]);
-        float o[8] = {}, den = 0.f;
-        if (m > -INFINITY) {
-#pragma unroll
-            for (int i = 0; i < NW; ++i) {
-                const float e = __builtin_amdgcn_exp2f((stat[(2 * i) * TR + row] - m) * t.c2);      // (a wavefront without a key: 0)
-                den = fmaf(e, stat[(2 * i + 1) * TR + row], den);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float4 x = *piece(rr_smem + i * R_::SLOT, row, 2 * c8 + h);
-                    o[4 * h] = fmaf(e, x.x, o[4 * h]);
-                    o[4 * h + 1] = fmaf(e, x.y, o[4 * h + 1]);
-                    o[4 * h + 2] = fmaf(e, x.z, o[4 * h + 2]);
-                    o[4 * h + 3] = fmaf(e, x.w, o[4 * h + 3]);
-                }
-            }
-        }
-        const float inv = den > 0.f ? a.v_scale / den : 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] *= inv;
-        const int tk = (int)a.by_group.of((unsigned)rr), gg = rr - tk * a.G;
-        // one range: the result itself; several: part `sp`, whose rows have places for max_new tokens of every sequence
-        const int64_t at = a.nsplit == 1 ? (int64_t)(q0 + tk) * a.Hq + kvh * a.G + gg : ((int64_t)b * a.few_tokens + tk) * a.Hq + kvh * a.G + gg;
-        const float lse = den > 0.f ? m * a.scale + __logf(den) : -INFINITY;
-        if (a.nsplit > 1) {
-            float* const O = a.part_O + ((int64_t)sp * a.part_rows + at) * D + 8 * c8;
-            *reinterpret_cast<float4*>(O) = make_float4(o[0], o[1], o[2], o[3]);
-            *reinterpret_cast<float4*>(O + 4) = make_float4(o[4], o[5], o[6], o[7]);
-            if (c8 == 0) a.part_L[(int64_t)sp * a.part_rows + at] = lse;
-            continue;
-        }
-        store_row8<D>(a.out, at, c8, o, lse);
-    }
-}
+template <int D, bool CODES, bool BOTH, int NW>
+__global__ __launch_bounds__(64 * NW) void ragged_rows_kernel(RaggedArgs a) { rows_workgroup<D, CODES, BOTH, NW>(a, blockIdx.x); }
 
 // One row's parts joined by Eq. 5: D / 8 lanes of eight columns.  Part p of row `at` is O[p * part_rows + at], L[p * part_rows + at].
 template <int D>
@@ -320,35 +90,36 @@ __global__ __launch_bounds__(256) void ragged_join_kernel(RaggedArgs a) {
                 seen > 0 ? min((seen + a.tile_chunk - 1) / a.tile_chunk, a.tile_nsplit) : 0, threadIdx.x % LPR, a.out, (int64_t)token * a.Hq + h);
 }
 
-template <int D, bool CODES, int TR, int NW>
+template <int D, bool CODES, bool BOTH, int NW>
 static hipError_t launch_rows_t(const RaggedArgs& a, unsigned grid, hipStream_t s) {
-    constexpr int bytes = RowsGeo<D, CODES, TR>::bytes(NW);
+    constexpr int bytes = rows_lds<D, CODES, BOTH>(NW);
     static bool attr_set[64] = {};
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
     if (bytes > 65536 && (dev < 0 || dev >= 64 || !attr_set[dev])) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&ragged_rows_kernel<D, CODES, TR, NW>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&ragged_rows_kernel<D, CODES, BOTH, NW>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
         if (dev >= 0 && dev < 64) attr_set[dev] = true;
     }
-    ragged_rows_kernel<D, CODES, TR, NW><<<grid, 64 * NW, bytes, s>>>(a);
+    ragged_rows_kernel<D, CODES, BOTH, NW><<<grid, 64 * NW, bytes, s>>>(a);
     return hipGetLastError();
 }
 
 template <int D, bool CODES>
 static hipError_t launch_rows_d(const RaggedArgs& a, unsigned grid, hipStream_t s) {
-    if (a.tile_rows == 16) return a.wavefronts == 8 ? launch_rows_t<D, CODES, 16, 8>(a, grid, s) : launch_rows_t<D, CODES, 16, 4>(a, grid, s);
-    return a.wavefronts == 8 ? launch_rows_t<D, CODES, 32, 8>(a, grid, s) : launch_rows_t<D, CODES, 32, 4>(a, grid, s);
+    if (!a.both_tiles) return a.wavefronts == 8 ? launch_rows_t<D, CODES, false, 8>(a, grid, s) : launch_rows_t<D, CODES, false, 4>(a, grid, s);
+    return a.wavefronts == 8 ? launch_rows_t<D, CODES, true, 8>(a, grid, s) : launch_rows_t<D, CODES, true, 4>(a, grid, s);
 }
 
 hipError_t launch_ragged_rows(const RaggedArgs& a, int D, bool codes, hipStream_t s) {
-    const int64_t grid = (int64_t)a.B * a.tiles * a.nsplit * a.Hkv;
-    if (grid >= (1LL << 31) || (a.nsplit > 1 && a.part_rows >= (1LL << 31))) return hipErrorInvalidValue;
-    hipError_t e;
-    if (D == 128) e = codes ? launch_rows_d<128, true>(a, (unsigned)grid, s) : launch_rows_d<128, false>(a, (unsigned)grid, s);
-    else e = codes ? launch_rows_d<64, true>(a, (unsigned)grid, s) : launch_rows_d<64, false>(a, (unsigned)grid, s);
-    if (e != hipSuccess || a.nsplit == 1) return e;
+    const int64_t grid = rows_grid(a);
+    if (grid >= (1LL << 31)) return hipErrorInvalidValue;
+    if (D == 128) return codes ? launch_rows_d<128, true>(a, (unsigned)grid, s) : launch_rows_d<128, false>(a, (unsigned)grid, s);
+    return codes ? launch_rows_d<64, true>(a, (unsigned)grid, s) : launch_rows_d<64, false>(a, (unsigned)grid, s);
+}
+
+hipError_t launch_ragged_merge(const RaggedArgs& a, int D, hipStream_t s) {
     const unsigned g = (unsigned)((a.part_rows + 2048 / D - 1) / (2048 / D));
     if (D == 128) ragged_merge_kernel<128><<<g, 256, 0, s>>>(a);
     else ragged_merge_kernel<64><<<g, 256, 0, s>>>(a);

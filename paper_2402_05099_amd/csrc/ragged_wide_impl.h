@@ -14,15 +14,15 @@
 //     pipeline behind is the same, and every code is expanded once per workgroup, not once per wavefront.
 //   * The output is divided by the sum of the rounded weights (LSE has the sum of the unrounded ones): where one key has nearly all the weight its rounding
 //     would otherwise show in O as a whole, since the largest weight is anywhere up to kMostWeight and not a power of two.
+#include <algorithm>
 #include <type_traits>
 
-#include "prefix_common.h"
-#include "ragged.h"
+#include "ragged_rows_impl.h"
 
 #pragma clang diagnostic ignored "-Winline-asm"
 
 namespace hg {
-
+namespace rw {
 namespace {
 
 constexpr int D = HG_RW_D;
@@ -94,8 +94,9 @@ extern __shared__ __attribute__((aligned(1024))) unsigned char rw_smem[];
 
 }  // namespace
 
+// Workgroup `id` of the `n` that take tiles.
 template <int MODE>
-__global__ __launch_bounds__(64 * NW, 2) void HG_RW_KERNEL(RaggedArgs a) {
+__device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id, unsigned n) {
     constexpr bool PAGED = MODE != kDense, CODES = MODE == kCodes;
     constexpr int ES = CODES ? 1 : 2, NKS = k_slots(MODE), VRING = NKS * STB, CRING = VRING + NS * STB;
     constexpr int KOPS = CODES ? 1 : CPW;                            // copy instructions per stage, tensor and wavefront
@@ -107,9 +108,9 @@ __global__ __launch_bounds__(64 * NW, 2) void HG_RW_KERNEL(RaggedArgs a) {
     // ---- which tile, which keys ----
     int b, tile, kvh, sp;
     {
-        const unsigned per_split = gridDim.x / (unsigned)a.tile_nsplit;
-        sp = (int)(blockIdx.x / per_split);
-        const unsigned u = blockIdx.x - (unsigned)sp * per_split;
+        const unsigned per_split = n / (unsigned)a.tile_nsplit;
+        sp = (int)(id / per_split);
+        const unsigned u = id - (unsigned)sp * per_split;
         // Workgroups whose ids are equal modulo 8 run on one XCD: the tiles of a KV head go to one of them, or to as few as there are heads for, so
         // that its rows are in that XCD's L2.  The last tiles, which see the most keys, go first.
         int number;
@@ -570,26 +571,49 @@ __global__ __launch_bounds__(64 * NW, 2) void HG_RW_KERNEL(RaggedArgs a) {
     }
 }
 
+}  // namespace rw
+
+using namespace rw;
+
 template <int MODE>
+__global__ __launch_bounds__(64 * NW, 2) void HG_RW_KERNEL(RaggedArgs a) { tile_workgroup<MODE>(a, blockIdx.x, gridDim.x); }
+
+// Both kinds of sequences in one launch, the tiles first: they are bound by the matrix pipes, the few rows by the reads of their cache, and two
+// workgroups of either kind share a CU.
+template <int MODE>
+__global__ __launch_bounds__(64 * NW, 2) void HG_RW_BOTH(RaggedArgs a) {
+    const unsigned n = (unsigned)a.tiles_all * (unsigned)a.Hkv * (unsigned)a.tile_nsplit;
+    if (blockIdx.x < n) tile_workgroup<MODE>(a, blockIdx.x, n);
+    else rr::rows_workgroup<D, MODE == kCodes, true, NW>(a, blockIdx.x - n);
+}
+
+template <int MODE, bool BOTH>
 static hipError_t launch_mode(const RaggedArgs& a, unsigned grid, hipStream_t s) {
+    constexpr int bytes = BOTH ? std::max(lds_bytes(MODE), rr::rows_lds<D, MODE == kCodes, true>(NW)) : lds_bytes(MODE);
+    static_assert(bytes <= 81920, "two workgroups to a CU");
     static bool attr_set[64] = {};
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
     if (dev < 0 || dev >= 64 || !attr_set[dev]) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&HG_RW_KERNEL<MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes(MODE));
+        const void* f;
+        if constexpr (BOTH) f = reinterpret_cast<const void*>(&HG_RW_BOTH<MODE>);
+        else f = reinterpret_cast<const void*>(&HG_RW_KERNEL<MODE>);
+        e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
         if (dev >= 0 && dev < 64) attr_set[dev] = true;
     }
-    HG_RW_KERNEL<MODE><<<grid, 64 * NW, lds_bytes(MODE), s>>>(a);
+    if constexpr (BOTH) HG_RW_BOTH<MODE><<<grid, 64 * NW, bytes, s>>>(a);
+    else HG_RW_KERNEL<MODE><<<grid, 64 * NW, bytes, s>>>(a);
     return hipGetLastError();
 }
 
-hipError_t HG_RW_LAUNCH(const RaggedArgs& a, bool codes, hipStream_t s) {
-    const int64_t grid = (int64_t)a.tiles_all * a.Hkv * a.tile_nsplit;
+hipError_t HG_RW_LAUNCH(const RaggedArgs& a, bool codes, bool with_rows, hipStream_t s) {
+    const int64_t tiles = (int64_t)a.tiles_all * a.Hkv * a.tile_nsplit, grid = tiles + (with_rows ? rows_grid(a) : 0);
     if (grid >= (1LL << 31)) return hipErrorInvalidValue;
-    if (!a.pg.table) return launch_mode<kDense>(a, (unsigned)grid, s);
-    return codes ? launch_mode<kCodes>(a, (unsigned)grid, s) : launch_mode<kPaged>(a, (unsigned)grid, s);
+    if (!a.pg.table) return launch_mode<kDense, false>(a, (unsigned)grid, s);
+    if (with_rows) return codes ? launch_mode<kCodes, true>(a, (unsigned)grid, s) : launch_mode<kPaged, true>(a, (unsigned)grid, s);
+    return codes ? launch_mode<kCodes, false>(a, (unsigned)grid, s) : launch_mode<kPaged, false>(a, (unsigned)grid, s);
 }
 
 }  // namespace hg
