@@ -13,7 +13,7 @@ none of them, so they go evenly into all the gaps, and the row sum is there befo
 says whether they have to be taken again against a larger maximum, which spares every step the search for it.
 
 The ragged form (ragged_wide_step.inc, ragged_wide_step_d64.inc, for ragged_wide_impl.h) has the same order with two differences: its copies are the kernel's
-own (issue_k, issue_v and, between them, work_k and work_v, which are empty but over 8-bit rows), and the sum of the rounded weights is taken beside that of the unrounded ones.
+own (issue_k, issue_v; read_k, read_v and, several products later, work_k, work_v are empty but over 8-bit rows), and the sum of the rounded weights is taken beside that of the unrounded ones.
 
 usage: gen_prefix_wide_step.py [D [out.inc [vector-ALU cycles per gap]]]     (no arguments: all files)
 """
@@ -60,8 +60,10 @@ def build(D=128, CAP=None, ragged=False):
     if ragged:
         mf[0][1].append("issue_k(j, slot);")
         mf[2][1].append("issue_v(j, slot);")
-        mf[6][1].append("work_k(j, slot);")
-        mf[9][1].append("work_v(j, slot);")
+        mf[1][1].append("read_k(slot);")
+        mf[4][1].append("read_v(slot);")
+        mf[7][1].append("work_k(slot);")
+        mf[11][1].append("work_v(slot);")
     else:
         mf[0][1].extend(["const int64_t cp_off = (int64_t)min(cur.ks + cur.t * KT, cur.kwin) * rstride_b;",
                          "const unsigned cp_dst = ldsw + (unsigned)((slot + AHEAD) & (NS - 1)) * STB;"])

@@ -33,7 +33,7 @@ struct RaggedArgs {
     int tiles;                // tiles of few_tokens tokens
     int both_tiles;           // 0: no sequence has more than 16 rows
     int wavefronts;           // of a workgroup: 4 or 8
-    Divider by_seq;           // division by tiles * nsplit
+    Divider by_seqs;          // division by B
     float* part_O;            // nsplit > 1: partial results [nsplit][part_rows][D], [nsplit][part_rows], part_rows = B * few_tokens * Hq
     float* part_L;
     int64_t part_rows;

@@ -94,13 +94,15 @@ void plan_few_rows(RaggedArgs& a, int D, Room& room) {
     const int most = a.few_tokens * a.G;
     a.both_tiles = most > 16;
     a.tiles = (most + 31) / 32;
-    // Four times the workgroups that fit the chip, so that contexts of different lengths even out; no ranges of fewer than 512 keys, which the join would cost more than
-    // they save.
+    // Four times the workgroups that fit the chip, so that contexts of different lengths even out, of at least 256 keys each.  Up to 1280 keys the join costs more than
+    // it saves.  us with 1 / 512 / 1024 / 2048 / 4096 workgroups wanted: 64 x 32/8 heads, up to 4096 rows 113 / 114 / 109 / 105 / 101, all of 4096 rows 173.6 / 173.7 / 178.8 /
+    // 182.7 / 188.6; 16 x 32/8, up to 8192 103.6 / 69.8 / 55.0 / 56.2 / 55.9; 32 x 64/8, up to 8192 122.1 / 127.5 / 111.5 / 103.8 / 105.4, codes 75.9 / 78.2 / 73.4 / 68.6 / 66.2; 16 x 40,
+    // up to 4096 140.0 / 138.6 / 130.2 / 122.2 / 120.2; one sequence of 65536 rows, 64/8 696 / 53.0 / 58.0 / 58.7 / 58.9; 256 x 8/1, up to 1024 17.7 / 20.4 / 21.5 / 21.3 / 21.3.
     const int64_t wgs = (int64_t)a.B * a.Hkv;
     a.part_rows = (int64_t)a.B * a.few_tokens * a.Hq;
-    split_keys((2048 + wgs - 1) / wgs, a.max_len, 512, 128, a.part_rows, D, room, a.nsplit, a.chunk, a.part_O, a.part_L);
+    split_keys(a.max_len <= 1280 ? 1 : (2048 + wgs - 1) / wgs, a.max_len, 256, 128, a.part_rows, D, room, a.nsplit, a.chunk, a.part_O, a.part_L);
     a.wavefronts = wgs * a.nsplit <= 256 ? 8 : 4;
-    a.by_seq = divider((unsigned)(a.tiles * a.nsplit));
+    a.by_seqs = divider((unsigned)a.B);
     a.by_q_heads = divider((unsigned)a.Hq);
     a.by_tokens = divider((unsigned)a.few_tokens);
 }
@@ -110,7 +112,7 @@ void plan_tiles(RaggedArgs& a, int D, Room& room) {
     // two workgroups to a CU; tiles of sequences with more than few_rows rows, from the host's bounds
     const int64_t tiles = ((int64_t)a.rows * a.G + kTile - 1) / kTile + std::min<int64_t>(a.B, (int64_t)a.rows * a.G / (a.few_rows + 1));
     const int64_t wgs = std::max<int64_t>(1, tiles * a.Hkv);
-    split_keys(wgs >= 512 ? 1 : (1024 + wgs - 1) / wgs, a.max_len, 512, 64, (int64_t)a.rows * a.Hq, D, room, a.tile_nsplit, a.tile_chunk, a.tile_part_O, a.tile_part_L);
+    split_keys(wgs >= 512 ? 1 : (2048 + wgs - 1) / wgs, a.max_len, 1024, 64, (int64_t)a.rows * a.Hq, D, room, a.tile_nsplit, a.tile_chunk, a.tile_part_O, a.tile_part_L);
 }
 
 int run_tiles(const hg_ctx* c, const RaggedArgs& a, int D, bool codes, bool with_rows) {

@@ -10,22 +10,23 @@ using namespace rr;
 template <int D, bool CODES, bool BOTH, int NW>
 __global__ __launch_bounds__(64 * NW) void ragged_rows_kernel(RaggedArgs a) { rows_workgroup<D, CODES, BOTH, NW>(a, blockIdx.x); }
 
-// One row's parts joined by Eq. 5: D / 8 lanes of eight columns.  Part p of row `at` is O[p * part_rows + at], L[p * part_rows + at].
+// Parts first, first + step, .. of a row's `parts` joined by Eq. 5 into (m, den, o): D / 8 lanes of eight columns.  Part p of row `at` is O[p * part_rows + at],
+// L[p * part_rows + at].
 template <int D>
-__device__ __forceinline__ void join_row(const float* O, const float* L, int64_t part_rows, int64_t at, int parts, int c8, const OutDev& out, int64_t row) {
-    float m = -INFINITY, den = 0.f, o[8] = {};
+__device__ __forceinline__ void join_parts(const float* O, const float* L, int64_t part_rows, int64_t at, int first, int step, int parts, int c8, float& m, float& den,
+                                           float (&o)[8]) {
     constexpr int U = 4;
-    for (int p0 = 0; p0 < parts; p0 += U) {
+    for (int p0 = first; p0 < parts; p0 += U * step) {
         float li[U];
         float4 x[U][2];
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            const int64_t i = (int64_t)min(p0 + k, parts - 1) * part_rows + at;
+            const int64_t i = (int64_t)min(p0 + k * step, parts - 1) * part_rows + at;
             li[k] = L[i];
             const float4* const src = reinterpret_cast<const float4*>(O + i * D + 8 * c8);
             x[k][0] = src[0];
             x[k][1] = src[1];
-            if (p0 + k >= parts) li[k] = -INFINITY;
+            if (p0 + k * step >= parts) li[k] = -INFINITY;
         }
         float gm = m;
 #pragma unroll
@@ -44,26 +45,57 @@ __device__ __forceinline__ void join_row(const float* O, const float* L, int64_t
             o[4] = fmaf(e, x[k][1].x, o[4]); o[5] = fmaf(e, x[k][1].y, o[5]); o[6] = fmaf(e, x[k][1].z, o[6]); o[7] = fmaf(e, x[k][1].w, o[7]);
         }
     }
+}
+template <int D>
+__device__ __forceinline__ void store_joined(const OutDev& out, int64_t row, int c8, float m, float den, float (&o)[8]) {
     const float inv = den > 0.f ? 1.0f / den : 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] *= inv;
     store_row8<D>(out, row, c8, o, den > 0.f ? m + __logf(den) : -INFINITY);
 }
 
-// The rows that ragged_rows_kernel computed: a workgroup takes 2048 / D rows of the places for few_tokens tokens of every sequence.  Part p holds
-// the keys from p * chunk on, so those of a row are its first ceil(seen / chunk).
-template <int D>
+// The rows that ragged_rows_kernel computed, PG groups of D / 8 lanes to a row, each with every PG-th of its parts (a row of many parts would be a chain of loads
+// otherwise); a workgroup takes 2048 / D / PG rows of the places for few_tokens tokens of every sequence.  Part p holds the keys from p * chunk on, so those
+// of a row are its first ceil(seen / chunk).
+template <int D, int PG>
 __global__ __launch_bounds__(256) void ragged_merge_kernel(RaggedArgs a) {
-    constexpr int LPR = D / 8;
-    const int64_t at = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
-    if (at >= a.part_rows) return;
-    const int bt = (int)a.by_q_heads.of((unsigned)at), h = (int)at - bt * a.Hq;
-    const int b = (int)a.by_tokens.of((unsigned)bt), tok = bt - b * a.few_tokens;
-    const RaggedSeq sq = ragged_seq(a, b);
-    if (tok >= sq.take || sq.take * a.G > a.few_rows) return;
-    const int seen = sq.seen(tok);
-    join_row<D>(a.part_O, a.part_L, a.part_rows, at, seen > 0 ? min((seen + a.chunk - 1) / a.chunk, a.nsplit) : 0, threadIdx.x % LPR, a.out,
-                (int64_t)(sq.q0 + tok) * a.Hq + h);
+    constexpr int LPR = D / 8, RPW = 256 / LPR / PG;
+    __shared__ float s_o[PG > 1 ? 256 : 1][8], s_m[256 / LPR], s_l[256 / LPR];
+    const int group = threadIdx.x / LPR, c8 = threadIdx.x % LPR, pg = group / RPW;
+    const int64_t at = (int64_t)blockIdx.x * RPW + group % RPW;
+    int parts = 0;
+    int64_t row = 0;
+    bool mine = false;
+    if (at < a.part_rows) {
+        const int bt = (int)a.by_q_heads.of((unsigned)at), h = (int)at - bt * a.Hq;
+        const int b = (int)a.by_tokens.of((unsigned)bt), tok = bt - b * a.few_tokens;
+        const RaggedSeq sq = ragged_seq(a, b);
+        mine = tok < sq.take && sq.take * a.G <= a.few_rows;
+        const int seen = mine ? sq.seen(tok) : 0;
+        parts = seen > 0 ? min((seen + a.chunk - 1) / a.chunk, a.nsplit) : 0;
+        row = (int64_t)(sq.q0 + tok) * a.Hq + h;
+    }
+    float m = -INFINITY, den = 0.f, o[8] = {};
+    join_parts<D>(a.part_O, a.part_L, a.part_rows, at, pg, PG, parts, c8, m, den, o);
+    if constexpr (PG > 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s_o[threadIdx.x][i] = o[i];
+        if (c8 == 0) { s_m[group] = m; s_l[group] = den; }
+        __syncthreads();
+        if (pg > 0) return;
+#pragma unroll 1
+        for (int k = 1; k < PG; ++k) {
+            const int other = group + k * RPW;
+            const float gm = fmaxf(m, s_m[other]);
+            if (gm == -INFINITY) continue;
+            const float x = __builtin_amdgcn_exp2f((m - gm) * kLog2e), y = __builtin_amdgcn_exp2f((s_m[other] - gm) * kLog2e);
+            m = gm;
+            den = den * x + s_l[other] * y;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = o[i] * x + s_o[threadIdx.x + k * RPW * LPR][i] * y;
+        }
+    }
+    if (mine) store_joined<D>(a.out, row, c8, m, den, o);
 }
 
 // The others' rows, and prompts': a workgroup takes one token's rows from blockIdx.y * 2048 / D on.
@@ -86,8 +118,10 @@ __global__ __launch_bounds__(256) void ragged_join_kernel(RaggedArgs a) {
     const int tok = token - sq.q0, h = (int)blockIdx.y * (256 / LPR) + (int)threadIdx.x / LPR;
     if (tok < 0 || tok >= sq.take || sq.take * a.G <= a.few_rows || h >= a.Hq) return;
     const int seen = sq.seen(tok);
-    join_row<D>(a.tile_part_O, a.tile_part_L, (int64_t)a.rows * a.Hq, (int64_t)token * a.Hq + h,
-                seen > 0 ? min((seen + a.tile_chunk - 1) / a.tile_chunk, a.tile_nsplit) : 0, threadIdx.x % LPR, a.out, (int64_t)token * a.Hq + h);
+    float m = -INFINITY, den = 0.f, o[8] = {};
+    join_parts<D>(a.tile_part_O, a.tile_part_L, (int64_t)a.rows * a.Hq, (int64_t)token * a.Hq + h, 0, 1,
+                  seen > 0 ? min((seen + a.tile_chunk - 1) / a.tile_chunk, a.tile_nsplit) : 0, threadIdx.x % LPR, m, den, o);
+    store_joined<D>(a.out, (int64_t)token * a.Hq + h, threadIdx.x % LPR, m, den, o);
 }
 
 template <int D, bool CODES, bool BOTH, int NW>
@@ -119,12 +153,14 @@ hipError_t launch_ragged_rows(const RaggedArgs& a, int D, bool codes, hipStream_
     return codes ? launch_rows_d<64, true>(a, (unsigned)grid, s) : launch_rows_d<64, false>(a, (unsigned)grid, s);
 }
 
-hipError_t launch_ragged_merge(const RaggedArgs& a, int D, hipStream_t s) {
-    const unsigned g = (unsigned)((a.part_rows + 2048 / D - 1) / (2048 / D));
-    if (D == 128) ragged_merge_kernel<128><<<g, 256, 0, s>>>(a);
-    else ragged_merge_kernel<64><<<g, 256, 0, s>>>(a);
+template <int D>
+static hipError_t launch_merge_d(const RaggedArgs& a, hipStream_t s) {
+    if (a.nsplit > 8) ragged_merge_kernel<D, 8><<<(unsigned)((a.part_rows + 256 / D - 1) / (256 / D)), 256, 0, s>>>(a);
+    else ragged_merge_kernel<D, 1><<<(unsigned)((a.part_rows + 2048 / D - 1) / (2048 / D)), 256, 0, s>>>(a);
     return hipGetLastError();
 }
+
+hipError_t launch_ragged_merge(const RaggedArgs& a, int D, hipStream_t s) { return D == 128 ? launch_merge_d<128>(a, s) : launch_merge_d<64>(a, s); }
 
 hipError_t launch_ragged_join(const RaggedArgs& a, int D, hipStream_t s) {
     const dim3 grid((unsigned)a.rows, (unsigned)((a.Hq * D / 8 + 255) / 256));

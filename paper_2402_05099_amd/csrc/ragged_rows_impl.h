@@ -228,13 +228,17 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
     }
 }
 
-// Workgroup `id` of the launch: (sequence, range, tile, KV head), heads fastest.  Sequences of at most 16 rows have tiles of 16, the others of 32 (`BOTH`: there may be such).
+// Workgroup `id` of the launch: (range, tile, sequence, KV head), heads fastest, ranges slowest.  Later ranges and tiles are empty for most sequences; were they
+// to alternate with the first ones, workgroups, which go to the shader engines of an XCD in turn, would leave some of those with little to do (64 x 32/8 heads, up
+// to 4096 rows, two and four ranges 122 and 123 us so, 114 with one).  Sequences of at most 16 rows have tiles of 16, the others of 32 (`BOTH`: there may be such).
 template <int D, bool CODES, bool BOTH, int NW>
 __device__ __forceinline__ void rows_workgroup(const RaggedArgs& a, unsigned id) {
     typedef const __attribute__((address_space(4))) int32_t* const_i32;
     const int rest = (int)a.by_heads.of(id), kvh = (int)id - rest * a.Hkv;
-    const int b = (int)a.by_seq.of((unsigned)rest), in_seq = rest - b * (a.tiles * a.nsplit);
-    const int rt = in_seq % a.tiles, sp = in_seq / a.tiles;
+    const int part = (int)a.by_seqs.of((unsigned)rest);
+    const int sp = part / a.tiles, rt = part - sp * a.tiles;
+    int b = rest - part * a.B + sp;
+    b -= (int)a.by_seqs.of((unsigned)b) * a.B;
     const int q0 = min(max(((const_i32)(uintptr_t)a.q_off)[b], 0), a.rows);
     const int n = min(max(((const_i32)(uintptr_t)a.q_off)[b + 1], q0), a.rows) - q0;
     const int len = max(min(((const_i32)(uintptr_t)a.lengths)[b], a.max_len), 0);

@@ -203,26 +203,26 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id,
             for (int i = 0; i < KOPS; ++i) copy16(scalar(first + (int64_t)(i * RPI) * kv_stride), is_k ? voffK[i] : voffV, dst + (unsigned)i * 1024u);
         }
     };
-    // codes: this wavefront's rows of stage s out of the staging ring, as bf16 into the K or V ring
-    const auto expand = [&](int s, bool is_k) {
-        if constexpr (CODES) {
-            const unsigned char* const from = smem + CRING + w * (kCodeSlots * kCodeBytes) + (s % kCodeSlots) * kCodeBytes + (is_k ? 0 : RPW * D);
-            unsigned char* const to = smem + (is_k ? 0 : VRING) + (s % (is_k ? NKS : NS)) * STB;
-            const uintx4 c = *reinterpret_cast<const uintx4*>(from + l * 16);
-            const int row = w * RPW + lrow;
+    // codes: this wavefront's rows of stage s out of the staging ring, and as bf16 into the K or V ring (`at`: s, or a number equal to it modulo 4)
+    const auto read_codes = [&](int at, bool is_k) -> uintx4 {
+        return *reinterpret_cast<const uintx4*>(smem + CRING + w * (kCodeSlots * kCodeBytes) + (at % kCodeSlots) * kCodeBytes + (is_k ? 0 : RPW * D) + l * 16);
+    };
+    const auto write_rows = [&](int at, bool is_k, const uintx4& c) {
+        unsigned char* const to = smem + (is_k ? 0 : VRING) + (at % (is_k ? NKS : NS)) * STB;
+        const int row = w * RPW + lrow;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uintx4 v;
+        for (int h = 0; h < 2; ++h) {
+            uintx4 v;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    v[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * h + i], 1.0f, false));
-                    v[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * h + i], 1.0f, true));
-                }
-                const int ch = 2 * lch + h;
-                *reinterpret_cast<uintx4*>(to + row * ROWB + ((ch ^ (is_k ? kswz(row) : vswz(row))) * 16)) = v;
+            for (int i = 0; i < 2; ++i) {
+                v[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * h + i], 1.0f, false));
+                v[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * h + i], 1.0f, true));
             }
+            const int ch = 2 * lch + h;
+            *reinterpret_cast<uintx4*>(to + row * ROWB + ((ch ^ (is_k ? kswz(row) : vswz(row))) * 16)) = v;
         }
     };
+    const auto expand = [&](int s, bool is_k) { write_rows(s, is_k, read_codes(s, is_k)); };
 
     // ---- LDS fragment reads, as in prefix_wide_impl.h ----
     unsigned kaddr[KS];
@@ -486,8 +486,11 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id,
         {
             const auto issue_k = [&](int j, int slot) { if constexpr (!kCareful) copy_stage(j + KA, slot + KA, true, std::false_type{}); };
             const auto issue_v = [&](int j, int slot) { if constexpr (!kCareful) copy_stage(j + VA, slot + VA, false, std::false_type{}); };
-            const auto work_k = [&](int, int slot) { if constexpr (!kCareful) expand(slot + 3, true); };
-            const auto work_v = [&](int, int slot) { if constexpr (!kCareful) expand(slot + 2, false); };
+            uintx4 ck{}, cv{};
+            const auto read_k = [&](int slot) { if constexpr (!kCareful && CODES) ck = read_codes(slot + 3, true); };
+            const auto read_v = [&](int slot) { if constexpr (!kCareful && CODES) cv = read_codes(slot + 2, false); };
+            const auto work_k = [&](int slot) { if constexpr (!kCareful && CODES) write_rows(slot + 3, true, ck); };
+            const auto work_v = [&](int slot) { if constexpr (!kCareful && CODES) write_rows(slot + 2, false, cv); };
 #if HG_RW_D == 128
 #include "ragged_wide_step.inc"
 #else
