@@ -26,38 +26,41 @@ struct RaggedArgs {
     float v_scale;            // of the values (1 for bf16 rows)
     OutDev out;               // packed rows t * Hq + h
 
-    // Sequences of at most few_rows query rows to a KV head (paged cache): ragged_rows.hip.  The tiles' kernel takes the others.
-    int few_rows;             // 0: none
-    int few_tokens;           // tokens that such a sequence has at most
-    int nsplit, chunk;        // key ranges a tile is split into, and their length (a multiple of 128)
-    int tiles;                // tiles of few_tokens tokens
-    int both_tiles;           // 0: no sequence has more than 16 rows
+    // Paged cache: a sequence's n G rows to a KV head are cut into tiles of kTile for the matrix pipes (ragged_wide_impl.h), and what remains, where it
+    // is no more than few_rows, goes to ragged_rows_impl.h, which is bound by the reads of the cache: all rows of a decode step, the last ones of a chunk.
+    int few_rows;             // 0: packed rows, where the tiles take everything
+    int few_most;             // rows that remain of a sequence, at most
+    int nsplit, chunk;        // key ranges they are split into, and their length (a multiple of 128)
+    int tiles;                // tiles of 32 rows in few_most
+    int both_tiles;           // 0: few_most <= 16
     int wavefronts;           // of a workgroup: 4 or 8
     Divider by_seqs;          // division by B
-    float* part_O;            // nsplit > 1: partial results [nsplit][part_rows][D], [nsplit][part_rows], part_rows = B * few_tokens * Hq
+    float* part_O;            // nsplit > 1: partial results [nsplit][part_rows][D], [nsplit][part_rows], part_rows = B * Hkv * few_most
     float* part_L;
     int64_t part_rows;
-    Divider by_q_heads, by_tokens;      // division by Hq and by few_tokens
+    Divider by_most;          // division by few_most
 
-    // The others, and prompts: ragged_wide_impl.h, tiles of kTile rows.
+    // Tiles.
     int tiles_all;            // numbers of tiles (ragged_tile)
     Divider by_heads8;        // division by Hkv / 8 where Hkv is a multiple of 8
     int tile_nsplit, tile_chunk;        // key ranges of a tile and their length (a multiple of 64)
     float* tile_part_O;       // tile_nsplit > 1: partial results [tile_nsplit][rows * Hq][D], [tile_nsplit][rows * Hq]
     float* tile_part_L;
 };
-constexpr int kTile = 128;
-constexpr int kFewRows = 64;
+constexpr int kTile = 128;        // rows of a tile
+constexpr int kFewRows = 64;      // a remainder of more rows is a tile
+// Of a sequence's n G rows, those that tiles take.
+__host__ __device__ inline int rows_in_tiles(int nrows, int few_rows) { return nrows % kTile <= few_rows ? nrows - nrows % kTile : nrows; }
 
-// Workgroups that take the sequences of few rows
+// Workgroups that take what remains
 inline int64_t rows_grid(const RaggedArgs& a) { return (int64_t)a.B * a.tiles * a.nsplit * a.Hkv; }
 
 // ---- launchers ----
-hipError_t launch_ragged_rows(const RaggedArgs& a, int D, bool codes, hipStream_t s);       // ragged_rows.hip: sequences of few rows
+hipError_t launch_ragged_rows(const RaggedArgs& a, int D, bool codes, hipStream_t s);       // ragged_rows.hip: what remains, or all there is
 hipError_t launch_ragged_merge(const RaggedArgs& a, int D, hipStream_t s);                  // ... their parts (nsplit > 1)
-hipError_t launch_ragged_wide(const RaggedArgs& a, bool codes, bool with_rows, hipStream_t s);           // ragged_wide.hip, D = 128: the others' tiles; with_rows: sequences of few rows in the same launch
-hipError_t launch_ragged_wide_d64(const RaggedArgs& a, bool codes, bool with_rows, hipStream_t s);          // ragged_wide_d64.hip
-hipError_t launch_ragged_join(const RaggedArgs& a, int D, hipStream_t s);                   // the parts of the others' rows (tile_nsplit > 1)
+hipError_t launch_ragged_wide(const RaggedArgs& a, bool codes, hipStream_t s);           // ragged_wide.hip, D = 128: tiles, and what remains in the same launch
+hipError_t launch_ragged_wide_d64(const RaggedArgs& a, bool codes, hipStream_t s);          // ragged_wide_d64.hip
+hipError_t launch_ragged_join(const RaggedArgs& a, int D, hipStream_t s);                   // the parts of tiles (tile_nsplit > 1)
 
 // ---- block tables, slots and the write into a paged cache (pages.hip) ----
 struct SlotArgs {
@@ -109,29 +112,52 @@ __device__ __forceinline__ RaggedSeq ragged_seq(const RaggedArgs& a, int b) {
     return s;
 }
 
-// Tiles of ROWS query rows are numbered so that no table is needed: those of sequence b start at floor(q_off[b] * G / ROWS) + b, which
-// leaves room for each of its ceil(n * G / ROWS) tiles before the next sequence's; a number between two sequences' tiles is nobody's.
-// Found with one look at 64 sequences at a time.  Every lane of a wavefront must call this; false: nobody's.
-template <int ROWS>
-__device__ __forceinline__ bool ragged_tile(const RaggedArgs& a, int number, int& b, int& tile) {
+// The `rank`-th of all sequences' tiles, and its sequence; false: nobody's.  Every lane of a wavefront must call this.  Tiles come sequence after sequence, so that
+// the rows of few sequences at a time are in the L2s (by size alone, whatever their sequence: 16 prompts up to 2048 tokens, 40 heads 329 -> 371 us), the last
+// tiles, which see the most keys, first, so that the last workgroups to start have little to do.
+// Tiles of sequence b are numbered from floor(q_off[b] * G / kTile) + b on, which leaves room for each of its at most ceil(n * G / kTile) tiles before the next
+// sequence's: no table is needed, and the sequence is found with a look at 64 at a time.  Up to eight sequences are taken in the order of their largest tiles
+// instead (lane i holds sequence i and adds up the tiles of those before it: 0.09 us a sequence, 5 us of the 16 that a workgroup had with 45 short prompts).
+__device__ __forceinline__ bool tile_of_rank(const RaggedArgs& a, int rank, RaggedSeq& seq, int& tile) {
     const int lane = threadIdx.x & 63;
-    const auto first = [&](int i) { return (int)(((unsigned)min(max(a.q_off[i], 0), a.rows) * (unsigned)a.G) / ROWS) + i; };
+    if (a.B <= 8) {
+        const RaggedSeq own = ragged_seq(a, min(lane, a.B - 1));
+        const int tiles = lane < a.B ? (rows_in_tiles(own.take * a.G, a.few_rows) + kTile - 1) / kTile : 0;
+        const int size = (max(own.seen(0), 0) / kTile) * a.G + tiles;      // of the largest tile, in units of a tile's tokens
+        int start = 0;
+        for (int i = 0; i < a.B; ++i) {
+            const int other = __builtin_amdgcn_readlane(size, i);
+            start += other > size || (other == size && i < lane) ? __builtin_amdgcn_readlane(tiles, i) : 0;
+        }
+        const unsigned long long at = __ballot(rank >= start && rank < start + tiles);
+        if (at == 0) return false;
+        const int b = __builtin_ctzll(at);
+        seq = RaggedSeq{b, __builtin_amdgcn_readlane(own.q0, b), __builtin_amdgcn_readlane(own.n, b), __builtin_amdgcn_readlane(own.take, b),
+                        __builtin_amdgcn_readlane(own.len, b)};
+        tile = __builtin_amdgcn_readlane(start + tiles - 1, b) - rank;
+        return true;
+    }
+    const int number = a.tiles_all - 1 - rank;
+    const auto first = [&](int q0, int i) { return (int)(((unsigned)q0 * (unsigned)a.G) / kTile) + i; };
     int lo = 0, n = a.B;
-    for (;;) {
+    while (n > 64) {
         const int step = (n + 63) / 64, i = lo + lane * step;
-        const bool at_or_before = lane * step < n && first(i) <= number;
-        const int c = __builtin_popcountll(__ballot(at_or_before));
+        const int c = __builtin_popcountll(__ballot(lane * step < n && first(min(max(a.q_off[i], 0), a.rows), i) <= number));
         if (c == 0) return false;
         lo += (c - 1) * step;
         n = min(step, n - (c - 1) * step);
-        if (n == 1) break;
     }
-    b = __builtin_amdgcn_readfirstlane(lo);
-    tile = __builtin_amdgcn_readfirstlane(number - first(b));
-    return tile >= 0;
+    const RaggedSeq own = ragged_seq(a, min(lo + lane, a.B - 1));
+    const int c = __builtin_popcountll(__ballot(lane < n && first(own.q0, lo + lane) <= number));
+    if (c == 0) return false;
+    const int at = __builtin_amdgcn_readfirstlane(c - 1);
+    seq = RaggedSeq{lo + at, __builtin_amdgcn_readlane(own.q0, at), __builtin_amdgcn_readlane(own.n, at), __builtin_amdgcn_readlane(own.take, at),
+                    __builtin_amdgcn_readlane(own.len, at)};
+    tile = number - first(seq.q0, seq.b);
+    return tile * kTile < rows_in_tiles(seq.take * a.G, a.few_rows);
 }
 #endif
 // Tile numbers of a call.
-inline int64_t ragged_tiles(int64_t rows, int G, int B, int tile_rows) { return rows * G / tile_rows + B; }
+inline int64_t ragged_tiles(int64_t rows, int G, int B) { return rows * G / kTile + B; }
 
 }  // namespace hg

@@ -57,7 +57,7 @@ RaggedArgs ragged_args(const void* Q, int64_t q_stride, const int32_t* q_off, in
     a.out.bf16 = o_dtype == HG_BF16;
     a.nsplit = a.tile_nsplit = 1;
     a.chunk = a.tile_chunk = kAllKeys;
-    a.tiles_all = (int)ragged_tiles(rows, a.G, B, kTile);
+    a.tiles_all = (int)ragged_tiles(rows, a.G, B);
     a.by_heads8 = divider((unsigned)std::max(Hkv / 8, 1));
     return a;
 }
@@ -86,37 +86,41 @@ void split_keys(int64_t want, int max_len, int least, int step, int64_t rows, in
     L = room.take((size_t)nsplit * rows);
 }
 
-// The sequences of at most kFewRows query rows to a KV head: how their keys are split.  a.few_rows is set for the kernel that takes the others.
+// What remains behind the tiles, at most kFewRows rows of a sequence to a KV head: how the keys are split.
 void plan_few_rows(RaggedArgs& a, int D, Room& room) {
     a.few_rows = kFewRows;
-    a.few_tokens = std::min(a.max_new, kFewRows / a.G);      // (0: even a single token has more)
-    if (a.few_tokens == 0) return;
-    const int most = a.few_tokens * a.G;
-    a.both_tiles = most > 16;
-    a.tiles = (most + 31) / 32;
+    a.few_most = (int)std::min<int64_t>((int64_t)a.max_new * a.G, kFewRows);
+    a.both_tiles = a.few_most > 16;
+    a.tiles = (a.few_most + 31) / 32;
     // Four times the workgroups that fit the chip, so that contexts of different lengths even out, of at least 256 keys each.  Up to 1280 keys the join costs more than
     // it saves.  us with 1 / 512 / 1024 / 2048 / 4096 workgroups wanted: 64 x 32/8 heads, up to 4096 rows 113 / 114 / 109 / 105 / 101, all of 4096 rows 173.6 / 173.7 / 178.8 /
     // 182.7 / 188.6; 16 x 32/8, up to 8192 103.6 / 69.8 / 55.0 / 56.2 / 55.9; 32 x 64/8, up to 8192 122.1 / 127.5 / 111.5 / 103.8 / 105.4, codes 75.9 / 78.2 / 73.4 / 68.6 / 66.2; 16 x 40,
     // up to 4096 140.0 / 138.6 / 130.2 / 122.2 / 120.2; one sequence of 65536 rows, 64/8 696 / 53.0 / 58.0 / 58.7 / 58.9; 256 x 8/1, up to 1024 17.7 / 20.4 / 21.5 / 21.3 / 21.3.
     const int64_t wgs = (int64_t)a.B * a.Hkv;
-    a.part_rows = (int64_t)a.B * a.few_tokens * a.Hq;
+    a.part_rows = wgs * a.few_most;
     split_keys(a.max_len <= 1280 ? 1 : (2048 + wgs - 1) / wgs, a.max_len, 256, 128, a.part_rows, D, room, a.nsplit, a.chunk, a.part_O, a.part_L);
     a.wavefronts = wgs * a.nsplit <= 256 ? 8 : 4;
     a.by_seqs = divider((unsigned)a.B);
-    a.by_q_heads = divider((unsigned)a.Hq);
-    a.by_tokens = divider((unsigned)a.few_tokens);
+    a.by_most = divider((unsigned)a.few_most);
 }
 
-// The others, and prompts.
+// Tiles.  A call of few tiles splits their keys; what that saves is weighed against the parts' way through memory and the join, from the host's bounds (tokens and
+// longest context; contexts are taken to be three quarters of that on average): 512 workgroups run at a time, 0.9 us a stage of 32 keys, or 0.75 where they have
+// little company; parts are written and read at 4.5 TB/s.
 void plan_tiles(RaggedArgs& a, int D, Room& room) {
-    // two workgroups to a CU; tiles of sequences with more than few_rows rows, from the host's bounds
-    const int64_t tiles = ((int64_t)a.rows * a.G + kTile - 1) / kTile + std::min<int64_t>(a.B, (int64_t)a.rows * a.G / (a.few_rows + 1));
-    const int64_t wgs = std::max<int64_t>(1, tiles * a.Hkv);
-    split_keys(wgs >= 512 ? 1 : (2048 + wgs - 1) / wgs, a.max_len, 1024, 64, (int64_t)a.rows * a.Hq, D, room, a.tile_nsplit, a.tile_chunk, a.tile_part_O, a.tile_part_L);
+    const double wgs = (double)(((int64_t)a.rows * a.G + kTile - 1) / kTile) * a.Hkv, stages = a.max_len * (D == 128 ? 1.0 : 0.5) / 32.0;
+    const double all = wgs * 0.75 * stages * 0.9 / 512.0, longest = stages * 0.75, part = 8.0 * a.rows * a.Hq * (D + 1) / 4.5e6;
+    int best = 1;
+    double least = 0.9 * std::max(all, longest);
+    for (int s = 2; wgs < 512.0 && s <= std::min(64, a.max_len / 1024); ++s) {
+        const double us = std::max(all, longest / s) + 0.5 * longest / s + part * s + 6.0;
+        if (us < least) { least = us; best = s; }
+    }
+    split_keys(best, a.max_len, 1024, 64, (int64_t)a.rows * a.Hq, D, room, a.tile_nsplit, a.tile_chunk, a.tile_part_O, a.tile_part_L);
 }
 
-int run_tiles(const hg_ctx* c, const RaggedArgs& a, int D, bool codes, bool with_rows) {
-    const int rc = rc_of(D == 128 ? launch_ragged_wide(a, codes, with_rows, c->stream) : launch_ragged_wide_d64(a, codes, with_rows, c->stream));
+int run_tiles(const hg_ctx* c, const RaggedArgs& a, int D, bool codes) {
+    const int rc = rc_of(D == 128 ? launch_ragged_wide(a, codes, c->stream) : launch_ragged_wide_d64(a, codes, c->stream));
     if (rc || a.tile_nsplit == 1) return rc;
     return rc_of(launch_ragged_join(a, D, c->stream));
 }
@@ -141,7 +145,7 @@ int hg_prompt_attn(hg_ctx* c, const void* Q, const void* K, const void* V, int64
     a.max_len = max_len;
     Room room = room_of(c);
     plan_tiles(a, D, room);
-    return run_tiles(c, a, D, false, false);
+    return run_tiles(c, a, D, false);
 }
 
 int hg_chunk_attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_t* q_off, int rows, const hg_paged_kv* kv, const int32_t* lengths,
@@ -177,15 +181,14 @@ int hg_chunk_attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_
     }
     Room room = room_of(c);
     plan_few_rows(a, D, room);
-    const bool few = a.few_tokens > 0, others = (int64_t)std::min(max_new, rows) * a.G > kFewRows;
-    int done = HG_OK;
-    if (others) {
+    int done;
+    if ((int64_t)std::min(max_new, rows) * a.G > kFewRows) {
         plan_tiles(a, D, room);
-        done = run_tiles(c, a, D, codes, few);
-    } else if (few) {
+        done = run_tiles(c, a, D, codes);
+    } else {
         done = rc_of(launch_ragged_rows(a, D, codes, c->stream));
     }
-    if (done == HG_OK && few && a.nsplit > 1) done = rc_of(launch_ragged_merge(a, D, c->stream));
+    if (done == HG_OK && a.nsplit > 1) done = rc_of(launch_ragged_merge(a, D, c->stream));
     return done;
 }
 

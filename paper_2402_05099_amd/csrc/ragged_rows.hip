@@ -54,8 +54,8 @@ __device__ __forceinline__ void store_joined(const OutDev& out, int64_t row, int
     store_row8<D>(out, row, c8, o, den > 0.f ? m + __logf(den) : -INFINITY);
 }
 
-// The rows that ragged_rows_kernel computed, PG groups of D / 8 lanes to a row, each with every PG-th of its parts (a row of many parts would be a chain of loads
-// otherwise); a workgroup takes 2048 / D / PG rows of the places for few_tokens tokens of every sequence.  Part p holds the keys from p * chunk on, so those
+// The rows of ragged_rows_impl.h, PG groups of D / 8 lanes to a row, each with every PG-th of its parts (a row of many parts would be a chain of loads
+// otherwise); a workgroup takes 2048 / D / PG of the places for few_most rows of every sequence and KV head.  Part p holds the keys from p * chunk on, so those
 // of a row are its first ceil(seen / chunk).
 template <int D, int PG>
 __global__ __launch_bounds__(256) void ragged_merge_kernel(RaggedArgs a) {
@@ -67,13 +67,13 @@ __global__ __launch_bounds__(256) void ragged_merge_kernel(RaggedArgs a) {
     int64_t row = 0;
     bool mine = false;
     if (at < a.part_rows) {
-        const int bt = (int)a.by_q_heads.of((unsigned)at), h = (int)at - bt * a.Hq;
-        const int b = (int)a.by_tokens.of((unsigned)bt), tok = bt - b * a.few_tokens;
+        const int bh = (int)a.by_most.of((unsigned)at), b = (int)a.by_heads.of((unsigned)bh), kvh = bh - b * a.Hkv;
         const RaggedSeq sq = ragged_seq(a, b);
-        mine = tok < sq.take && sq.take * a.G <= a.few_rows;
+        const int r = rows_in_tiles(sq.take * a.G, a.few_rows) + ((int)at - bh * a.few_most), tok = (int)a.by_group.of((unsigned)r);
+        mine = r < sq.take * a.G;
         const int seen = mine ? sq.seen(tok) : 0;
         parts = seen > 0 ? min((seen + a.chunk - 1) / a.chunk, a.nsplit) : 0;
-        row = (int64_t)(sq.q0 + tok) * a.Hq + h;
+        row = (int64_t)(sq.q0 + tok) * a.Hq + kvh * a.G + (r - tok * a.G);
     }
     float m = -INFINITY, den = 0.f, o[8] = {};
     join_parts<D>(a.part_O, a.part_L, a.part_rows, at, pg, PG, parts, c8, m, den, o);
@@ -98,12 +98,12 @@ __global__ __launch_bounds__(256) void ragged_merge_kernel(RaggedArgs a) {
     if (mine) store_joined<D>(a.out, row, c8, m, den, o);
 }
 
-// The others' rows, and prompts': a workgroup takes one token's rows from blockIdx.y * 2048 / D on.
+// The rows of tiles: a workgroup takes one token's rows from blockIdx.y * 2048 / D on.
 template <int D>
 __global__ __launch_bounds__(256) void ragged_join_kernel(RaggedArgs a) {
     constexpr int LPR = D / 8;
     const int token = blockIdx.x;
-    // the sequence that owns the token: the last that begins at or before it (tiles of one row, but for the room between the sequences)
+    // the sequence that owns the token: the last that begins at or before it 
     int lo = 0, n = a.B;
     const int lane = threadIdx.x & 63;
     while (true) {
@@ -116,7 +116,8 @@ __global__ __launch_bounds__(256) void ragged_join_kernel(RaggedArgs a) {
     }
     const RaggedSeq sq = ragged_seq(a, __builtin_amdgcn_readfirstlane(lo));
     const int tok = token - sq.q0, h = (int)blockIdx.y * (256 / LPR) + (int)threadIdx.x / LPR;
-    if (tok < 0 || tok >= sq.take || sq.take * a.G <= a.few_rows || h >= a.Hq) return;
+    if (tok < 0 || tok >= sq.take || h >= a.Hq) return;
+    if (tok * a.G + (h - (h / a.G) * a.G) >= rows_in_tiles(sq.take * a.G, a.few_rows)) return;
     const int seen = sq.seen(tok);
     float m = -INFINITY, den = 0.f, o[8] = {};
     join_parts<D>(a.tile_part_O, a.tile_part_L, (int64_t)a.rows * a.Hq, (int64_t)token * a.Hq + h, 0, 1,

@@ -1,4 +1,5 @@
-// Attention of a paged cache's few newest tokens (decode steps, drafted tokens): sequences with at most kFewRows query rows to a KV head.
+// Attention over a paged cache of what remains of a sequence's query rows behind its tiles, at most kFewRows to a KV head: all rows of decode steps and drafted
+// tokens, the last ones of a chunk.
 // What bounds it is the cache that is read, once for every KV head whatever the rows, so the rows of a head's group and of all
 // new tokens form one tile of 16 or 32 rows (v_mfma_f32_16x16x32_bf16, v_mfma_f32_32x32x16_bf16; decode_mfma_core.h has the products and the softmax).
 //
@@ -47,7 +48,7 @@ __device__ __forceinline__ void store_row8(const OutDev& out, int64_t row, int c
 
 // What workgroup `id` does for a sequence whose tiles have TR rows; everything up to the tile is known to the caller.
 template <int D, bool CODES, int TR, int NW>
-__device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, int sp, int kvh, int q0, int n, int len, int nrows) {
+__device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, int sp, int kvh, int q0, int n, int len, int row0, int nrows) {
     using Tile = MfmaTile<D, CODES, TR>;
     using G_ = Geo<D>;
     using R_ = RowsGeo<D, CODES, TR>;
@@ -55,9 +56,10 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
     const int l = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
 
-    if (rt * TR >= nrows) return;
+    const int r0 = row0 + rt * TR;      // the tile's first row; the sequence's rows are [0, nrows), those from row0 on are taken here
+    if (r0 >= nrows) return;
     const auto seen_by = [&](int t) { return len - (n - 1 - t); };
-    const int t_first = (int)a.by_group.of((unsigned)(rt * TR)), t_last = (int)a.by_group.of((unsigned)(min(rt * TR + TR, nrows) - 1));
+    const int t_first = (int)a.by_group.of((unsigned)r0), t_last = (int)a.by_group.of((unsigned)(min(r0 + TR, nrows) - 1));
     const int k0 = sp * a.chunk, ke = min(seen_by(t_last), k0 + a.chunk);      // keys [k0, ke)
     if (sp > 0 && k0 >= ke) return;      // (the join looks at no part that starts behind a row's keys)
     const int all_see = seen_by(t_first);       // every row of the tile sees the keys below
@@ -66,9 +68,9 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
     // ---- this lane's query row ----
     Tile t(a.scale, l);
     t.tau_raw = 0.f;      // sums follow every maximum: the largest weight of a row is 1, which bf16 holds exactly (with scores of many nats it is nearly the only one)
-    const int r = rt * TR + t.row();
+    const int r = r0 + t.row();
     const bool rv = r < nrows;
-    const int tok = (int)a.by_group.of((unsigned)(rv ? r : 0)), g = (rv ? r : 0) - tok * a.G;
+    const int tok = (int)a.by_group.of((unsigned)(rv ? r : r0)), g = (rv ? r : r0) - tok * a.G;
     const int seen = rv ? seen_by(tok) : 0;
     {
         const unsigned char* const qp = reinterpret_cast<const unsigned char*>(a.Q) + (int64_t)(q0 + tok) * a.q_stride + (kvh * a.G + g) * (D * 2);
@@ -188,7 +190,7 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
     __syncthreads();
     constexpr int LPR = D / 8;      // lanes per row, eight columns each
     for (int row = (int)threadIdx.x / LPR; row < TR; row += 64 * NW / LPR) {
-        const int rr = rt * TR + row;
+        const int rr = r0 + row;
         if (rr >= nrows) break;
         const int c8 = (int)threadIdx.x % LPR;
         float m = -INFINITY;
@@ -214,8 +216,8 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] *= inv;
         const int tk = (int)a.by_group.of((unsigned)rr), gg = rr - tk * a.G;
-        // one range: the result itself; several: part `sp`, whose rows have places for max_new tokens of every sequence
-        const int64_t at = a.nsplit == 1 ? (int64_t)(q0 + tk) * a.Hq + kvh * a.G + gg : ((int64_t)b * a.few_tokens + tk) * a.Hq + kvh * a.G + gg;
+        // one range: the result itself; several: part `sp`
+        const int64_t at = a.nsplit == 1 ? (int64_t)(q0 + tk) * a.Hq + kvh * a.G + gg : ((int64_t)b * a.Hkv + kvh) * a.few_most + (rr - row0);
         const float lse = den > 0.f ? m * a.scale + __logf(den) : -INFINITY;
         if (a.nsplit > 1) {
             float* const O = a.part_O + ((int64_t)sp * a.part_rows + at) * D + 8 * c8;
@@ -230,7 +232,7 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
 
 // Workgroup `id` of the launch: (range, tile, sequence, KV head), heads fastest, ranges slowest.  Later ranges and tiles are empty for most sequences; were they
 // to alternate with the first ones, workgroups, which go to the shader engines of an XCD in turn, would leave some of those with little to do (64 x 32/8 heads, up
-// to 4096 rows, two and four ranges 122 and 123 us so, 114 with one).  Sequences of at most 16 rows have tiles of 16, the others of 32 (`BOTH`: there may be such).
+// to 4096 rows, two and four ranges 122 and 123 us so, 114 with one).  At most 16 rows make a tile of 16, more of them tiles of 32 (`BOTH`: there may be more).
 template <int D, bool CODES, bool BOTH, int NW>
 __device__ __forceinline__ void rows_workgroup(const RaggedArgs& a, unsigned id) {
     typedef const __attribute__((address_space(4))) int32_t* const_i32;
@@ -243,9 +245,9 @@ __device__ __forceinline__ void rows_workgroup(const RaggedArgs& a, unsigned id)
     const int n = min(max(((const_i32)(uintptr_t)a.q_off)[b + 1], q0), a.rows) - q0;
     const int len = max(min(((const_i32)(uintptr_t)a.lengths)[b], a.max_len), 0);
     const int nrows = min(n, a.max_new) * a.G;
-    if (nrows > a.few_rows) return;
-    if (!BOTH || nrows <= 16) rows_tile<D, CODES, 16, NW>(a, b, rt, sp, kvh, q0, n, len, nrows);
-    else rows_tile<D, CODES, 32, NW>(a, b, rt, sp, kvh, q0, n, len, nrows);
+    const int row0 = rows_in_tiles(nrows, a.few_rows);
+    if (!BOTH || nrows - row0 <= 16) rows_tile<D, CODES, 16, NW>(a, b, rt, sp, kvh, q0, n, len, row0, nrows);
+    else rows_tile<D, CODES, 32, NW>(a, b, rt, sp, kvh, q0, n, len, row0, nrows);
 }
 
 }  // namespace rr

@@ -2,5 +2,4 @@
 #define HG_RW_D 128
 #define HG_RW_KERNEL ragged_wide_kernel
 #define HG_RW_LAUNCH launch_ragged_wide
-#define HG_RW_BOTH ragged_both_kernel
 #include "ragged_wide_impl.h"

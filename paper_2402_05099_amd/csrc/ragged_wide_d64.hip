@@ -2,5 +2,4 @@
 #define HG_RW_D 64
 #define HG_RW_KERNEL ragged_wide_kernel_d64
 #define HG_RW_LAUNCH launch_ragged_wide_d64
-#define HG_RW_BOTH ragged_both_kernel_d64
 #include "ragged_wide_impl.h"

@@ -1,5 +1,5 @@
 // Causal attention of packed tokens on the matrix cores, 128 query rows to a workgroup: the body shared by ragged_wide.hip (D = 128) and
-// ragged_wide_d64.hip (D = 64), which define HG_RW_D.  Sequences of more than a.few_rows query rows to a KV head: prompts, long chunks.
+// ragged_wide_d64.hip (D = 64), which define HG_RW_D.  Prompts, and long chunks but for what remains behind their tiles.
 //
 // Mathematics and pipeline are those of prefix_wide_impl.h (transposed products with v_mfma_f32_32x32x16_bf16, a lane owns one query row, weights
 // against a maximum that is only raised when their sum says so, one step = scores of stage j + 2, weights of stage j + 1 and P V of stage j, written out by
@@ -94,9 +94,9 @@ extern __shared__ __attribute__((aligned(1024))) unsigned char rw_smem[];
 
 }  // namespace
 
-// Workgroup `id` of the `n` that take tiles.
+// Workgroup `id` of those that take tiles.
 template <int MODE>
-__device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id, unsigned n) {
+__device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id) {
     constexpr bool PAGED = MODE != kDense, CODES = MODE == kCodes;
     constexpr int ES = CODES ? 1 : 2, NKS = k_slots(MODE), VRING = NKS * STB, CRING = VRING + NS * STB;
     constexpr int KOPS = CODES ? 1 : CPW;                            // copy instructions per stage, tensor and wavefront
@@ -106,28 +106,26 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id,
     unsigned char* const smem = rw_smem;
 
     // ---- which tile, which keys ----
-    int b, tile, kvh, sp;
+    int tile, kvh, sp;
+    RaggedSeq sq;
     {
-        const unsigned per_split = n / (unsigned)a.tile_nsplit;
-        sp = (int)(id / per_split);
-        const unsigned u = id - (unsigned)sp * per_split;
         // Workgroups whose ids are equal modulo 8 run on one XCD: the tiles of a KV head go to one of them, or to as few as there are heads for, so
-        // that its rows are in that XCD's L2.  The last tiles, which see the most keys, go first.
-        int number;
+        // that its rows are in that XCD's L2.  They go to the shader engines of an XCD in turn, whatever those have to do, so the numbers that are nobody's come
+        // last (key ranges slowest, with each range's own of these: drafted tokens behind up to 64K rows of codes, 48 and 30 workgroups to an engine).
+        unsigned v;
         if (a.Hkv % 8 == 0) {
-            const unsigned v = u >> 3;
-            number = (int)a.by_heads8.of(v);
-            kvh = (int)((v - (unsigned)number * (unsigned)(a.Hkv / 8)) * 8u + (u & 7u));
+            v = a.by_heads8.of(id >> 3);
+            kvh = (int)(((id >> 3) - v * (unsigned)(a.Hkv / 8)) * 8u + (id & 7u));
         } else {
-            number = (int)a.by_heads.of(u);
-            kvh = (int)(u - (unsigned)number * (unsigned)a.Hkv);
+            v = a.by_heads.of(id);
+            kvh = (int)(id - v * (unsigned)a.Hkv);
         }
-        number = a.tiles_all - 1 - number;
-        if (!ragged_tile<kTileRows>(a, number, b, tile)) return;
+        const int rank = (int)(v / (unsigned)a.tile_nsplit);
+        sp = (int)(v - (unsigned)rank * (unsigned)a.tile_nsplit);
+        if (!tile_of_rank(a, rank, sq, tile)) return;
     }
-    const RaggedSeq sq = ragged_seq(a, b);
-    const int nrows = __builtin_amdgcn_readfirstlane(sq.take * a.G), row0 = tile * kTileRows;
-    if (row0 >= nrows || nrows <= a.few_rows) return;
+    const int b = __builtin_amdgcn_readfirstlane(sq.b);
+    const int nrows = __builtin_amdgcn_readfirstlane(rows_in_tiles(sq.take * a.G, a.few_rows)), row0 = tile * kTileRows;      // rows that tiles take
     const int q0 = __builtin_amdgcn_readfirstlane(sq.q0);
     const int before = __builtin_amdgcn_readfirstlane(sq.len - (sq.n - 1));      // keys that the sequence's first token sees
     const int tid = threadIdx.x, l = tid & 63, lq = l & 31, hl = l >> 5;
@@ -360,40 +358,35 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id,
     lds_done();
     meet();
 
-#pragma unroll
-    for (int i = 0; i < DB; ++i)
-#pragma unroll
-        for (int k = 0; k < 16; ++k) Oacc[i][k] = 0.f;
-    lsum = lround = 0.f;
-    mc = 0.f;
     uintx4 kf[NKF];
     shortx8 vf[NVF];
     STile SA, SB;
     uintx4 PA[KT / 16], PB[KT / 16];
-    const auto scores = [&](int slot, STile& S) {
-        uintx4 kk[KB * KS];
+    if (mine > 0) {      // scores of the first two stages, product by product in turn (each waits for its own one before)
+        uintx4 k0[KB * KS], k1[KB * KS];
 #pragma unroll
-        for (int q = 0; q < KB * KS; ++q) kk[q] = lds_k(slot, q);
+        for (int q = 0; q < KB * KS; ++q) { k0[q] = lds_k(0, q); k1[q] = lds_k(1, q); }
 #if HG_RW_D == 128
-        mfma_first(S, kk[0], qf[0]);
+        mfma_first(SB, k0[0], qf[0]);
+        mfma_first(SA, k1[0], qf[0]);
 #pragma unroll
-        for (int q = 1; q < KS; ++q) mfma_acc(S, kk[q], qf[q]);
-        asm volatile("s_nop 11" : "+v"(S));
-        __builtin_amdgcn_sched_barrier(0);
+        for (int q = 1; q < KS; ++q) { mfma_acc(SB, k0[q], qf[q]); mfma_acc(SA, k1[q], qf[q]); }
+        asm volatile("s_nop 11" : "+v"(SB), "+v"(SA));
 #else
-        mfma_first(S.a, kk[0], qf[0]);
-        mfma_first(S.b, kk[KS], qf[0]);
+        mfma_first(SB.a, k0[0], qf[0]);
+        mfma_first(SB.b, k0[KS], qf[0]);
+        mfma_first(SA.a, k1[0], qf[0]);
+        mfma_first(SA.b, k1[KS], qf[0]);
 #pragma unroll
         for (int q = 1; q < KS; ++q) {
-            mfma_acc(S.a, kk[q], qf[q]);
-            mfma_acc(S.b, kk[KS + q], qf[q]);
+            mfma_acc(SB.a, k0[q], qf[q]);
+            mfma_acc(SB.b, k0[KS + q], qf[q]);
+            mfma_acc(SA.a, k1[q], qf[q]);
+            mfma_acc(SA.b, k1[KS + q], qf[q]);
         }
-        asm volatile("s_nop 11" : "+v"(S.a), "+v"(S.b));
+        asm volatile("s_nop 11" : "+v"(SB.a), "+v"(SB.b), "+v"(SA.a), "+v"(SA.b));
 #endif
-    };
-    if (mine > 0) {
-        scores(0, SB);
-        scores(1, SA);
+        __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (CODES) {
         // K of stage 2 takes the slot of stage 0 when everyone has its scores
@@ -403,6 +396,12 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id,
         meet();
         if (4 < nst) copy_stage(4, 4, true, TAIL);
     }
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) Oacc[i][k] = 0.f;
+    lsum = lround = 0.f;
+    mc = 0.f;
     if (mine > 0) {
         if (k0 + KT > w_least) mask_stage(SB, 0);
         // (a finite number for a row with nothing but -inf, see prefix_wide_impl.h)
@@ -534,7 +533,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id,
         careful_expand(j);
     }
 
-    // ---- results: through LDS as whole lines, 32 columns of a wavefront's 32 rows at a time (the ring is free once everyone is here) ----
+    // ---- results: a wavefront's 32 rows through LDS, to leave as whole lines (the ring is free once everyone is here) ----
     wait_vm<0>();
     meet();
     if (!any) return;
@@ -547,29 +546,41 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id,
         if (in_parts) a.tile_part_L[(int64_t)sp * a.rows * a.Hq + row_at] = lse;
         else if (a.out.LSE) a.out.LSE[row_at] = lse;
     }
-    unsigned char* const stg = smem + w * 4096;
-    const int my_row = rv ? (int)row_at : -1;
-    int row_of[4];
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk) row_of[kk] = __shfl(my_row, 8 * kk + (l >> 3));
     float* const Of = in_parts ? a.tile_part_O + (int64_t)sp * a.rows * a.Hq * D : static_cast<float*>(a.out.O);
     uint16_t* const Ob = static_cast<uint16_t*>(a.out.O);
-    const bool out_bf16 = a.out.bf16 && !in_parts;
+    const int my_row = rv ? (int)row_at : -1;
+    const auto element = [&](int db, int q4, int i) { return Oacc[db][4 * q4 + i] * inv; };      // column 32 db + 8 q4 + 4 hl + i of row lq
+    if (a.out.bf16 && !in_parts) {
+        unsigned char* const stg = smem + w * (32 * ROWB);
+        // pieces of four columns, 8 bytes, at piece ^ 2 (row % 8): rows are 256 (128) bytes, a whole number of bank periods (half a one)
 #pragma unroll
-    for (int db = 0; db < DB; ++db) {
+        for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4)
-            *reinterpret_cast<float4*>(stg + lq * 128 + (((2 * q4 + hl) ^ (lq & 7)) * 16)) =
-                make_float4(Oacc[db][4 * q4] * inv, Oacc[db][4 * q4 + 1] * inv, Oacc[db][4 * q4 + 2] * inv, Oacc[db][4 * q4 + 3] * inv);
+            for (int q4 = 0; q4 < 4; ++q4)
+                *reinterpret_cast<uint2*>(stg + lq * ROWB + (((8 * db + 2 * q4 + hl) ^ (2 * (lq & 7))) * 8)) =
+                    make_uint2(pack_bf16_pair(element(db, q4, 0), element(db, q4, 1)), pack_bf16_pair(element(db, q4, 2), element(db, q4, 3)));
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            const int rr = 8 * kk + (l >> 3), c = l & 7;
-            const float4 v = *reinterpret_cast<const float4*>(stg + rr * 128 + ((c ^ (rr & 7)) * 16));
-            if (row_of[kk] >= 0) {
-                const int64_t at = (int64_t)row_of[kk] * D + 32 * db + 4 * c;
-                if (out_bf16) *reinterpret_cast<uint2*>(Ob + at) = make_uint2(pack_bf16_pair(v.x, v.y), pack_bf16_pair(v.z, v.w));
-                else *reinterpret_cast<float4*>(Of + at) = v;
-            }
+        for (int kk = 0; kk < 32 / RPI; ++kk) {
+            const int rr = RPI * kk + l / CPR, c = l % CPR;
+            const uint4 v = *reinterpret_cast<const uint4*>(stg + rr * ROWB + ((c ^ (rr & 7)) * 16));
+            const int row = __shfl(my_row, rr);
+            if (row >= 0) *reinterpret_cast<uint4*>(Ob + (int64_t)row * D + 8 * c) = v;
+        }
+    } else {
+        unsigned char* const stg = smem + w * (32 * 2 * ROWB);
+        constexpr int PCS = D / 4;      // 16-byte pieces of an fp32 row
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4)
+                *reinterpret_cast<float4*>(stg + lq * (2 * ROWB) + (((8 * db + 2 * q4 + hl) ^ (lq & 15)) * 16)) =
+                    make_float4(element(db, q4, 0), element(db, q4, 1), element(db, q4, 2), element(db, q4, 3));
+#pragma unroll
+        for (int kk = 0; kk < 32 * PCS / 64; ++kk) {
+            const int rr = (64 / PCS) * kk + l / PCS, c = l % PCS;
+            const float4 v = *reinterpret_cast<const float4*>(stg + rr * (2 * ROWB) + ((c ^ (rr & 15)) * 16));
+            const int row = __shfl(my_row, rr);
+            if (row >= 0) *reinterpret_cast<float4*>(Of + (int64_t)row * D + 4 * c) = v;
         }
     }
 }
@@ -578,45 +589,41 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id,
 
 using namespace rw;
 
+// Packed rows: tiles are all there is.  Paged rows: what remains behind the tiles is in the same launch, the tiles first: they are bound by the matrix pipes, the
+// others by the reads of their cache, and two workgroups of either kind share a CU.
 template <int MODE>
-__global__ __launch_bounds__(64 * NW, 2) void HG_RW_KERNEL(RaggedArgs a) { tile_workgroup<MODE>(a, blockIdx.x, gridDim.x); }
-
-// Both kinds of sequences in one launch, the tiles first: they are bound by the matrix pipes, the few rows by the reads of their cache, and two
-// workgroups of either kind share a CU.
-template <int MODE>
-__global__ __launch_bounds__(64 * NW, 2) void HG_RW_BOTH(RaggedArgs a) {
-    const unsigned n = (unsigned)a.tiles_all * (unsigned)a.Hkv * (unsigned)a.tile_nsplit;
-    if (blockIdx.x < n) tile_workgroup<MODE>(a, blockIdx.x, n);
-    else rr::rows_workgroup<D, MODE == kCodes, true, NW>(a, blockIdx.x - n);
+__global__ __launch_bounds__(64 * NW, 2) void HG_RW_KERNEL(RaggedArgs a) {
+    if constexpr (MODE == kDense) {
+        tile_workgroup<MODE>(a, blockIdx.x);
+    } else {
+        const unsigned n = (unsigned)a.tiles_all * (unsigned)a.Hkv * (unsigned)a.tile_nsplit;
+        if (blockIdx.x < n) tile_workgroup<MODE>(a, blockIdx.x);
+        else rr::rows_workgroup<D, MODE == kCodes, true, NW>(a, blockIdx.x - n);
+    }
 }
 
-template <int MODE, bool BOTH>
-static hipError_t launch_mode(const RaggedArgs& a, unsigned grid, hipStream_t s) {
-    constexpr int bytes = BOTH ? std::max(lds_bytes(MODE), rr::rows_lds<D, MODE == kCodes, true>(NW)) : lds_bytes(MODE);
+template <int MODE>
+static hipError_t launch_mode(const RaggedArgs& a, hipStream_t s) {
+    constexpr int bytes = MODE == kDense ? lds_bytes(MODE) : std::max(lds_bytes(MODE), rr::rows_lds<D, MODE == kCodes, true>(NW));
     static_assert(bytes <= 81920, "two workgroups to a CU");
+    const int64_t grid = (int64_t)a.tiles_all * a.Hkv * a.tile_nsplit + (MODE == kDense ? 0 : rows_grid(a));
+    if (grid >= (1LL << 31)) return hipErrorInvalidValue;
     static bool attr_set[64] = {};
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
     if (dev < 0 || dev >= 64 || !attr_set[dev]) {
-        const void* f;
-        if constexpr (BOTH) f = reinterpret_cast<const void*>(&HG_RW_BOTH<MODE>);
-        else f = reinterpret_cast<const void*>(&HG_RW_KERNEL<MODE>);
-        e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&HG_RW_KERNEL<MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
         if (dev >= 0 && dev < 64) attr_set[dev] = true;
     }
-    if constexpr (BOTH) HG_RW_BOTH<MODE><<<grid, 64 * NW, bytes, s>>>(a);
-    else HG_RW_KERNEL<MODE><<<grid, 64 * NW, bytes, s>>>(a);
+    HG_RW_KERNEL<MODE><<<(unsigned)grid, 64 * NW, bytes, s>>>(a);
     return hipGetLastError();
 }
 
-hipError_t HG_RW_LAUNCH(const RaggedArgs& a, bool codes, bool with_rows, hipStream_t s) {
-    const int64_t tiles = (int64_t)a.tiles_all * a.Hkv * a.tile_nsplit, grid = tiles + (with_rows ? rows_grid(a) : 0);
-    if (grid >= (1LL << 31)) return hipErrorInvalidValue;
-    if (!a.pg.table) return launch_mode<kDense, false>(a, (unsigned)grid, s);
-    if (with_rows) return codes ? launch_mode<kCodes, true>(a, (unsigned)grid, s) : launch_mode<kPaged, true>(a, (unsigned)grid, s);
-    return codes ? launch_mode<kCodes, false>(a, (unsigned)grid, s) : launch_mode<kPaged, false>(a, (unsigned)grid, s);
+hipError_t HG_RW_LAUNCH(const RaggedArgs& a, bool codes, hipStream_t s) {
+    if (!a.pg.table) return launch_mode<kDense>(a, s);
+    return codes ? launch_mode<kCodes>(a, s) : launch_mode<kPaged>(a, s);
 }
 
 }  // namespace hg
