@@ -105,16 +105,17 @@ void plan_few_rows(RaggedArgs& a, int D, Room& room) {
 }
 
 // Tiles.  A call of few tiles splits their keys; what that saves is weighed against the parts' way through memory and the join, from the host's bounds (tokens and
-// longest context; contexts are taken to be three quarters of that on average): 512 workgroups run at a time, 0.9 us a stage of 32 keys, or 0.75 where they have
-// little company; parts are written and read at 4.5 TB/s.
+// longest context; contexts are taken to be three quarters of that on average).  512 workgroups run at a time, so their number is made to go into whole rounds; a
+// stage of 32 keys takes 0.95 us, 0.6 where a workgroup has its CU to itself, a workgroup 8 us beside its stages; parts are written and read at 4.5 TB/s.
 void plan_tiles(RaggedArgs& a, int D, Room& room) {
     const double wgs = (double)(((int64_t)a.rows * a.G + kTile - 1) / kTile) * a.Hkv, stages = a.max_len * (D == 128 ? 1.0 : 0.5) / 32.0;
-    const double all = wgs * 0.75 * stages * 0.9 / 512.0, longest = stages * 0.75, part = 8.0 * a.rows * a.Hq * (D + 1) / 4.5e6;
+    const double part = 8.0 * a.rows * a.Hq * (D + 1) / 4.5e6;
     int best = 1;
-    double least = 0.9 * std::max(all, longest);
-    for (int s = 2; wgs < 512.0 && s <= std::min(64, a.max_len / 1024); ++s) {
-        const double us = std::max(all, longest / s) + 0.5 * longest / s + part * s + 6.0;
-        if (us < least) { least = us; best = s; }
+    double least = 1e300;
+    for (int s = 1; s <= std::max(1, std::min(64, a.max_len / 1024)); ++s) {
+        const double n = 0.75 * wgs * s, us = std::max(1.0, ceil(n / 512.0)) * (stages / s * (n <= 256.0 ? 0.6 : 0.95) + 8.0) + (s > 1 ? part * s + 6.0 : 0.0);
+        if (us < (best == 1 ? 0.9 : 1.0) * least) { least = us; best = s; }      // (a tenth at least, or there is nothing to join)
+        if (wgs >= 512.0) break;
     }
     split_keys(best, a.max_len, 1024, 64, (int64_t)a.rows * a.Hq, D, room, a.tile_nsplit, a.tile_chunk, a.tile_part_O, a.tile_part_L);
 }

@@ -300,20 +300,32 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
         }
     };
 
-    // ---- start: the first stages, Q, the stages behind them ----
-    const std::true_type TAIL{};
-    if constexpr (PAGED) look_up(0);
-    if constexpr (CODES) {
-        static_assert(kCodeSlots == 4, "");
-#pragma unroll
-        for (int s = 0; s < kCodeSlots; ++s) {
-            if (s < nst) copy_stage(s, s, true, TAIL);
-            if (s < nst) copy_stage(s, s, false, TAIL);
+    // Copies of the start and of careful steps: with a look at the tensor's end only where the tile's keys come near it.
+    const bool edge = !PAGED && q0 + k0 + nst * KT > a.rows;
+    const auto copy_some = [&](auto what) {
+        if constexpr (PAGED) {
+            what(std::false_type{});
+        } else {
+            if (__builtin_expect(edge, 0)) what(std::true_type{});
+            else what(std::false_type{});
         }
-    } else {
-        if (0 < nst) { copy_stage(0, 0, true, TAIL); copy_stage(0, 0, false, TAIL); }
-        if (1 < nst) copy_stage(1, 1, true, TAIL);
-    }
+    };
+
+    // ---- start: the first stages, Q, the stages behind them ----
+    if constexpr (PAGED) look_up(0);
+    copy_some([&](auto tail) {
+        if constexpr (CODES) {
+            static_assert(kCodeSlots == 4, "");
+#pragma unroll
+            for (int s = 0; s < kCodeSlots; ++s) {
+                if (s < nst) copy_stage(s, s, true, tail);
+                if (s < nst) copy_stage(s, s, false, tail);
+            }
+        } else {
+            if (0 < nst) { copy_stage(0, 0, true, tail); copy_stage(0, 0, false, tail); }
+            if (1 < nst) copy_stage(1, 1, true, tail);
+        }
+    });
     bf16x8 qf[KS];
     {
         const unsigned char* const qp = reinterpret_cast<const unsigned char*>(a.Q) + (int64_t)(q0 + tok) * a.q_stride + head * ROWB + 16 * hl;
@@ -344,15 +356,19 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
         if (1 < nst) { expand(1, true); expand(1, false); }
         if (partial == 0) clear_rows(0);
         if (partial == 1) clear_rows(1);
-        if (4 < nst) { copy_stage(4, 4, true, TAIL); copy_stage(4, 4, false, TAIL); }
-        if (5 < nst) copy_stage(5, 5, true, TAIL);
+        copy_some([&](auto tail) {
+            if (4 < nst) { copy_stage(4, 4, true, tail); copy_stage(4, 4, false, tail); }
+            if (5 < nst) copy_stage(5, 5, true, tail);
+        });
     } else {
         if (partial == 0) clear_rows(0);
         // (in this order: step 0 waits for all but the last K and the last V)
-        if (2 < nst) copy_stage(2, 2, true, TAIL);
-        if (1 < nst) copy_stage(1, 1, false, TAIL);
-        if (3 < nst) copy_stage(3, 3, true, TAIL);
-        if (2 < nst) copy_stage(2, 2, false, TAIL);
+        copy_some([&](auto tail) {
+            if (2 < nst) copy_stage(2, 2, true, tail);
+            if (1 < nst) copy_stage(1, 1, false, tail);
+            if (3 < nst) copy_stage(3, 3, true, tail);
+            if (2 < nst) copy_stage(2, 2, false, tail);
+        });
         // K of stage 4 has the slot of stage 0, whose scores are taken first
     }
     lds_done();
@@ -394,7 +410,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
         if (2 < nst) { expand(2, true); }
     } else {
         meet();
-        if (4 < nst) copy_stage(4, 4, true, TAIL);
+        copy_some([&](auto tail) { if (4 < nst) copy_stage(4, 4, true, tail); });
     }
 #pragma unroll
     for (int i = 0; i < DB; ++i)
@@ -455,8 +471,10 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
         meet();
     };
     const auto careful_copies = [&](int j) {
-        if (j + KA < nst) copy_stage(j + KA, j + KA, true, TAIL);
-        if (j + VA < nst) copy_stage(j + VA, j + VA, false, TAIL);
+        copy_some([&](auto tail) {
+            if (j + KA < nst) copy_stage(j + KA, j + KA, true, tail);
+            if (j + VA < nst) copy_stage(j + VA, j + VA, false, tail);
+        });
     };
     const auto careful_expand = [&](int j) {
         if constexpr (CODES) {
