@@ -511,3 +511,82 @@ def test_nothing_to_do_is_fine():
     hb.hg_kv_write_paged(ctx, e, e, torch.zeros(0, dtype=torch.int32, device=DEV), kv)
     torch.cuda.synchronize()
     ctx.close()
+
+
+def test_same_results_through_the_checks_in_python(monkeypatch):
+    """the native marshalling and the checks in Python make the same calls"""
+    calls = []
+    for native in (hb.native(), hb._PythonOnly):
+        monkeypatch.setattr(hb, "_native", native)
+        run_prompt([40, 3, 200], (8, 2), 128, fused=True, lse=False)
+        run_chunk([(300, 33), (65, 1), (3, 5)], (8, 2), 64, codes=True, fused=True, mib=16)
+        run_slots([3, 40, 9], [5, 20, 100], 16, 60, 60)
+        calls.append(native)
+    assert len(calls) == 2
+    m = hb.native() if hb._native is not hb._PythonOnly else calls[0]
+    q = torch.zeros(2, 2, 64, dtype=torch.bfloat16)      # host tensors: left to Python
+    assert m.prompt(None, q, q, q, q, 1, q, q, 0.0) is None and m.chunk(*[object()] * 10) is None
+    assert m.slots() is None and m.write(1, 2, 3, 4, 5) is None
+
+
+# ---- where tiles end and what remains begins ---------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_every_kind_of_remainder(D, codes):
+    # one row a token: 128-row tiles, and behind them 0, 1, 16, 17, 32, 33, 64 (few rows) or 65, 127 rows (a tile)
+    for counts in ([64, 65, 127, 128, 129], [144, 145, 160, 161, 192, 193, 255, 256, 257]):
+        run_chunk([(n + 37 * i, n) for i, n in enumerate(counts)], (2, 2), D, codes=codes, mib=16)
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("heads", [(80, 1), (64, 1), (9, 3), (14, 2)])
+def test_groups_of_heads_of_every_size(heads, codes):
+    run_chunk([(100, 1), (90, 2), (77, 3), (200, 40), (5, 0)], heads, 64, codes=codes, mib=16)
+    if not codes:
+        run_prompt([1, 2, 3, 30, 70], heads, 64)
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_tokens_of_long_chunks_that_see_nothing(D, codes):
+    run_chunk([(200, 300), (0, 200), (100, 400), (1, 130)], (2, 2), D, codes=codes, mib=16)
+    run_chunk([(5, 200), (300, 290)], (8, 2), D, codes=codes, fp32=True)
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("B", [8, 9, 64, 65, 150])
+def test_long_chunks_among_many_sequences(B, codes):
+    run_chunk([(40 + 7 * i % 90 + n, n) for i, n in ((i, (1, 0, 150, 1, 70, 1, 1, 33)[i % 8]) for i in range(B))], (4, 2), 64, codes=codes, mib=16, lead=1)
+    if not codes:
+        run_prompt([(1, 0, 150, 3, 70)[i % 5] for i in range(B)], (4, 2), 64, lead=3, trail=2)
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_tiles_of_long_contexts_are_split(D, codes):
+    run_chunk([(17000, 140)], (2, 2), D, codes=codes, mib=256, ps=64)
+    run_chunk([(9000, 130), (12000, 1), (300, 200), (2048, 64)], (4, 2), D, codes=codes, mib=256, ps=64, fp32=True)
+    run_chunk([(9000, 130), (12000, 1)], (4, 2), D, codes=codes, mib=256, ps=64, lse=False)
+
+
+def test_a_long_prompt_of_one_head_is_split():
+    run_prompt([5000], (1, 1), 128, mib=256)
+    run_prompt([4000, 17], (1, 1), 64, mib=256, fp32=True)
+
+
+def test_the_same_call_gives_the_same_bits():
+    g = torch.Generator().manual_seed(2)
+    pairs = [(5000, 140), (9000, 1), (300, 33)]
+    Kp, Vp, table, _, _ = make_cache(g, [r for r, _ in pairs], 2, 128, 64, False)
+    off = offsets([n for _, n in pairs])
+    Q = rand(g, int(off[-1]), 8, 128).to(DEV)
+    kv = hb.PagedKV(K=Kp, V=Vp, page_table=table, page_size=64)
+    ctx = context(64)
+    got = []
+    for _ in range(3):
+        O, L = torch.empty(int(off[-1]), 8, 128, device=DEV), torch.empty(int(off[-1]), 8, device=DEV)
+        hb.hg_chunk_attn_paged(ctx, Q, i32(off), kv, i32([r for r, _ in pairs]), 140, 9000, O, L)
+        got.append((O.clone(), L.clone()))
+    assert all(torch.equal(a, b) for g_ in got[1:] for a, b in zip(g_, got[0]))
+    ctx.close()
