@@ -13,7 +13,7 @@ none of them, so they go evenly into all the gaps, and the row sum is there befo
 says whether they have to be taken again against a larger maximum, which spares every step the search for it.
 
 The ragged form (ragged_wide_step.inc, ragged_wide_step_d64.inc, for ragged_wide_impl.h) has the same order with two differences: its copies are the kernel's
-own (issue_k, issue_v; read_k, read_v and, several products later, work_k, work_v are empty but over 8-bit rows), and the sum of the rounded weights is taken beside that of the unrounded ones.
+own (issue_k, issue_v; read_k and, several products later, work_k are empty but over 8-bit rows, whose V fragments v_operand makes bf16), and the sum of the rounded weights is taken beside that of the unrounded ones.
 
 usage: gen_prefix_wide_step.py [D [out.inc [vector-ALU cycles per gap]]]     (no arguments: all files)
 """
@@ -42,7 +42,8 @@ def build(D=128, CAP=None, ragged=False):
     mf = []         # [MFMA statement, statements before the gap's ALU work, statements after it]
 
     def value(i):
-        return f"mfma_acc(Oacc[{i % DB}], vf[{i & 3}], pb[{i // DB}]);"
+        v = f"v_operand(vf[{i & 3}])" if ragged else f"vf[{i & 3}]"
+        return f"mfma_acc(Oacc[{i % DB}], {v}, pb[{i // DB}]);"
 
     def v_load(i, slot):      # fragment i (0 .. 7) of a stage's V
         return f"vf[{i & 3}] = lds_v({slot}, {i // DB}, {i % DB});"
@@ -60,10 +61,8 @@ def build(D=128, CAP=None, ragged=False):
     if ragged:
         mf[0][1].append("issue_k(j, slot);")
         mf[2][1].append("issue_v(j, slot);")
-        mf[1][1].append("read_k(slot);")
-        mf[4][1].append("read_v(slot);")
-        mf[7][1].append("work_k(slot);")
-        mf[11][1].append("work_v(slot);")
+        mf[4][1].append("read_k(slot);")
+        mf[9][1].append("work_k(slot);")
     else:
         mf[0][1].extend(["const int64_t cp_off = (int64_t)min(cur.ks + cur.t * KT, cur.kwin) * rstride_b;",
                          "const unsigned cp_dst = ldsw + (unsigned)((slot + AHEAD) & (NS - 1)) * STB;"])

@@ -10,8 +10,9 @@
 //   * K and V have rings of their own: in step j the K of stages j + 3 .. j + 5 and the V of j + 2 and j + 3 are in flight.  One barrier per step.
 //   * A row's own tokens bound its keys: steps that reach that bound, or the end of the keys, mask the scores and copy with care (`kCareful`).
 //   * Paged rows: a wavefront copies rows of one page per stage; the pages of its next 64 stages lie in the lanes of a register.
-//   * Codes are copied to a staging ring of the wavefront's own, and become bf16 on the way from there into the K and V rings: the
-//     pipeline behind is the same, and every code is expanded once per workgroup, not once per wavefront.
+//   * Codes of K are copied to a staging ring of the wavefront's own, and become bf16 on the way from there into the K ring, once per workgroup; those of V stay
+//     codes in LDS and become bf16 behind the transposing read, in every wavefront.  The LDS is what codes press on (K and V both expanded into rings: 1767 cycles a
+//     stage where bf16 rows take 1417, of which the LDS needs some 770 for each of a CU's two workgroups), and this way the vector ALU carries half of it.
 //   * The output is divided by the sum of the rounded weights (LSE has the sum of the unrounded ones): where one key has nearly all the weight its rounding
 //     would otherwise show in O as a whole, since the largest weight is anywhere up to kMostWeight and not a power of two.
 #include <algorithm>
@@ -46,19 +47,27 @@ constexpr float kRoom = 16.f;
 static_assert(CPW == 2 && RPW <= 16, "a wavefront's rows of a stage lie in one page");
 
 enum { kDense = 0, kPaged = 1, kCodes = 2 };
-// LDS: K ring, V ring, and for codes the wavefronts' staging rings
+// LDS: K ring (bf16), V ring (bf16 or codes), and for codes the wavefronts' staging rings of K
 constexpr int k_slots(int mode) { return mode == kCodes ? 2 : 4; }
-constexpr int kCodeSlots = 4, kCodeBytes = 2 * RPW * D;      // per wavefront and stage: its rows of K, then of V
-constexpr int lds_bytes(int mode) { return (k_slots(mode) + NS) * STB + (mode == kCodes ? NW * kCodeSlots * kCodeBytes : 0); }
+constexpr int v_stage(int mode) { return mode == kCodes ? STB / 2 : STB; }
+constexpr int kCodeSlots = 4, kCodeBytes = RPW * D;      // staging: stages, and bytes of a wavefront's rows of one
+constexpr int lds_bytes(int mode) {
+    const int ring = k_slots(mode) * STB + NS * v_stage(mode) + (mode == kCodes ? NW * kCodeSlots * kCodeBytes : 0), results = NW * 32 * 2 * ROWB;
+    return ring > results ? ring : results;
+}
+static_assert(kCodeBytes == 1024, "one copy instruction per wavefront, stage and tensor of codes");
 static_assert(lds_bytes(kCodes) <= 81920 && lds_bytes(kDense) <= 81920, "two workgroups to a CU");
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+typedef int intx2 __attribute__((ext_vector_type(2)));
 
 // XOR swizzles of the 16-byte chunks of LDS row `row`, as in prefix_wide_impl.h
 __device__ __forceinline__ int kswz(int row) { return D == 128 ? row % 16 : (row >> 1) & 7; }
 __device__ __forceinline__ int vswz(int row) { return D == 128 ? 4 * (row % 4) : 4 * ((row >> 1) & 1); }
+// ... and of those of a row of V codes (as decode_mfma_core.h has it for 128-byte rows; 64-byte rows: the eight rows of a transposing read are 0 .. 3 and 8 .. 11)
+__device__ __forceinline__ int cswz(int row) { return D == 128 ? ((row >> 1) & 1) | (((row >> 3) & 1) << 1) : 2 * ((row >> 3) & 1); }
 
 #if HG_RW_D == 128
 typedef floatx16 STile;
@@ -98,11 +107,11 @@ extern __shared__ __attribute__((aligned(1024))) unsigned char rw_smem[];
 template <int MODE>
 __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id) {
     constexpr bool PAGED = MODE != kDense, CODES = MODE == kCodes;
-    constexpr int ES = CODES ? 1 : 2, NKS = k_slots(MODE), VRING = NKS * STB, CRING = VRING + NS * STB;
+    constexpr int ES = CODES ? 1 : 2, NKS = k_slots(MODE), VRING = NKS * STB, VSTB = v_stage(MODE), CRING = VRING + NS * VSTB;
     constexpr int KOPS = CODES ? 1 : CPW;                            // copy instructions per stage, tensor and wavefront
-    // How far ahead of step j the copies run, and what the step needs: K of stage j + 2, V of stage j + 1.  Codes: the stages that step j expands
-    // (K of j + 3, V of j + 2) were requested kCodeSlots - 1 steps before.
-    constexpr int KA = CODES ? 3 + kCodeSlots - 1 : 5, VA = CODES ? 2 + kCodeSlots - 1 : 3;
+    // How far ahead of step j the copies run; the step needs K of stage j + 2 and V of stage j + 1.  Codes: the K that step j expands (of stage j + 3) was requested
+    // kCodeSlots - 1 steps before.
+    constexpr int KA = CODES ? 3 + kCodeSlots - 1 : 5, VA = 3;
     unsigned char* const smem = rw_smem;
 
     // ---- which tile, which keys ----
@@ -153,7 +162,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
 #pragma unroll
     for (int i = 0; i < KOPS; ++i)
         voffK[i] = (unsigned)lrow * (unsigned)kv_stride + (CODES ? (unsigned)lch : (unsigned)(lch ^ kswz(w * RPW + i * RPI + lrow))) * 16u;
-    voffV = (unsigned)lrow * (unsigned)kv_stride + (CODES ? (unsigned)lch : (unsigned)(lch ^ vswz(lrow))) * 16u;      // (rows RPI and RPW apart share their V swizzle)
+    voffV = (unsigned)lrow * (unsigned)kv_stride + (unsigned)(lch ^ (CODES ? cswz(w * RPW + lrow) : vswz(lrow))) * 16u;      // (bf16 rows RPI and RPW apart share their V swizzle)
     const unsigned lds0 = (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)HG_LDS(smem));
     const unsigned lds_rows = lds0 + (unsigned)(w * RPW * ROWB);
     const unsigned char* const Kh = a.K + (int64_t)kvh * (D * ES);
@@ -186,7 +195,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
     const auto copy_stage = [&](int s, int at, bool is_k, auto tail) {
         const unsigned char* const tensor = is_k ? Kh : Vh;
         unsigned dst;
-        if constexpr (CODES) dst = lds0 + (unsigned)(CRING + w * (kCodeSlots * kCodeBytes) + (at % kCodeSlots) * kCodeBytes + (is_k ? 0 : RPW * D));
+        if constexpr (CODES) dst = lds0 + (unsigned)(is_k ? CRING + w * (kCodeSlots * kCodeBytes) + (at % kCodeSlots) * kCodeBytes : VRING + (at % NS) * VSTB + w * kCodeBytes);
         else dst = lds_rows + (unsigned)((is_k ? 0 : VRING) + (at % (is_k ? NKS : NS)) * STB);
         if constexpr (decltype(tail)::value && !PAGED) {
 #pragma unroll
@@ -201,26 +210,23 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
             for (int i = 0; i < KOPS; ++i) copy16(scalar(first + (int64_t)(i * RPI) * kv_stride), is_k ? voffK[i] : voffV, dst + (unsigned)i * 1024u);
         }
     };
-    // codes: this wavefront's rows of stage s out of the staging ring, and as bf16 into the K or V ring (`at`: s, or a number equal to it modulo 4)
-    const auto read_codes = [&](int at, bool is_k) -> uintx4 {
-        return *reinterpret_cast<const uintx4*>(smem + CRING + w * (kCodeSlots * kCodeBytes) + (at % kCodeSlots) * kCodeBytes + (is_k ? 0 : RPW * D) + l * 16);
+    // codes: this wavefront's rows of K out of the staging ring, and as bf16 into the K ring (`at`: the stage, or a number equal to it modulo 4)
+    const auto read_codes = [&](int at) -> uintx4 {
+        return *reinterpret_cast<const uintx4*>(smem + CRING + w * (kCodeSlots * kCodeBytes) + (at % kCodeSlots) * kCodeBytes + l * 16);
     };
-    const auto write_rows = [&](int at, bool is_k, const uintx4& c) {
-        unsigned char* const to = smem + (is_k ? 0 : VRING) + (at % (is_k ? NKS : NS)) * STB;
+    const auto bf16_of = [](unsigned c0, unsigned c1) -> uintx4 {      // eight codes
+        return uintx4{__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, 1.0f, false)),
+                      __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, 1.0f, true)),
+                      __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, 1.0f, false)),
+                      __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, 1.0f, true))};
+    };
+    const auto write_k = [&](int at, const uintx4& c) {
         const int row = w * RPW + lrow;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            uintx4 v;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                v[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * h + i], 1.0f, false));
-                v[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * h + i], 1.0f, true));
-            }
-            const int ch = 2 * lch + h;
-            *reinterpret_cast<uintx4*>(to + row * ROWB + ((ch ^ (is_k ? kswz(row) : vswz(row))) * 16)) = v;
-        }
+        for (int h = 0; h < 2; ++h)
+            *reinterpret_cast<uintx4*>(smem + (at % NKS) * STB + row * ROWB + (((2 * lch + h) ^ kswz(row)) * 16)) = bf16_of(c[2 * h], c[2 * h + 1]);
     };
-    const auto expand = [&](int s, bool is_k) { write_rows(s, is_k, read_codes(s, is_k)); };
+    const auto expand = [&](int s) { write_k(s, read_codes(s)); };
 
     // ---- LDS fragment reads, as in prefix_wide_impl.h ----
     unsigned kaddr[KS];
@@ -233,18 +239,32 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
         const int fv = vswz(keyq);
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
-            const int chunk = 4 * db + 2 * g1 + ((i16 & 3) >> 1);
-            vaddr[db] = (unsigned)(VRING + keyq * ROWB + ((chunk ^ fv) * 16) + (i16 & 1) * 8);
+            if constexpr (CODES) {      // ds_read_b64_tr_b8, see decode_mfma_core.h: lane s of 16 points at key 8 (j / 4) + 4 hl + j % 4, j = s / 2, columns 16 g1 + 8 (s % 2) .. + 7
+                const int j = i16 >> 1, row = 8 * (j >> 2) + 4 * hl + (j & 3);
+                vaddr[db] = (unsigned)(VRING + row * D + (((2 * db + g1) ^ cswz(row)) * 16) + (i16 & 1) * 8);
+            } else {
+                const int chunk = 4 * db + 2 * g1 + ((i16 & 3) >> 1);
+                vaddr[db] = (unsigned)(VRING + keyq * ROWB + ((chunk ^ fv) * 16) + (i16 & 1) * 8);
+            }
         }
     }
     const auto lds_k = [&](int slot, int f) -> uintx4 {
         return *reinterpret_cast<const uintx4*>(smem + (slot % NKS) * STB + (f / KS) * 32 * ROWB + kaddr[f % KS]);
     };
-    const auto lds_v = [&](int slot, int tt, int db) -> shortx8 {
-        const unsigned char* vp = smem + slot * STB + vaddr[db] + tt * 16 * ROWB;
-        const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)HG_LDS(vp));
-        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)HG_LDS(vp + 8 * ROWB));
-        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    typedef std::conditional_t<CODES, intx2, shortx8> VFragment;
+    const auto lds_v = [&](int slot, int tt, int db) -> VFragment {
+        const unsigned char* vp = smem + slot * VSTB + vaddr[db] + tt * 16 * (D * ES);
+        if constexpr (CODES) {
+            return __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) intx2*)HG_LDS(vp));
+        } else {
+            const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)HG_LDS(vp));
+            const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)HG_LDS(vp + 8 * ROWB));
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    };
+    const auto v_operand = [&](const VFragment& v) -> shortx8 {
+        if constexpr (CODES) return __builtin_bit_cast(shortx8, bf16_of((unsigned)v[0], (unsigned)v[1]));
+        else return v;
     };
 
     // ---- online softmax state ----
@@ -319,7 +339,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
 #pragma unroll
             for (int s = 0; s < kCodeSlots; ++s) {
                 if (s < nst) copy_stage(s, s, true, tail);
-                if (s < nst) copy_stage(s, s, false, tail);
+                if (s < VA && s < nst) copy_stage(s, s, false, tail);
             }
         } else {
             if (0 < nst) { copy_stage(0, 0, true, tail); copy_stage(0, 0, false, tail); }
@@ -338,11 +358,10 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
     // Rows of the last stage from ke on may hold anything, and 0 * NaN would be NaN: whoever has copied them clears them once they have landed
     const int partial = nst > nfull ? nst - 1 : -1;
     const auto clear_rows = [&](int s) {
+        constexpr int RPC = CODES ? RPW : RPI;      // rows of one copy instruction
 #pragma unroll
-        for (int i = 0; i < CPW; ++i) {
-            const int row = w * RPW + i * RPI + l / CPR;
-            if (k0 + s * KT + row >= ke) *reinterpret_cast<uintx4*>(smem + VRING + (s % NS) * STB + row * ROWB + (l % CPR) * 16) = uintx4{0u, 0u, 0u, 0u};
-        }
+        for (int i = 0; i < KOPS; ++i)
+            if (k0 + s * KT + w * RPW + i * RPC + lrow >= ke) *reinterpret_cast<uintx4*>(smem + VRING + (s % NS) * VSTB + (w * RPW + i * RPC) * (D * ES) + l * 16) = uintx4{0u, 0u, 0u, 0u};
     };
     const auto meet = [&]() {      // barrier of the workgroup, which no memory operation is moved over
         asm volatile("" ::: "memory");
@@ -351,13 +370,12 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
     };
     const auto lds_done = [&]() { __builtin_amdgcn_s_waitcnt(0xC07F); };      // lgkmcnt(0)
     if constexpr (CODES) {
-        // K of stages 0 .. 1 and V of stages 0 .. 1 by hand: there are only two K slots, so stage 2 waits for the scores of stage 0 (below)
-        if (0 < nst) { expand(0, true); expand(0, false); }
-        if (1 < nst) { expand(1, true); expand(1, false); }
+        // there are only two K slots: stage 2 waits for the scores of stage 0 (below)
+        if (0 < nst) expand(0);
+        if (1 < nst) expand(1);
         if (partial == 0) clear_rows(0);
-        if (partial == 1) clear_rows(1);
         copy_some([&](auto tail) {
-            if (4 < nst) { copy_stage(4, 4, true, tail); copy_stage(4, 4, false, tail); }
+            if (4 < nst) copy_stage(4, 4, true, tail);
             if (5 < nst) copy_stage(5, 5, true, tail);
         });
     } else {
@@ -375,7 +393,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
     meet();
 
     uintx4 kf[NKF];
-    shortx8 vf[NVF];
+    VFragment vf[NVF];
     STile SA, SB;
     uintx4 PA[KT / 16], PB[KT / 16];
     if (mine > 0) {      // scores of the first two stages, product by product in turn (each waits for its own one before)
@@ -407,7 +425,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
     if constexpr (CODES) {
         // K of stage 2 takes the slot of stage 0 when everyone has its scores
         meet();
-        if (2 < nst) { expand(2, true); }
+        if (2 < nst) expand(2);
     } else {
         meet();
         copy_some([&](auto tail) { if (4 < nst) copy_stage(4, 4, true, tail); });
@@ -450,23 +468,16 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
     };
     // The wait before step j: its K and V have landed while the younger copies may be in flight (those of the step before, careful ones only where there were any)
     const auto wait_plain = [&]() {
-        if constexpr (CODES) wait_vm<2 * (kCodeSlots - 2)>();
-        else wait_vm<2 * CPW>();
+        wait_vm<2 * KOPS>();
     };
     const auto wait_careful = [&](int j) {
-        if constexpr (CODES) {
-            wait_vm<0>();
-        } else {
-            if (j + KA - 1 < nst) wait_vm<2 * CPW>();
-            else if (j + VA - 1 < nst) wait_vm<CPW>();
-            else wait_vm<0>();
-        }
+        if (j + KA - 1 < nst) wait_vm<2 * KOPS>();
+        else if (j + VA - 1 < nst) wait_vm<KOPS>();
+        else wait_vm<0>();
     };
     const auto before_step = [&](int j) {      // the careful form; the partial stage's V rows are first read in the step before its own
         wait_careful(j);
-        if constexpr (!CODES) {
-            if (j + 1 == partial) clear_rows(partial);
-        }
+        if (j + 1 == partial) clear_rows(partial);
         lds_done();
         meet();
     };
@@ -478,9 +489,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
     };
     const auto careful_expand = [&](int j) {
         if constexpr (CODES) {
-            if (j + 3 < nst) expand(j + 3, true);
-            if (j + 2 < nst) expand(j + 2, false);
-            if (j + 2 == partial) clear_rows(partial);
+            if (j + 3 < nst) expand(j + 3);
         }
     };
     const auto step = [&](int j, auto slotc, auto careful) {
@@ -503,11 +512,9 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
         {
             const auto issue_k = [&](int j, int slot) { if constexpr (!kCareful) copy_stage(j + KA, slot + KA, true, std::false_type{}); };
             const auto issue_v = [&](int j, int slot) { if constexpr (!kCareful) copy_stage(j + VA, slot + VA, false, std::false_type{}); };
-            uintx4 ck{}, cv{};
-            const auto read_k = [&](int slot) { if constexpr (!kCareful && CODES) ck = read_codes(slot + 3, true); };
-            const auto read_v = [&](int slot) { if constexpr (!kCareful && CODES) cv = read_codes(slot + 2, false); };
-            const auto work_k = [&](int slot) { if constexpr (!kCareful && CODES) write_rows(slot + 3, true, ck); };
-            const auto work_v = [&](int slot) { if constexpr (!kCareful && CODES) write_rows(slot + 2, false, cv); };
+            uintx4 ck{};
+            const auto read_k = [&](int slot) { if constexpr (!kCareful && CODES) ck = read_codes(slot + 3); };
+            const auto work_k = [&](int slot) { if constexpr (!kCareful && CODES) write_k(slot + 3, ck); };
 #if HG_RW_D == 128
 #include "ragged_wide_step.inc"
 #else
