@@ -56,8 +56,8 @@
  *   - The calls of a context share its workspace.  Two of them that keep partial results in it must not be in flight
  *     at the same time, be they enqueued on two streams, replayed from a graph or on two branches of one: such calls
  *     spoil each other's results (but no later call's).  hg_set_stream does not order anything by itself.  A call whose
- *     result comes out in one piece uses no workspace and may run beside any other: hg_merge, hg_kv_append*, and
- *     hg_hydragen_attn on packed bf16 rows with little work (see HG_OPT_FUSED_KERNEL), which also needs none.
+ *     result comes out in one piece uses no workspace and may run beside any other: hg_merge, hg_kv_append*, hg_page_slots,
+ *     hg_kv_write_paged, and hg_hydragen_attn on packed bf16 rows with little work (see HG_OPT_FUSED_KERNEL), which also needs none.
  *   - Calls in flight, and graphs that hold calls, may outlive their context (not the workspace they were given).
  */
 #ifndef HYDRAGEN_H

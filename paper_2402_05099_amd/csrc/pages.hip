@@ -18,14 +18,14 @@ constexpr int kTokens = 1024;                    // tokens that a workgroup find
 // len + t.  Two prefix sums over the sequences (tokens, new pages) are all that ties the sequences to each other; every workgroup takes them
 // for itself, so that one launch does: 8 bytes per sequence out of L2 instead of a second launch.  A new page begins with a new token, so the
 // page's entry in the table is written where that token's slot is found.
-// What bounds it is latency, a chain of loads and barriers; the largest call here, 512 sequences with 131 thousand tokens, takes as long as a small one and a half.
+// What bounds it is latency: loads, two scans, the search of a token's sequence (ten looks into LDS), its page, 4.1 us for four sequences with 125 tokens, of which
+// the launch is most; 512 sequences with 131 thousand tokens 6.1 us, 0.6 MB in and out.  (256 sequences at a time, the pages of a sequence entered by the one
+// workgroup that has it, 20.5 us.)
 __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a) {
     __shared__ int s_q0[kSeqs], s_len[kSeqs], s_have[kSeqs], s_first[kSeqs], s_sum[2][kThreads / 64];
     const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;
     const int ps_mask = (1 << a.shift) - 1, cap = a.stride << a.shift;
-    // the last workgroup also enters the pages of the tokens that have no place in `slots`
-    const bool last = blockIdx.x == gridDim.x - 1;
-    const int tok0 = (int)blockIdx.x * kTokens, tok1 = last ? 0x7fffffff : tok0 + kTokens;
+    const int tok0 = (int)blockIdx.x * kTokens, tok1 = min(tok0 + kTokens, a.rows);
     int base_q = 0, base_p = 0;
     for (int b0 = 0; b0 < a.B; b0 += kSeqs) {
         const int b = b0 + kPer * tid;
@@ -83,6 +83,17 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a) {
             *a.pages_used = base_p + all_p;
         }
         __syncthreads();
+        if (blockIdx.x == gridDim.x - 1 && base_q + all_q > a.rows) {      // pages that begin with a token that has no place in `slots`
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int at = kPer * tid + i, from = max(a.rows - s_q0[at], 0);      // the first such token of the sequence
+                const int e0 = max((int)(((int64_t)s_len[at] + from + ps_mask) >> a.shift), s_have[at]);
+                for (int e = e0; b + i < a.B && e < s_have[at] + fresh[i]; ++e) {
+                    const int f = s_first[at] + e - s_have[at];
+                    a.table[(int64_t)(b + i) * a.stride + e] = f < a.n_free ? a.free_pages[f] : -1;
+                }
+            }
+        }
         // the tokens of this workgroup that belong to these sequences
         const int t_end = min(tok1, base_q + all_q);
         for (int i = max(tok0, base_q) + tid; i < t_end; i += kThreads) {
@@ -92,7 +103,7 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a) {
                 if (s_q0[lo + d] <= i) lo += d;
             const int64_t j = (int64_t)s_len[lo] + (i - s_q0[lo]);
             int slot = -1;
-            if (j < cap) {
+            if (j >= 0 && j < cap && b0 + lo < a.B) {      // (j < 0, or a sequence behind the last: the counts' sum has left 32 bits)
                 const int e = (int)j >> a.shift;
                 int32_t* const entry = a.table + (int64_t)(b0 + lo) * a.stride + e;
                 int page;
@@ -103,9 +114,9 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a) {
                     page = f < a.n_free ? a.free_pages[f] : -1;
                     if (((int)j & ps_mask) == 0) *entry = page;
                 }
-                if (page >= 0) slot = (page << a.shift) + ((int)j & ps_mask);
+                if (page >= 0 && page <= 0x7fffffff >> a.shift) slot = (page << a.shift) + ((int)j & ps_mask);
             }
-            if (i < a.rows) a.slots[i] = slot;
+            a.slots[i] = slot;
         }
         base_q += all_q;
         base_p += all_p;
@@ -115,7 +126,7 @@ __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a) {
         a.q_off[0] = 0;
         *a.pages_used = 0;
     }
-    for (int i = max(tok0, base_q) + tid; i < min(tok1, a.rows); i += kThreads) a.slots[i] = -1;      // behind the last token
+    for (int i = max(tok0, base_q) + tid; i < tok1; i += kThreads) a.slots[i] = -1;      // behind the last token
 }
 
 hipError_t launch_page_slots(const SlotArgs& a, hipStream_t s) {
@@ -143,7 +154,8 @@ __device__ __forceinline__ uint2 codes8(const uint4& r, float scale) {
 }
 }
 
-// A thread takes a piece of eight elements of K and of V.
+// A thread takes a piece of eight elements of K and of V.  Bound by HBM: 16.8 thousand tokens, 40 heads of 128, as codes 91 us, 5.5 TB/s of 503 MB (a large copy
+// reaches 4.8); a decode step's rows 4.1 us, a launch.
 template <bool CODES>
 __global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a) {
     using Piece = std::conditional_t<CODES, uint2, uint4>;

@@ -57,10 +57,9 @@ inline int64_t rows_grid(const RaggedArgs& a) { return (int64_t)a.B * a.tiles * 
 
 // ---- launchers ----
 hipError_t launch_ragged_rows(const RaggedArgs& a, int D, bool codes, hipStream_t s);       // ragged_rows.hip: what remains, or all there is
-hipError_t launch_ragged_merge(const RaggedArgs& a, int D, hipStream_t s);                  // ... their parts (nsplit > 1)
 hipError_t launch_ragged_wide(const RaggedArgs& a, bool codes, hipStream_t s);           // ragged_wide.hip, D = 128: tiles, and what remains in the same launch
 hipError_t launch_ragged_wide_d64(const RaggedArgs& a, bool codes, hipStream_t s);          // ragged_wide_d64.hip
-hipError_t launch_ragged_join(const RaggedArgs& a, int D, hipStream_t s);                   // the parts of tiles (tile_nsplit > 1)
+hipError_t launch_ragged_join(const RaggedArgs& a, int D, hipStream_t s);                   // ragged_rows.hip: the parts of either (nsplit > 1, tile_nsplit > 1)
 
 // ---- block tables, slots and the write into a paged cache (pages.hip) ----
 struct SlotArgs {
@@ -154,7 +153,7 @@ __device__ __forceinline__ bool tile_of_rank(const RaggedArgs& a, int rank, Ragg
     seq = RaggedSeq{lo + at, __builtin_amdgcn_readlane(own.q0, at), __builtin_amdgcn_readlane(own.n, at), __builtin_amdgcn_readlane(own.take, at),
                     __builtin_amdgcn_readlane(own.len, at)};
     tile = number - first(seq.q0, seq.b);
-    return tile * kTile < rows_in_tiles(seq.take * a.G, a.few_rows);
+    return tile >= 0 && tile * kTile < rows_in_tiles(seq.take * a.G, a.few_rows);      // (tile < 0: offsets out of order)
 }
 #endif
 // Tile numbers of a call.

@@ -33,7 +33,9 @@ int check_ragged(const hg_ctx* c, const void* Q, int64_t q_stride, const int32_t
     if ((int64_t)rows * Hq >= (1LL << 31) || B >= (1 << 24) || ((int64_t)rows * (Hq / Hkv) + 256LL * B) * Hkv >= (1LL << 31)) return HG_ERR_UNSUPPORTED;
     if (rows > 0 && B > 0 && max_new > 0) {
         if (!Q || !q_off || !O) return HG_ERR_INVALID_ARG;
-        if (q_stride < (int64_t)Hq * D || q_stride % 8 != 0 || reinterpret_cast<uintptr_t>(Q) % 16 != 0) return HG_ERR_INVALID_ARG;
+        if (q_stride < (int64_t)Hq * D || q_stride % 8 != 0 ||
+            (reinterpret_cast<uintptr_t>(Q) | reinterpret_cast<uintptr_t>(O)) % 16 != 0)
+            return HG_ERR_INVALID_ARG;
     }
     return HG_OK;
 }
@@ -112,7 +114,8 @@ void plan_tiles(RaggedArgs& a, int D, Room& room) {
     const double part = 8.0 * a.rows * a.Hq * (D + 1) / 4.5e6;
     int best = 1;
     double least = 1e300;
-    for (int s = 1; s <= std::max(1, std::min(64, a.max_len / 1024)); ++s) {
+    const int most = std::max(1, (int)std::min<int64_t>({64, a.max_len / 1024, (1LL << 30) / std::max<int64_t>(1, (int64_t)a.tiles_all * a.Hkv)}));      // (a grid of 32 bits)
+    for (int s = 1; s <= most; ++s) {
         const double n = 0.75 * wgs * s, us = std::max(1.0, ceil(n / 512.0)) * (stages / s * (n <= 256.0 ? 0.6 : 0.95) + 8.0) + (s > 1 ? part * s + 6.0 : 0.0);
         if (us < (best == 1 ? 0.9 : 1.0) * least) { least = us; best = s; }      // (a tenth at least, or there is nothing to join)
         if (wgs >= 512.0) break;
@@ -120,9 +123,10 @@ void plan_tiles(RaggedArgs& a, int D, Room& room) {
     split_keys(best, a.max_len, 1024, 64, (int64_t)a.rows * a.Hq, D, room, a.tile_nsplit, a.tile_chunk, a.tile_part_O, a.tile_part_L);
 }
 
-int run_tiles(const hg_ctx* c, const RaggedArgs& a, int D, bool codes) {
-    const int rc = rc_of(D == 128 ? launch_ragged_wide(a, codes, c->stream) : launch_ragged_wide_d64(a, codes, c->stream));
-    if (rc || a.tile_nsplit == 1) return rc;
+// tiles: the call has any; what remains behind them, or is all there is, goes along
+int run(const hg_ctx* c, const RaggedArgs& a, int D, bool codes, bool tiles) {
+    const int rc = rc_of(!tiles ? launch_ragged_rows(a, D, codes, c->stream) : D == 128 ? launch_ragged_wide(a, codes, c->stream) : launch_ragged_wide_d64(a, codes, c->stream));
+    if (rc || (a.nsplit == 1 && a.tile_nsplit == 1)) return rc;
     return rc_of(launch_ragged_join(a, D, c->stream));
 }
 
@@ -130,23 +134,23 @@ int run_tiles(const hg_ctx* c, const RaggedArgs& a, int D, bool codes) {
 
 extern "C" {
 
-int hg_prompt_attn(hg_ctx* c, const void* Q, const void* K, const void* V, int64_t q_stride, int64_t kv_stride, const int32_t* seq_off, int rows,
+int hg_prompt_attn(hg_ctx* c, const void* Q, const void* K, const void* V, int64_t q_stride, int64_t kv_stride, const int32_t* q_off, int rows,
                    int max_len, int B, int Hq, int Hkv, int D, float scale, void* O, int o_dtype, float* LSE) {
-    const int rc = check_ragged(c, Q, q_stride, seq_off, rows, max_len, B, Hq, Hkv, D, O, o_dtype);
+    const int rc = check_ragged(c, Q, q_stride, q_off, rows, max_len, B, Hq, Hkv, D, O, o_dtype);
     if (rc) return rc;
     if (rows == 0 || B == 0 || max_len == 0) return HG_OK;
     if (!K || !V || kv_stride < (int64_t)Hkv * D || kv_stride % 8 != 0 ||
         (reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V)) % 16 != 0) return HG_ERR_INVALID_ARG;
     if (kv_stride >= (1LL << 26)) return HG_ERR_UNSUPPORTED;      // (a copy's rows lie within 32 bits of each other)
     if (hipSetDevice(c->device) != hipSuccess) return HG_ERR_HIP;
-    RaggedArgs a = ragged_args(Q, q_stride, seq_off, rows, max_len, B, Hq, Hkv, D, scale, O, o_dtype, LSE);
+    RaggedArgs a = ragged_args(Q, q_stride, q_off, rows, max_len, B, Hq, Hkv, D, scale, O, o_dtype, LSE);
     a.K = static_cast<const unsigned char*>(K);
     a.V = static_cast<const unsigned char*>(V);
     a.kv_stride = 2 * kv_stride;
     a.max_len = max_len;
     Room room = room_of(c);
     plan_tiles(a, D, room);
-    return run_tiles(c, a, D, false);
+    return run(c, a, D, false, true);
 }
 
 int hg_chunk_attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_t* q_off, int rows, const hg_paged_kv* kv, const int32_t* lengths,
@@ -182,22 +186,16 @@ int hg_chunk_attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_
     }
     Room room = room_of(c);
     plan_few_rows(a, D, room);
-    int done;
-    if ((int64_t)std::min(max_new, rows) * a.G > kFewRows) {
-        plan_tiles(a, D, room);
-        done = run_tiles(c, a, D, codes);
-    } else {
-        done = rc_of(launch_ragged_rows(a, D, codes, c->stream));
-    }
-    if (done == HG_OK && a.nsplit > 1) done = rc_of(launch_ragged_merge(a, D, c->stream));
-    return done;
+    const bool tiles = (int64_t)std::min(max_new, rows) * a.G > kFewRows;
+    if (tiles) plan_tiles(a, D, room);
+    return run(c, a, D, codes, tiles);
 }
 
 int hg_page_slots(hg_ctx* c, const int32_t* lengths, const int32_t* counts, const int32_t* free_pages, int n_free, int page_size, int B, int rows,
                   int32_t* page_table, int table_stride, int32_t* q_off, int32_t* slots, int32_t* new_lengths, int32_t* pages_used) {
     const int shift = page_shift(page_size);
     if (!c || shift < 0 || n_free < 0 || B < 0 || rows < 0 || table_stride < 0 || !q_off || !pages_used) return HG_ERR_INVALID_ARG;
-    if ((int64_t)table_stride * page_size >= (1LL << 31)) return HG_ERR_UNSUPPORTED;
+    if ((int64_t)table_stride * page_size >= (1LL << 31) || (int64_t)B * table_stride >= (1LL << 31)) return HG_ERR_UNSUPPORTED;
     if (B > 0 && (!lengths || !counts || !new_lengths || (table_stride > 0 && !page_table))) return HG_ERR_INVALID_ARG;
     if ((rows > 0 && !slots) || (n_free > 0 && !free_pages)) return HG_ERR_INVALID_ARG;
     // every workgroup reads the lengths and the counts: none may write over them

@@ -54,29 +54,60 @@ __device__ __forceinline__ void store_joined(const OutDev& out, int64_t row, int
     store_row8<D>(out, row, c8, o, den > 0.f ? m + __logf(den) : -INFINITY);
 }
 
-// The rows of ragged_rows_impl.h, PG groups of D / 8 lanes to a row, each with every PG-th of its parts (a row of many parts would be a chain of loads
-// otherwise); a workgroup takes 2048 / D / PG of the places for few_most rows of every sequence and KV head.  Part p holds the keys from p * chunk on, so those
-// of a row are its first ceil(seen / chunk).
+// Joins the parts of both kinds of rows, PG groups of D / 8 lanes to a row, each with every PG-th of its parts (a row of many parts would be a chain of loads
+// otherwise), so a workgroup takes 2048 / D / PG rows.  Part p holds the keys from p * chunk on: those of a row are its first ceil(seen / chunk).
+// The first a.rows * per_token workgroups (tile_nsplit > 1) take the rows of tiles, per_token of them one token's heads; the others (nsplit > 1) the places for
+// few_most rows of every sequence and KV head.
 template <int D, int PG>
-__global__ __launch_bounds__(256) void ragged_merge_kernel(RaggedArgs a) {
+__global__ __launch_bounds__(256) void ragged_join_kernel(RaggedArgs a, int per_token) {
     constexpr int LPR = D / 8, RPW = 256 / LPR / PG;
     __shared__ float s_o[PG > 1 ? 256 : 1][8], s_m[256 / LPR], s_l[256 / LPR];
     const int group = threadIdx.x / LPR, c8 = threadIdx.x % LPR, pg = group / RPW;
-    const int64_t at = (int64_t)blockIdx.x * RPW + group % RPW;
+    const unsigned of_tiles = (unsigned)a.rows * (unsigned)per_token;
+    const float *O, *L;
+    int64_t stride, at, row = 0;
     int parts = 0;
-    int64_t row = 0;
     bool mine = false;
-    if (at < a.part_rows) {
-        const int bh = (int)a.by_most.of((unsigned)at), b = (int)a.by_heads.of((unsigned)bh), kvh = bh - b * a.Hkv;
-        const RaggedSeq sq = ragged_seq(a, b);
-        const int r = rows_in_tiles(sq.take * a.G, a.few_rows) + ((int)at - bh * a.few_most), tok = (int)a.by_group.of((unsigned)r);
-        mine = r < sq.take * a.G;
+    if (blockIdx.x < of_tiles) {
+        const int token = (int)(blockIdx.x / (unsigned)per_token), h = (int)(blockIdx.x - (unsigned)token * (unsigned)per_token) * RPW + group % RPW;
+        // the sequence that owns the token: the last that begins at or before it
+        int lo = 0, n = a.B;
+        const int lane = threadIdx.x & 63;
+        while (true) {
+            const int step = (n + 63) / 64, i = lo + lane * step;
+            const int c = __builtin_popcountll(__ballot(lane * step < n && a.q_off[i] <= token));
+            if (c == 0) return;
+            lo += (c - 1) * step;
+            n = min(step, n - (c - 1) * step);
+            if (n == 1) break;
+        }
+        const RaggedSeq sq = ragged_seq(a, __builtin_amdgcn_readfirstlane(lo));
+        const int tok = token - sq.q0, g = h - (int)a.by_group.of((unsigned)h) * a.G;
+        if (tok < 0 || tok >= sq.take) return;
+        mine = h < a.Hq && tok * a.G + g < rows_in_tiles(sq.take * a.G, a.few_rows);
         const int seen = mine ? sq.seen(tok) : 0;
-        parts = seen > 0 ? min((seen + a.chunk - 1) / a.chunk, a.nsplit) : 0;
-        row = (int64_t)(sq.q0 + tok) * a.Hq + kvh * a.G + (r - tok * a.G);
+        parts = seen > 0 ? min((seen + a.tile_chunk - 1) / a.tile_chunk, a.tile_nsplit) : 0;
+        O = a.tile_part_O;
+        L = a.tile_part_L;
+        stride = (int64_t)a.rows * a.Hq;
+        row = at = (int64_t)token * a.Hq + h;
+    } else {
+        at = (int64_t)(blockIdx.x - of_tiles) * RPW + group % RPW;
+        if (at < a.part_rows) {
+            const int bh = (int)a.by_most.of((unsigned)at), b = (int)a.by_heads.of((unsigned)bh), kvh = bh - b * a.Hkv;
+            const RaggedSeq sq = ragged_seq(a, b);
+            const int r = rows_in_tiles(sq.take * a.G, a.few_rows) + ((int)at - bh * a.few_most), tok = (int)a.by_group.of((unsigned)r);
+            mine = r < sq.take * a.G;
+            const int seen = mine ? sq.seen(tok) : 0;
+            parts = seen > 0 ? min((seen + a.chunk - 1) / a.chunk, a.nsplit) : 0;
+            row = (int64_t)(sq.q0 + tok) * a.Hq + kvh * a.G + (r - tok * a.G);
+        }
+        O = a.part_O;
+        L = a.part_L;
+        stride = a.part_rows;
     }
     float m = -INFINITY, den = 0.f, o[8] = {};
-    join_parts<D>(a.part_O, a.part_L, a.part_rows, at, pg, PG, parts, c8, m, den, o);
+    join_parts<D>(O, L, stride, at, pg, PG, parts, c8, m, den, o);
     if constexpr (PG > 1) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) s_o[threadIdx.x][i] = o[i];
@@ -96,33 +127,6 @@ __global__ __launch_bounds__(256) void ragged_merge_kernel(RaggedArgs a) {
         }
     }
     if (mine) store_joined<D>(a.out, row, c8, m, den, o);
-}
-
-// The rows of tiles: a workgroup takes one token's rows from blockIdx.y * 2048 / D on.
-template <int D>
-__global__ __launch_bounds__(256) void ragged_join_kernel(RaggedArgs a) {
-    constexpr int LPR = D / 8;
-    const int token = blockIdx.x;
-    // the sequence that owns the token: the last that begins at or before it 
-    int lo = 0, n = a.B;
-    const int lane = threadIdx.x & 63;
-    while (true) {
-        const int step = (n + 63) / 64, i = lo + lane * step;
-        const int c = __builtin_popcountll(__ballot(lane * step < n && a.q_off[i] <= token));
-        if (c == 0) return;
-        lo += (c - 1) * step;
-        n = min(step, n - (c - 1) * step);
-        if (n == 1) break;
-    }
-    const RaggedSeq sq = ragged_seq(a, __builtin_amdgcn_readfirstlane(lo));
-    const int tok = token - sq.q0, h = (int)blockIdx.y * (256 / LPR) + (int)threadIdx.x / LPR;
-    if (tok < 0 || tok >= sq.take || h >= a.Hq) return;
-    if (tok * a.G + (h - (h / a.G) * a.G) >= rows_in_tiles(sq.take * a.G, a.few_rows)) return;
-    const int seen = sq.seen(tok);
-    float m = -INFINITY, den = 0.f, o[8] = {};
-    join_parts<D>(a.tile_part_O, a.tile_part_L, (int64_t)a.rows * a.Hq, (int64_t)token * a.Hq + h, 0, 1,
-                  seen > 0 ? min((seen + a.tile_chunk - 1) / a.tile_chunk, a.tile_nsplit) : 0, threadIdx.x % LPR, m, den, o);
-    store_joined<D>(a.out, (int64_t)token * a.Hq + h, threadIdx.x % LPR, m, den, o);
 }
 
 template <int D, bool CODES, bool BOTH, int NW>
@@ -154,21 +158,20 @@ hipError_t launch_ragged_rows(const RaggedArgs& a, int D, bool codes, hipStream_
     return codes ? launch_rows_d<64, true>(a, (unsigned)grid, s) : launch_rows_d<64, false>(a, (unsigned)grid, s);
 }
 
-template <int D>
-static hipError_t launch_merge_d(const RaggedArgs& a, hipStream_t s) {
-    if (a.nsplit > 8) ragged_merge_kernel<D, 8><<<(unsigned)((a.part_rows + 256 / D - 1) / (256 / D)), 256, 0, s>>>(a);
-    else ragged_merge_kernel<D, 1><<<(unsigned)((a.part_rows + 2048 / D - 1) / (2048 / D)), 256, 0, s>>>(a);
+template <int D, int PG>
+static hipError_t launch_join_t(const RaggedArgs& a, hipStream_t s) {
+    constexpr int rows = 2048 / D / PG;
+    const int per_token = a.tile_nsplit > 1 ? (a.Hq + rows - 1) / rows : 0;
+    const int64_t grid = (int64_t)a.rows * per_token + (a.nsplit > 1 ? (a.part_rows + rows - 1) / rows : 0);
+    if (grid >= (1LL << 31)) return hipErrorInvalidValue;
+    ragged_join_kernel<D, PG><<<(unsigned)grid, 256, 0, s>>>(a, per_token);
     return hipGetLastError();
 }
 
-hipError_t launch_ragged_merge(const RaggedArgs& a, int D, hipStream_t s) { return D == 128 ? launch_merge_d<128>(a, s) : launch_merge_d<64>(a, s); }
-
 hipError_t launch_ragged_join(const RaggedArgs& a, int D, hipStream_t s) {
-    const dim3 grid((unsigned)a.rows, (unsigned)((a.Hq * D / 8 + 255) / 256));
-    if (grid.y > 65535) return hipErrorInvalidValue;
-    if (D == 128) ragged_join_kernel<128><<<grid, 256, 0, s>>>(a);
-    else ragged_join_kernel<64><<<grid, 256, 0, s>>>(a);
-    return hipGetLastError();
+    const bool many = a.nsplit > 8 || a.tile_nsplit > 8;
+    if (D == 128) return many ? launch_join_t<128, 8>(a, s) : launch_join_t<128, 1>(a, s);
+    return many ? launch_join_t<64, 8>(a, s) : launch_join_t<64, 1>(a, s);
 }
 
 }  // namespace hg

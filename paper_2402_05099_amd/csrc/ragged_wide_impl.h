@@ -614,16 +614,21 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
 
 using namespace rw;
 
-// Packed rows: tiles are all there is.  Paged rows: what remains behind the tiles is in the same launch, the tiles first: they are bound by the matrix pipes, the
-// others by the reads of their cache, and two workgroups of either kind share a CU.
+// Packed rows: tiles are all there is.  Paged rows: what remains behind the tiles is in the same launch: they are bound by the matrix pipes, the
+// others by the reads of their cache, and two workgroups of either kind share a CU.  While there are both, 256 workgroups of one kind, one for every CU, come
+// after 256 of the other.
 template <int MODE>
 __global__ __launch_bounds__(64 * NW, 2) void HG_RW_KERNEL(RaggedArgs a) {
     if constexpr (MODE == kDense) {
         tile_workgroup<MODE>(a, blockIdx.x);
     } else {
-        const unsigned n = (unsigned)a.tiles_all * (unsigned)a.Hkv * (unsigned)a.tile_nsplit;
-        if (blockIdx.x < n) tile_workgroup<MODE>(a, blockIdx.x);
-        else rr::rows_workgroup<D, MODE == kCodes, true, NW>(a, blockIdx.x - n);
+        const unsigned tiles = (unsigned)a.tiles_all * (unsigned)a.Hkv * (unsigned)a.tile_nsplit, rows = (unsigned)a.B * (unsigned)a.tiles * (unsigned)a.nsplit * (unsigned)a.Hkv;
+        const unsigned both = min((tiles + 255u) / 256u, (rows + 255u) / 256u), block = blockIdx.x >> 8, in = blockIdx.x & 255u;
+        const bool is_tile = block < 2u * both ? (block & 1u) == 0u : tiles > rows;
+        const unsigned id = (block < 2u * both ? block >> 1 : block - both) * 256u + in;
+        if (id >= (is_tile ? tiles : rows)) return;
+        if (is_tile) tile_workgroup<MODE>(a, id);
+        else rr::rows_workgroup<D, MODE == kCodes, true, NW>(a, id);
     }
 }
 
@@ -631,7 +636,7 @@ template <int MODE>
 static hipError_t launch_mode(const RaggedArgs& a, hipStream_t s) {
     constexpr int bytes = MODE == kDense ? lds_bytes(MODE) : std::max(lds_bytes(MODE), rr::rows_lds<D, MODE == kCodes, true>(NW));
     static_assert(bytes <= 81920, "two workgroups to a CU");
-    const int64_t grid = (int64_t)a.tiles_all * a.Hkv * a.tile_nsplit + (MODE == kDense ? 0 : rows_grid(a));
+    const int64_t tiles = (int64_t)a.tiles_all * a.Hkv * a.tile_nsplit, grid = MODE == kDense ? tiles : ((tiles + 255) / 256 + (rows_grid(a) + 255) / 256) * 256;
     if (grid >= (1LL << 31)) return hipErrorInvalidValue;
     static bool attr_set[64] = {};
     int dev = 0;
