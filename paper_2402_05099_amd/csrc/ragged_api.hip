@@ -116,7 +116,7 @@ void plan_tiles(RaggedArgs& a, int D, Room& room) {
     double least = 1e300;
     const int most = std::max(1, (int)std::min<int64_t>({64, a.max_len / 1024, (1LL << 30) / std::max<int64_t>(1, (int64_t)a.tiles_all * a.Hkv)}));      // (a grid of 32 bits)
     for (int s = 1; s <= most; ++s) {
-        const double n = 0.75 * wgs * s, us = std::max(1.0, ceil(n / 512.0)) * (stages / s * (n <= 256.0 ? 0.6 : 0.95) + 8.0) + (s > 1 ? part * s + 6.0 : 0.0);
+        const double n = 0.75 * wgs * s, us = std::max(1.0, ceil(n / 512.0)) * (stages / s * (n <= 256.0 ? 0.6 : 0.95) + 8.0) + (s > 1 ? part * s + (a.nsplit > 1 ? 1.0 : 6.0) : 0.0);
         if (us < (best == 1 ? 0.9 : 1.0) * least) { least = us; best = s; }      // (a tenth at least, or there is nothing to join)
         if (wgs >= 512.0) break;
     }

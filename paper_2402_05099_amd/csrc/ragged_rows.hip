@@ -55,7 +55,8 @@ __device__ __forceinline__ void store_joined(const OutDev& out, int64_t row, int
 }
 
 // Joins the parts of both kinds of rows, PG groups of D / 8 lanes to a row, each with every PG-th of its parts (a row of many parts would be a chain of loads
-// otherwise), so a workgroup takes 2048 / D / PG rows.  Part p holds the keys from p * chunk on: those of a row are its first ceil(seen / chunk).
+// otherwise), so a workgroup takes 2048 / D / PG rows.  Part p holds the keys from p * chunk on: those of a row are its first ceil(seen / chunk).  Where
+// a tile, or what remains of a sequence, has one range, its rows are there already.
 // The first a.rows * per_token workgroups (tile_nsplit > 1) take the rows of tiles, per_token of them one token's heads; the others (nsplit > 1) the places for
 // few_most rows of every sequence and KV head.
 template <int D, int PG>
@@ -84,7 +85,8 @@ __global__ __launch_bounds__(256) void ragged_join_kernel(RaggedArgs a, int per_
         const RaggedSeq sq = ragged_seq(a, __builtin_amdgcn_readfirstlane(lo));
         const int tok = token - sq.q0, g = h - (int)a.by_group.of((unsigned)h) * a.G;
         if (tok < 0 || tok >= sq.take) return;
-        mine = h < a.Hq && tok * a.G + g < rows_in_tiles(sq.take * a.G, a.few_rows);
+        const int in_tiles = rows_in_tiles(sq.take * a.G, a.few_rows), r = tok * a.G + g;
+        mine = h < a.Hq && r < in_tiles && sq.seen((int)a.by_group.of((unsigned)(min(r / kTile * kTile + kTile, in_tiles) - 1))) > a.tile_chunk;
         const int seen = mine ? sq.seen(tok) : 0;
         parts = seen > 0 ? min((seen + a.tile_chunk - 1) / a.tile_chunk, a.tile_nsplit) : 0;
         O = a.tile_part_O;
@@ -97,7 +99,7 @@ __global__ __launch_bounds__(256) void ragged_join_kernel(RaggedArgs a, int per_
             const int bh = (int)a.by_most.of((unsigned)at), b = (int)a.by_heads.of((unsigned)bh), kvh = bh - b * a.Hkv;
             const RaggedSeq sq = ragged_seq(a, b);
             const int r = rows_in_tiles(sq.take * a.G, a.few_rows) + ((int)at - bh * a.few_most), tok = (int)a.by_group.of((unsigned)r);
-            mine = r < sq.take * a.G;
+            mine = r < sq.take * a.G && sq.seen(sq.take - 1) > a.chunk;
             const int seen = mine ? sq.seen(tok) : 0;
             parts = seen > 0 ? min((seen + a.chunk - 1) / a.chunk, a.nsplit) : 0;
             row = (int64_t)(sq.q0 + tok) * a.Hq + kvh * a.G + (r - tok * a.G);

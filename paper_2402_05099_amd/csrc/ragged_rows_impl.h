@@ -63,6 +63,7 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
     const int k0 = sp * a.chunk, ke = min(seen_by(t_last), k0 + a.chunk);      // keys [k0, ke)
     if (sp > 0 && k0 >= ke) return;      // (the join looks at no part that starts behind a row's keys)
     const int all_see = seen_by(t_first);       // every row of the tile sees the keys below
+    const bool in_parts = seen_by((int)a.by_group.of((unsigned)(nrows - 1))) > a.chunk;      // the sequence has several ranges
     const int nst = ke > k0 ? (ke - k0 + KT - 1) / KT : 0;
 
     // ---- this lane's query row ----
@@ -217,9 +218,9 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
         for (int i = 0; i < 8; ++i) o[i] *= inv;
         const int tk = (int)a.by_group.of((unsigned)rr), gg = rr - tk * a.G;
         // one range: the result itself; several: part `sp`
-        const int64_t at = a.nsplit == 1 ? (int64_t)(q0 + tk) * a.Hq + kvh * a.G + gg : ((int64_t)b * a.Hkv + kvh) * a.few_most + (rr - row0);
+        const int64_t at = !in_parts ? (int64_t)(q0 + tk) * a.Hq + kvh * a.G + gg : ((int64_t)b * a.Hkv + kvh) * a.few_most + (rr - row0);
         const float lse = den > 0.f ? m * a.scale + __logf(den) : -INFINITY;
-        if (a.nsplit > 1) {
+        if (in_parts) {
             float* const O = a.part_O + ((int64_t)sp * a.part_rows + at) * D + 8 * c8;
             *reinterpret_cast<float4*>(O) = make_float4(o[0], o[1], o[2], o[3]);
             *reinterpret_cast<float4*>(O + 4) = make_float4(o[4], o[5], o[6], o[7]);

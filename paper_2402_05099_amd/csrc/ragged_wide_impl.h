@@ -141,7 +141,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const auto token_of = [&](int r) { return (int)a.by_group.of((unsigned)r); };
     const int k0 = sp * a.tile_chunk;
-    const int ke = __builtin_amdgcn_readfirstlane(min(before + token_of(min(row0 + kTileRows, nrows) - 1), k0 + a.tile_chunk));      // keys [k0, ke)
+    const int k_all = __builtin_amdgcn_readfirstlane(before + token_of(min(row0 + kTileRows, nrows) - 1)), ke = min(k_all, k0 + a.tile_chunk);      // keys [k0, ke) of k_all
     const int nst = ke > k0 ? (ke - k0 + KT - 1) / KT : 0, nfull = ke > k0 ? (ke - k0) / KT : 0;
     if (sp > 0 && nst == 0) return;      // (the join looks at no part that starts behind a row's keys)
     // this wavefront's rows, and this lane's
@@ -564,7 +564,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
     if (!any) return;
     const float ltot = half_sum(lsum), lr = half_sum(lround);
     const float inv = lr > 0.f ? a.v_scale / lr : 0.f;
-    const bool in_parts = a.tile_nsplit > 1;
+    const bool in_parts = k_all > a.tile_chunk;      // (a tile of one range has the result itself)
     const int64_t row_at = (int64_t)(q0 + tok) * a.Hq + head;
     if (rv && hl == 0) {
         const float lse = ltot > 0.f ? (mc + __log2f(ltot)) * kLn2 : -INFINITY;
