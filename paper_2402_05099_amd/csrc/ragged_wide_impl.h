@@ -66,8 +66,8 @@ typedef int intx2 __attribute__((ext_vector_type(2)));
 // XOR swizzles of the 16-byte chunks of LDS row `row`, as in prefix_wide_impl.h
 __device__ __forceinline__ int kswz(int row) { return D == 128 ? row % 16 : (row >> 1) & 7; }
 __device__ __forceinline__ int vswz(int row) { return D == 128 ? 4 * (row % 4) : 4 * ((row >> 1) & 1); }
-// ... and of those of a row of V codes (as decode_mfma_core.h has it for 128-byte rows; 64-byte rows: the eight rows of a transposing read are 0 .. 3 and 8 .. 11)
-__device__ __forceinline__ int cswz(int row) { return D == 128 ? ((row >> 1) & 1) | (((row >> 3) & 1) << 1) : 2 * ((row >> 3) & 1); }
+// ... and of those of a row of V codes: 32 lanes of a transposing read take 32 bytes of each of the rows 0 .. 3 and 8 .. 11 (or of those four further), 128 or 64 bytes apart
+__device__ __forceinline__ int cswz(int row) { return 2 * (D == 128 ? ((row >> 1) & 1) | (((row >> 3) & 1) << 1) : (row >> 3) & 1); }
 
 #if HG_RW_D == 128
 typedef floatx16 STile;
