@@ -48,7 +48,8 @@ struct RaggedArgs {
     float* tile_part_L;
 };
 constexpr int kTile = 128;        // rows of a tile
-constexpr int kFewRows = 64;      // a remainder of more rows is a tile
+constexpr int kFewRows = 32;      // a remainder of more rows is a tile: beside tiles, and wherever a read of the cache for every 32 rows is what costs
+constexpr int kFewRowsAlone = 64; // ... in small calls of no more rows than these, where a launch without tiles is over sooner (plan_few_rows)
 // Of a sequence's n G rows, those that tiles take.
 __host__ __device__ inline int rows_in_tiles(int nrows, int few_rows) { return nrows % kTile <= few_rows ? nrows - nrows % kTile : nrows; }
 

@@ -88,10 +88,18 @@ void split_keys(int64_t want, int max_len, int least, int step, int64_t rows, in
     L = room.take((size_t)nsplit * rows);
 }
 
-// What remains behind the tiles, at most kFewRows rows of a sequence to a KV head: how the keys are split.
-void plan_few_rows(RaggedArgs& a, int D, Room& room) {
-    a.few_rows = kFewRows;
-    a.few_most = (int)std::min<int64_t>((int64_t)a.max_new * a.G, kFewRows);
+// What remains behind the tiles, or all there is: how many rows that may be, and how the keys are split.
+//
+// 33 .. 64 rows are two tiles of the few rows, which each read the cache, or one of 128, which reads it once and multiplies for nothing what is not there.  The latter is
+// slower to start and end, and has at most a range for every 1024 keys.  us by the first / by the second, 64 rows at most of B sequences, bf16, 32/8 heads, D = 128: B = 4, up to 1200 keys
+// 12.5 / 23.5, up to 2400 20.9 / 28.1, up to 8000 35.1 / 29.7; B = 16, up to 600 11.6 / 16.8, 1200 19.1 / 24.3, 2400 40.8 / 35.8, 8000 113 / 73; B = 32 (two workgroups to a
+// CU by the first), up to 300 17.0 / 13.9, 8000 209 / 134; codes, B = 16, up to 2400 31.5 / 40.1, 8000 77.8 / 57.0; D = 64, B = 16, up to 2400 25.2 / 27.8, 8000 59.9 / 41.5.  Behind tiles (that
+// is, in calls of more rows) the second is as good or better: 64 x 32/8, 8 chunks up to 256 tokens among single ones, up to 4096 keys 130 / 125, chunks of 1 .. 64 tokens 198 / 179.
+void plan_few_rows(RaggedArgs& a, int D, bool codes, Room& room) {
+    const double cache = (double)a.B * a.Hkv * a.max_len * D * (codes ? 2 : 4);      // bytes, at most
+    const bool alone = (int64_t)a.max_new * a.G <= kFewRowsAlone && (int64_t)a.B * a.Hkv <= 128 && cache <= 1e8;
+    a.few_rows = alone ? kFewRowsAlone : kFewRows;
+    a.few_most = (int)std::min<int64_t>((int64_t)a.max_new * a.G, a.few_rows);
     a.both_tiles = a.few_most > 16;
     a.tiles = (a.few_most + 31) / 32;
     // Four times the workgroups that fit the chip, so that contexts of different lengths even out, of at least 256 keys each.  Up to 1280 keys the join costs more than
@@ -185,8 +193,8 @@ int hg_chunk_attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_
         a.v_scale = kv->v_scale;
     }
     Room room = room_of(c);
-    plan_few_rows(a, D, room);
-    const bool tiles = (int64_t)std::min(max_new, rows) * a.G > kFewRows;
+    plan_few_rows(a, D, codes, room);
+    const bool tiles = (int64_t)std::min(max_new, rows) * a.G > a.few_rows;
     if (tiles) plan_tiles(a, D, room);
     return run(c, a, D, codes, tiles);
 }

@@ -1,4 +1,4 @@
-// Attention over a paged cache of what remains of a sequence's query rows behind its tiles, at most kFewRows to a KV head: all rows of decode steps and drafted
+// Attention over a paged cache of what remains of a sequence's query rows behind its tiles, at most 32 (64 in small calls) to a KV head: all rows of decode steps and drafted
 // tokens, the last ones of a chunk.
 // What bounds it is the cache that is read, once for every KV head whatever the rows, so the rows of a head's group and of all
 // new tokens form one tile of 16 or 32 rows (v_mfma_f32_16x16x32_bf16, v_mfma_f32_32x32x16_bf16; decode_mfma_core.h has the products and the softmax).

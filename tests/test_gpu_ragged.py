@@ -590,3 +590,13 @@ def test_the_same_call_gives_the_same_bits():
         got.append((O.clone(), L.clone()))
     assert all(torch.equal(a, b) for g_ in got[1:] for a, b in zip(g_, got[0]))
     ctx.close()
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B", [30, 40])      # 120 columns of 64 rows at most are a small call, 160 are not
+def test_calls_of_up_to_sixty_four_rows(B, D, codes):
+    pairs = [(3 + 29 * i % 500, (9, 16, 1, 12, 0, 8)[i % 6]) for i in range(B)]
+    run_chunk(pairs, (16, 4), D, codes=codes, mib=16)
+    run_chunk(pairs, (16, 4), D, codes=codes, fp32=True, lead=1)
+    run_chunk([(3000, 16), (1, 16)] + pairs, (16, 4), D, codes=codes, mib=64, ps=64)
