@@ -35,6 +35,9 @@ struct RaggedArgs {
     int both_tiles;           // 0: few_most <= 16
     int wavefronts;           // of a workgroup: 4 or 8
     Divider by_seqs;          // division by B
+    int paired;               // neighbouring KV heads share lines of the cache: their workgroups have ids that differ by 8
+    Divider by_pairs;         // division by Hkv / 2 where they do
+    unsigned row_wgs;         // workgroups
     float* part_O;            // nsplit > 1: partial results [nsplit][part_rows][D], [nsplit][part_rows], part_rows = B * Hkv * few_most
     float* part_L;
     int64_t part_rows;
@@ -53,8 +56,11 @@ constexpr int kFewRowsAlone = 64; // ... in small calls of no more rows than the
 // Of a sequence's n G rows, those that tiles take.
 __host__ __device__ inline int rows_in_tiles(int nrows, int few_rows) { return nrows % kTile <= few_rows ? nrows - nrows % kTile : nrows; }
 
-// Workgroups that take what remains
-inline int64_t rows_grid(const RaggedArgs& a) { return (int64_t)a.B * a.tiles * a.nsplit * a.Hkv; }
+// Workgroups that take what remains (whole groups of sixteen where they come in pairs)
+inline int64_t rows_grid(const RaggedArgs& a) {
+    const int64_t n = (int64_t)a.B * a.tiles * a.nsplit * a.Hkv;
+    return a.paired ? (n + 15) / 16 * 16 : n;
+}
 
 // ---- launchers ----
 hipError_t launch_ragged_rows(const RaggedArgs& a, int D, bool codes, hipStream_t s);       // ragged_rows.hip: what remains, or all there is

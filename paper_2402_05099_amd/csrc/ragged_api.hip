@@ -111,6 +111,9 @@ void plan_few_rows(RaggedArgs& a, int D, bool codes, Room& room) {
     split_keys(a.max_len <= 1280 ? 1 : (2048 + wgs - 1) / wgs, a.max_len, 256, 128, a.part_rows, D, room, a.nsplit, a.chunk, a.part_O, a.part_L);
     a.wavefronts = wgs * a.nsplit <= 256 ? 8 : 4;
     a.by_seqs = divider((unsigned)a.B);
+    a.paired = codes && D == 64 && a.Hkv % 2 == 0;
+    a.by_pairs = divider((unsigned)std::max(a.Hkv / 2, 1));
+    a.row_wgs = (unsigned)std::min<int64_t>(rows_grid(a), 0xffffffffLL);      // (the launch refuses what does not fit a grid)
     a.by_most = divider((unsigned)a.few_most);
 }
 

@@ -132,7 +132,10 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
             for (int k = 0; k < CPS / 2; ++k) {
                 const unsigned char* const base = first + (int64_t)(k * RPI) * a.kv_stride;
                 const int c = h * (CPS / 2) + k;
-                asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(voff[c]), "s"(scalar(base)), "s"(to + (unsigned)c * 1024u) : "memory", "m0");
+                const unsigned at = to + (unsigned)c * 1024u;
+                // a line is used once, unless it has rows of two heads (32 x 64/8 heads, 8192 keys, bf16 179 us so, 199 without the hint; codes at D = 64 75 and 69)
+                if constexpr (CODES && D == 64) asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff[c]), "s"(scalar(base)), "s"(at) : "memory", "m0");
+                else asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(voff[c]), "s"(scalar(base)), "s"(at) : "memory", "m0");
             }
         }
     };
@@ -234,10 +237,21 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
 // Workgroup `id` of the launch: (range, tile, sequence, KV head), heads fastest, ranges slowest.  Later ranges and tiles are empty for most sequences; were they
 // to alternate with the first ones, workgroups, which go to the shader engines of an XCD in turn, would leave some of those with little to do (64 x 32/8 heads, up
 // to 4096 rows, two and four ranges 122 and 123 us so, 114 with one).  At most 16 rows make a tile of 16, more of them tiles of 32 (`BOTH`: there may be more).
+// Codes of a row at D = 64 are half a line, and heads that follow each other on different XCDs fetched every line twice: 32 x 64/8 heads, 8192 keys 94 us, 40/40 heads, 2048 keys
+// 114; in pairs (Hkv even) 69 and 84.
 template <int D, bool CODES, bool BOTH, int NW>
 __device__ __forceinline__ void rows_workgroup(const RaggedArgs& a, unsigned id) {
     typedef const __attribute__((address_space(4))) int32_t* const_i32;
-    const int rest = (int)a.by_heads.of(id), kvh = (int)id - rest * a.Hkv;
+    int rest, kvh;
+    if (CODES && D == 64 && a.paired) {      // the two heads of a line on one XCD: its L2 fetches the line once
+        const unsigned pair = 8u * (id >> 4) + (id & 7u);
+        rest = (int)a.by_pairs.of(pair);
+        kvh = 2 * ((int)pair - rest * (a.Hkv / 2)) + (int)((id >> 3) & 1u);
+        if (rest >= a.B * a.tiles * a.nsplit) return;
+    } else {
+        rest = (int)a.by_heads.of(id);
+        kvh = (int)id - rest * a.Hkv;
+    }
     const int part = (int)a.by_seqs.of((unsigned)rest);
     const int sp = part / a.tiles, rt = part - sp * a.tiles;
     int b = rest - part * a.B + sp;

@@ -622,7 +622,7 @@ __global__ __launch_bounds__(64 * NW, 2) void HG_RW_KERNEL(RaggedArgs a) {
     if constexpr (MODE == kDense) {
         tile_workgroup<MODE>(a, blockIdx.x);
     } else {
-        const unsigned tiles = (unsigned)a.tiles_all * (unsigned)a.Hkv * (unsigned)a.tile_nsplit, rows = (unsigned)a.B * (unsigned)a.tiles * (unsigned)a.nsplit * (unsigned)a.Hkv;
+        const unsigned tiles = (unsigned)a.tiles_all * (unsigned)a.Hkv * (unsigned)a.tile_nsplit, rows = a.row_wgs;
         const unsigned both = min((tiles + 255u) / 256u, (rows + 255u) / 256u), block = blockIdx.x >> 8, in = blockIdx.x & 255u;
         const bool is_tile = block < 2u * both ? (block & 1u) == 0u : tiles > rows;
         const unsigned id = (block < 2u * both ? block >> 1 : block - both) * 256u + in;
