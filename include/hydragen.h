@@ -303,7 +303,7 @@ int hg_kv_append_fp8(hg_ctx* ctx, const void* Knew, const void* Vnew, void* Ks8,
  * there; token t attends to rows [0, lengths[b] - (n-1-t)).  n = 1 is decode; a token that sees no row gets O = 0, LSE = -inf.  Rows above
  * max_len are ignored (min(lengths[b], max_len) takes the place of lengths[b]); tokens of a sequence from max_new (a host upper bound) on are not computed.  The
  * pool may hold 2^31 - 1 rows, bf16 or codes (weights are rounded to bf16 over either); pool rows that no sequence owns may hold anything, NaN included.
- * In both, a key that a token does not see may hold anything, but the value rows of one sequence must be finite: they are multiplied with weights of zero.
+ * In both, the key and value rows that a token does not see may hold anything, infinities and NaN included, its own sequence's later rows among them.
  * Both use the workspace, where there is one, to split long key ranges over more workgroups, and run without it.
  *
  * hg_page_slots: places for the new tokens.  lengths, counts: DEVICE int32[B], rows that sequence b has in the cache and new tokens that it brings

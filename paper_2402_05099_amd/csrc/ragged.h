@@ -100,6 +100,52 @@ struct WriteArgs {
 hipError_t launch_kv_write(const WriteArgs& a, hipStream_t s);
 
 #ifdef __HIPCC__
+// A value that is infinite or NaN would reach the rows of a tile that do not see its key: 0 times it is NaN.  So in stages that some row does not see as a whole such values are
+// 0 in LDS (take_out), and the rows that do see them have them added at the end, from memory (value_if_not_finite).
+template <bool CODES>      // the top bit of every element of the word that is not finite
+__device__ __forceinline__ unsigned not_finite(unsigned v) {
+    return CODES ? ((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : ((v & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
+}
+// Of N pieces of 16 bytes at `at`, `step` bytes apart; true: some lane had one.
+template <bool CODES, int N>
+__device__ __forceinline__ bool take_out(unsigned char* at, int step) {
+    typedef unsigned V4 __attribute__((ext_vector_type(4)));
+    V4 v[N];
+    unsigned bad = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = *reinterpret_cast<const V4*>(at + i * step);
+    if constexpr (CODES) {
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i) bad |= not_finite<CODES>(v[i / 4][i % 4]);
+    } else {      // two instructions a word: the largest magnitude
+        typedef unsigned short Pair __attribute__((ext_vector_type(2)));
+        Pair most = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(Pair, v[i / 4][i % 4] & 0x7fff7fffu));
+        bad = not_finite<CODES>(__builtin_bit_cast(unsigned, most));
+    }
+    if (__builtin_expect(!__any(bad != 0u), 1)) return false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const unsigned x = not_finite<CODES>(v[i][k]);
+            v[i][k] &= ~(CODES ? (x >> 7) * 0xffu : (x >> 15) * 0xffffu);
+        }
+        *reinterpret_cast<V4*>(at + i * step) = v[i];
+    }
+    return true;
+}
+template <bool CODES>
+__device__ __forceinline__ float value_if_not_finite(const unsigned char* e) {
+    if constexpr (CODES) {
+        return (*e & 0x7f) == 0x7f ? __builtin_nanf("") : 0.f;
+    } else {
+        const unsigned x = *reinterpret_cast<const uint16_t*>(e);
+        return (x & 0x7f80u) == 0x7f80u ? __builtin_bit_cast(float, x << 16) : 0.f;
+    }
+}
+
 // What a tile's kernel knows of its sequence; uniform over the workgroup.
 struct RaggedSeq {
     int b;

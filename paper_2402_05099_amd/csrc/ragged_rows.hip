@@ -8,7 +8,7 @@ namespace hg {
 using namespace rr;
 
 template <int D, bool CODES, bool BOTH, int NW>
-__global__ __launch_bounds__(64 * NW) void ragged_rows_kernel(RaggedArgs a) { rows_workgroup<D, CODES, BOTH, NW>(a, blockIdx.x); }
+__global__ __launch_bounds__(64 * NW, 2) void ragged_rows_kernel(RaggedArgs a) { rows_workgroup<D, CODES, BOTH, NW>(a, blockIdx.x); }
 
 // Parts first, first + step, .. of a row's `parts` joined by Eq. 5 into (m, den, o): D / 8 lanes of eight columns.  Part p of row `at` is O[p * part_rows + at],
 // L[p * part_rows + at].

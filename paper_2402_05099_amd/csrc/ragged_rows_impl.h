@@ -143,6 +143,7 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
         }
     };
     const int mine = nst > w ? (nst - w + NW - 1) / NW : 0;
+    int spoiled = mine;      // the first stage of this wavefront with values that were taken out: infinite or NaN, and not seen by every row
     if (mine > 0) {
         look_up(0);
         copy(a.K, voffK, 0, dst);
@@ -170,8 +171,32 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
             for (int c = 0; c < CPS; ++c)
                 if (c * RPI + l / (64 / RPI) >= ke - key0) *reinterpret_cast<uintx4*>(slot + R_::TENSOR + c * 1024 + l * 16) = uintx4{0u, 0u, 0u, 0u};
         }
+        if (key0 + KT > all_see && all_see < ke) {      // some row does not see the stage as a whole
+            if (take_out<CODES, CPS>(slot + R_::TENSOR + l * 16, 1024)) spoiled = min(spoiled, i);
+        }
         t.values(slot + R_::TENSOR, pb);
         if (more) copy(a.V, voffV, i + 1, dst + R_::TENSOR);
+    }
+
+    if (__builtin_expect(spoiled < mine, 0)) {      // the rows that see them get them from memory
+#pragma unroll 1
+        for (int i = spoiled; i < mine; ++i)
+#pragma unroll 1
+            for (int key = k0 + (w + i * NW) * KT, end = min(key + KT, min(ke, seen)); key < end; ++key) {
+                const int page = min(max(a.pg.table[(int64_t)b * a.pg.stride + min(key >> shift, a.pg.stride - 1)], 0), a.pg.n_pages - 1);
+                const unsigned char* const vr = a.V + (((int64_t)page << shift) + (key & ((1 << shift) - 1))) * a.kv_stride + (int64_t)kvh * (D * ES);
+                if constexpr (TR == 16) {
+#pragma unroll
+                    for (int db = 0; db < Tile::DB16; ++db)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) t.Oacc16[db][k] += value_if_not_finite<CODES>(vr + (16 * db + 4 * t.lg + k) * ES);
+                } else {
+#pragma unroll
+                    for (int db = 0; db < Tile::DB; ++db)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) t.Oacc[db][k] += value_if_not_finite<CODES>(vr + (32 * db + 8 * (k / 4) + 4 * t.hl + k % 4) * ES);
+                }
+            }
     }
 
     // ---- the wavefronts' (m, l, O) meet: O as [row][16-byte piece ^ row], statistics behind the slots ----

@@ -61,7 +61,7 @@ constexpr int lds_bytes(int mode) {
     return ring > results ? ring : results;
 }
 static_assert(kCodeBytes == 1024, "one copy instruction per wavefront, stage and tensor of codes");
-static_assert(lds_bytes(kCodes) <= 81920 && lds_bytes(kDense) <= 81920, "two workgroups to a CU");
+static_assert(lds_bytes(kCodes) + 16 <= 81920 && lds_bytes(kDense) + 16 <= 81920, "two workgroups to a CU");      // (16: a flag)
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
@@ -149,6 +149,9 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
     const int k_all = __builtin_amdgcn_readfirstlane(before + token_of(min(row0 + kTileRows, nrows) - 1)), ke = min(k_all, k0 + a.tile_chunk);      // keys [k0, ke) of k_all
     const int nst = ke > k0 ? (ke - k0 + KT - 1) / KT : 0, nfull = ke > k0 ? (ke - k0) / KT : 0;
     if (sp > 0 && nst == 0) return;      // (the join looks at no part that starts behind a row's keys)
+    // stages from here on have keys that some row of the tile does not see
+    const int all_see = __builtin_amdgcn_readfirstlane(max(min(before + token_of(row0), ke), k0));
+    const int masked = all_see < ke ? (all_see - k0) / KT : nst;
     // this wavefront's rows, and this lane's
     const int wrow0 = row0 + 32 * w;
     const bool any = wrow0 < nrows;
@@ -368,6 +371,13 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
         for (int i = 0; i < KOPS; ++i)
             if (k0 + s * KT + w * RPW + i * RPC + lrow >= ke) *reinterpret_cast<uintx4*>(smem + VRING + (s % NS) * VSTB + (w * RPW + i * RPC) * (D * ES) + l * 16) = uintx4{0u, 0u, 0u, 0u};
     };
+    // Whoever has copied the values of a stage that some row does not see as a whole takes those out that are not finite (take_out, ragged.h)
+    unsigned char* const flag = smem + lds_bytes(MODE);
+    bool spoiled = false;
+    const auto finite_only = [&](int s) {
+        constexpr int RPC = CODES ? RPW : RPI;
+        if (take_out<CODES, KOPS>(smem + VRING + (s % NS) * VSTB + w * RPW * (D * ES) + l * 16, RPC * (D * ES))) spoiled = true;
+    };
     const auto meet = [&]() {      // barrier of the workgroup, which no memory operation is moved over
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
@@ -379,12 +389,14 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
         if (0 < nst) expand(0);
         if (1 < nst) expand(1);
         if (partial == 0) clear_rows(0);
+        if (masked == 0 && nst > 0) finite_only(0);
         copy_some([&](auto tail) {
             if (4 < nst) copy_stage(4, 4, true, tail);
             if (5 < nst) copy_stage(5, 5, true, tail);
         });
     } else {
         if (partial == 0) clear_rows(0);
+        if (masked == 0 && nst > 0) finite_only(0);
         // (in this order: step 0 waits for all but the last K and the last V)
         copy_some([&](auto tail) {
             if (2 < nst) copy_stage(2, 2, true, tail);
@@ -394,6 +406,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
         });
         // K of stage 4 has the slot of stage 0, whose scores are taken first
     }
+    if (tid == 0) *reinterpret_cast<int*>(flag) = 0;
     lds_done();
     meet();
 
@@ -483,6 +496,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
     const auto before_step = [&](int j) {      // the careful form; the partial stage's V rows are first read in the step before its own
         wait_careful(j);
         if (j + 1 == partial) clear_rows(partial);
+        if (j + 1 >= masked && j + 1 < nst) finite_only(j + 1);
         lds_done();
         meet();
     };
@@ -529,8 +543,8 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
         add_sum(Scur, ssum, rsum, pn);
     };
     int j = 0;
-    // groups of plain steps: every copy they make is of a full stage, every weight they take of a stage that all rows see
-    const int plain = min(nfull - KA, (w_least - k0) / KT - 1);
+    // groups of plain steps: every copy they make is of a full stage, every weight they take, and the values they are the first to read, of a stage that all rows see
+    const int plain = min(min(nfull - KA, (w_least - k0) / KT - 1), masked - 1);
     for (; j + NS <= plain; j += NS) {
         if constexpr (PAGED) {
             if (j + NS + KA > page_base + 64) look_up(j);
@@ -565,8 +579,30 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
 
     // ---- results: a wavefront's 32 rows through LDS, to leave as whole lines (the ring is free once everyone is here) ----
     wait_vm<0>();
+    if (spoiled && l == 0) *reinterpret_cast<int*>(flag) = 1;
+    lds_done();
     meet();
     if (!any) return;
+    if (__builtin_expect(*reinterpret_cast<const volatile int*>(flag) != 0, 0)) {      // the rows that see what was taken out
+#pragma unroll 1
+        for (int key = k0 + masked * KT; key < ke; ++key) {
+            int64_t row;
+            if constexpr (PAGED) {
+                const int page = min(max(a.pg.table[(int64_t)b * a.pg.stride + min(key >> a.pg.shift, a.pg.stride - 1)], 0), a.pg.n_pages - 1);
+                row = ((int64_t)page << a.pg.shift) + (key & ((1 << a.pg.shift) - 1));
+            } else {
+                row = q0 + key;
+            }
+            if (key >= seen) continue;
+            const unsigned char* const vr = Vh + row * kv_stride + 4 * hl * ES;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) Oacc[db][4 * q4 + i] += value_if_not_finite<CODES>(vr + (32 * db + 8 * q4 + i) * ES);
+        }
+    }
     const float ltot = half_sum(lsum), lr = half_sum(lround);
     const float inv = lr > 0.f ? a.v_scale / lr : 0.f;
     const bool in_parts = k_all > a.tile_chunk;      // (a tile of one range has the result itself)
@@ -639,7 +675,7 @@ __global__ __launch_bounds__(64 * NW, 2) void HG_RW_KERNEL(RaggedArgs a) {
 
 template <int MODE>
 static hipError_t launch_mode(const RaggedArgs& a, hipStream_t s) {
-    constexpr int bytes = MODE == kDense ? lds_bytes(MODE) : std::max(lds_bytes(MODE), rr::rows_lds<D, MODE == kCodes, true>(NW));
+    constexpr int bytes = MODE == kDense ? lds_bytes(MODE) + 16 : std::max(lds_bytes(MODE) + 16, rr::rows_lds<D, MODE == kCodes, true>(NW));
     static_assert(bytes <= 81920, "two workgroups to a CU");
     const int64_t tiles = (int64_t)a.tiles_all * a.Hkv * a.tile_nsplit, grid = MODE == kDense ? tiles : ((tiles + 255) / 256 + (rows_grid(a) + 255) / 256) * 256;
     if (grid >= (1LL << 31)) return hipErrorInvalidValue;

@@ -600,3 +600,89 @@ def test_calls_of_up_to_sixty_four_rows(B, D, codes):
     run_chunk(pairs, (16, 4), D, codes=codes, mib=16)
     run_chunk(pairs, (16, 4), D, codes=codes, fp32=True, lead=1)
     run_chunk([(3000, 16), (1, 16)] + pairs, (16, 4), D, codes=codes, mib=64, ps=64)
+
+
+# ---- values that are infinite or NaN reach the tokens that see them, and no others -----------------------------------------------------
+
+BAD = [(math.nan, 3), (math.inf, 17), (-math.inf, 40), (math.nan, 63)]      # value, column
+
+
+def with_bad_values(run, O, L, Oref, Lref, off, lens, counts, spoiled, G, what):
+    """spoiled: (sequence, key, KV head, column, value); Oref was taken with zeros in their places"""
+    run()
+    torch.cuda.synchronize()
+    O, L = O.cpu().double(), L.cpu().double()
+    got_all = O.clone()
+    assert torch.isfinite(Oref).all()
+    for b, key, h, d, x in spoiled:
+        for t in range(counts[b]):
+            if key < lens[b] - (counts[b] - 1 - t):
+                got = got_all[int(off[b]) + t, h * G:(h + 1) * G, d]
+                assert not torch.isfinite(got).any(), f"{what}: token {t} of {b} sees {x} in row {key} and does not show it"
+                O[int(off[b]) + t, h * G:(h + 1) * G, d] = Oref[int(off[b]) + t, h * G:(h + 1) * G, d]
+    check(O.numpy(), L.numpy(), Oref.numpy(), Lref.numpy(), what)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("heads", [(2, 2), (8, 2), (16, 1)])
+def test_values_that_are_not_seen_yet_may_be_anything(heads, D):
+    Hq, Hkv = heads
+    G = Hq // Hkv
+    lens = [300, 1, 77, 140, 33]
+    off = offsets(lens)
+    g = torch.Generator().manual_seed(D + Hq)
+    T = int(off[-1])
+    Q, K, V = rand(g, T, Hq, D), rand(g, T, Hkv, D), rand(g, T, Hkv, D)
+    spoiled = [(b, key, i % Hkv, BAD[i % 4][1], BAD[i % 4][0]) for i, (b, key) in
+               enumerate([(0, 5), (0, 100), (0, 131), (0, 255), (0, 256), (0, 299), (2, 40), (2, 76), (3, 127), (3, 128), (4, 31), (4, 32)])]
+    bad = V.clone()
+    for b, key, h, d, x in spoiled:
+        V[int(off[b]) + key, h, d] = 0
+        bad[int(off[b]) + key, h, d] = x
+    rows = [(int(off[b]), int(off[b + 1])) for b in range(len(lens))]
+    Oref, Lref = plain.attention(Q, off, [K[a:z].double() for a, z in rows], [V[a:z].double() for a, z in rows], lens)
+    O, L = torch.empty(T, Hq, D, device=DEV), torch.empty(T, Hq, device=DEV)
+    ctx = context()
+    with_bad_values(lambda: hb.hg_prompt_attn(ctx, Q.to(DEV), K.to(DEV), bad.to(DEV), i32(off), max(lens), O, L), O, L, Oref, Lref, off, lens, lens, spoiled, G,
+                    f"prompts {heads} {D}")
+    ctx.close()
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("heads", [(2, 2), (8, 2), (16, 1)])
+def test_values_of_later_tokens_in_the_cache_may_be_anything(heads, D, codes):
+    Hq, Hkv = heads
+    G = Hq // Hkv
+    ps, scales = 32, (0.02, 0.015)
+    pairs = [(200, 3), (90, 1), (300, 150), (64, 64), (2000, 9), (33, 2)]
+    lens, counts = [r for r, _ in pairs], [n for _, n in pairs]
+    off = offsets(counts)
+    g = torch.Generator().manual_seed(D + Hq)
+    Kp, Vp, table, keys, values = make_cache(g, lens, Hkv, D, ps, codes, scales)
+    spoiled = [(b, key, i % Hkv, BAD[i % 4][1], BAD[i % 4][0]) for i, (b, key) in
+               enumerate([(0, 198), (0, 199), (2, 160), (2, 191), (2, 230), (2, 299), (3, 0), (3, 31), (3, 63), (4, 1992), (4, 1999), (5, 32)])]
+    for b, key, h, d, x in spoiled:
+        values[b][key, h, d] = 0
+        row = int(table[b, key // ps]) * ps + key % ps
+        Vp[row, h, d] = (0x7F if x > 0 else 0xFF) if codes else x
+    Q = rand(g, int(off[-1]), Hq, D)
+    Oref, Lref = plain.attention(Q, off, keys, values, lens)
+    kv = hb.PagedKV(K=Kp, V=Vp, page_table=table, page_size=ps, kv_format=hb.HG_KV_E4M3 if codes else hb.HG_KV_BF16, k_scale=scales[0], v_scale=scales[1])
+    O, L = torch.empty(int(off[-1]), Hq, D, device=DEV), torch.empty(int(off[-1]), Hq, device=DEV)
+    for mib in (0, 64):
+        ctx = context(mib)
+        with_bad_values(lambda: hb.hg_chunk_attn_paged(ctx, Q.to(DEV), i32(off), kv, i32(lens), max(counts), max(lens), O, L), O, L, Oref, Lref, off, lens, counts,
+                        spoiled, G, f"chunks {heads} {D} {'codes' if codes else 'bf16'} {mib}")
+        ctx.close()
+    # few rows alone
+    few = [0, 1, 4, 5]
+    qo, ln, ct = offsets([counts[b] for b in few]), [lens[b] for b in few], [counts[b] for b in few]
+    Qf = torch.cat([Q[int(off[b]):int(off[b + 1])] for b in few])
+    kv = hb.PagedKV(K=Kp, V=Vp, page_table=table[few].contiguous(), page_size=ps, kv_format=kv.kv_format, k_scale=scales[0], v_scale=scales[1])
+    O, L = torch.empty(int(qo[-1]), Hq, D, device=DEV), torch.empty(int(qo[-1]), Hq, device=DEV)
+    ctx = context(64)
+    Oref, Lref = plain.attention(Qf, qo, [keys[b] for b in few], [values[b] for b in few], ln)
+    with_bad_values(lambda: hb.hg_chunk_attn_paged(ctx, Qf.to(DEV), i32(qo), kv, i32(ln), max(ct), max(ln), O, L), O, L, Oref, Lref, qo, ln, ct,
+                    [(few.index(b), *rest) for b, *rest in spoiled if b in few], G, f"few rows {heads} {D} {'codes' if codes else 'bf16'}")
+    ctx.close()
