@@ -100,6 +100,9 @@ struct WriteArgs {
 hipError_t launch_kv_write(const WriteArgs& a, hipStream_t s);
 
 #ifdef __HIPCC__
+// LSE of a part whose row is NaN: infinity, which no maximum passes over, and with which every sum of parts becomes NaN.
+__device__ __forceinline__ float part_lse(float lse) { return lse != lse ? INFINITY : lse; }
+
 // A value that is infinite or NaN would reach the rows of a tile that do not see its key: 0 times it is NaN.  So in stages that some row does not see as a whole such values are
 // 0 in LDS (take_out), and the rows that do see them have them added at the end, from memory (value_if_not_finite).
 template <bool CODES>      // the top bit of every element of the word that is not finite

@@ -48,10 +48,10 @@ __device__ __forceinline__ void join_parts(const float* O, const float* L, int64
 }
 template <int D>
 __device__ __forceinline__ void store_joined(const OutDev& out, int64_t row, int c8, float m, float den, float (&o)[8]) {
-    const float inv = den > 0.f ? 1.0f / den : 0.f;
+    const float inv = den == 0.f ? 0.f : 1.0f / den;
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] *= inv;
-    store_row8<D>(out, row, c8, o, den > 0.f ? m + __logf(den) : -INFINITY);
+    store_row8<D>(out, row, c8, o, den == 0.f ? -INFINITY : m + __logf(den));
 }
 
 // Joins the parts of both kinds of rows, PG groups of D / 8 lanes to a row, each with every PG-th of its parts (a row of many parts would be a chain of loads

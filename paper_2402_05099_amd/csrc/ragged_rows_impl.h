@@ -203,6 +203,7 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
     float lsum = t.lsum;
     if constexpr (TR == 16) lsum += __shfl_xor(lsum, 16);
     lsum = half_sum(lsum);
+    const float m_row = lsum != lsum ? INFINITY : t.m_used;      // (as part_lse)
     float* const stat = reinterpret_cast<float*>(rr_smem + NW * R_::SLOT);      // [NW][2][TR]
     constexpr int PCS = D / 4;
     const auto piece = [&](unsigned char* base, int row, int c) { return reinterpret_cast<float4*>(base + row * (D * 4) + ((c ^ (row & (PCS - 1))) * 16)); };
@@ -210,14 +211,14 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
 #pragma unroll
         for (int db = 0; db < Tile::DB16; ++db)
             *piece(slot, t.ln, 4 * db + t.lg) = make_float4(t.Oacc16[db][0], t.Oacc16[db][1], t.Oacc16[db][2], t.Oacc16[db][3]);
-        if (t.lg == 0) { stat[(2 * w) * TR + t.ln] = t.m_used; stat[(2 * w + 1) * TR + t.ln] = lsum; }
+        if (t.lg == 0) { stat[(2 * w) * TR + t.ln] = m_row; stat[(2 * w + 1) * TR + t.ln] = lsum; }
     } else {
 #pragma unroll
         for (int db = 0; db < Tile::DB; ++db)
 #pragma unroll
             for (int q4 = 0; q4 < 4; ++q4)
                 *piece(slot, t.lq, 8 * db + 2 * q4 + t.hl) = make_float4(t.Oacc[db][4 * q4], t.Oacc[db][4 * q4 + 1], t.Oacc[db][4 * q4 + 2], t.Oacc[db][4 * q4 + 3]);
-        if (t.hl == 0) { stat[(2 * w) * TR + t.lq] = t.m_used; stat[(2 * w + 1) * TR + t.lq] = lsum; }
+        if (t.hl == 0) { stat[(2 * w) * TR + t.lq] = m_row; stat[(2 * w + 1) * TR + t.lq] = lsum; }
     }
     __syncthreads();
     constexpr int LPR = D / 8;      // lanes per row, eight columns each
@@ -244,18 +245,18 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
                 }
             }
         }
-        const float inv = den > 0.f ? a.v_scale / den : 0.f;
+        const float inv = den == 0.f ? 0.f : a.v_scale / den;
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] *= inv;
         const int tk = (int)a.by_group.of((unsigned)rr), gg = rr - tk * a.G;
         // one range: the result itself; several: part `sp`
         const int64_t at = !in_parts ? (int64_t)(q0 + tk) * a.Hq + kvh * a.G + gg : ((int64_t)b * a.Hkv + kvh) * a.few_most + (rr - row0);
-        const float lse = den > 0.f ? m * a.scale + __logf(den) : -INFINITY;
+        const float lse = den == 0.f ? -INFINITY : m * a.scale + __logf(den);
         if (in_parts) {
             float* const O = a.part_O + ((int64_t)sp * a.part_rows + at) * D + 8 * c8;
             *reinterpret_cast<float4*>(O) = make_float4(o[0], o[1], o[2], o[3]);
             *reinterpret_cast<float4*>(O + 4) = make_float4(o[4], o[5], o[6], o[7]);
-            if (c8 == 0) a.part_L[(int64_t)sp * a.part_rows + at] = lse;
+            if (c8 == 0) a.part_L[(int64_t)sp * a.part_rows + at] = part_lse(lse);
             continue;
         }
         store_row8<D>(a.out, at, c8, o, lse);

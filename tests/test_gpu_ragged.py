@@ -686,3 +686,59 @@ def test_values_of_later_tokens_in_the_cache_may_be_anything(heads, D, codes):
     with_bad_values(lambda: hb.hg_chunk_attn_paged(ctx, Qf.to(DEV), i32(qo), kv, i32(ln), max(ct), max(ln), O, L), O, L, Oref, Lref, qo, ln, ct,
                     [(few.index(b), *rest) for b, *rest in spoiled if b in few], G, f"few rows {heads} {D} {'codes' if codes else 'bf16'}")
     ctx.close()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("where", ["query", "key"])
+def test_a_token_that_meets_a_nan_says_so(D, where):
+    lens = [200, 40]
+    off, g = offsets(lens), torch.Generator().manual_seed(D)
+    Q, K, V = rand(g, 240, 4, D), rand(g, 240, 2, D), rand(g, 240, 2, D)
+    rows = [(0, 200), (200, 240)]
+    Oref, Lref = plain.attention(Q, off, [K[a:z].double() for a, z in rows], [V[a:z].double() for a, z in rows], lens)
+    if where == "query":
+        lost = torch.tensor([3, 150, 239])
+        Q[lost] = NAN
+    else:
+        lost = torch.arange(100, 200)
+        K[100] = NAN
+    kept = torch.ones(240, dtype=torch.bool)
+    kept[lost] = False
+    O, L = torch.empty(240, 4, D, device=DEV), torch.empty(240, 4, device=DEV)
+    ctx = context()
+    hb.hg_prompt_attn(ctx, Q.to(DEV), K.to(DEV), V.to(DEV), i32(off), 200, O, L)
+    O, L = O.cpu().double(), L.cpu().double()
+    assert torch.isnan(O[~kept]).all() and torch.isnan(L[~kept]).all()
+    check(O[kept].numpy(), L[kept].numpy(), Oref[kept].numpy(), Lref[kept].numpy(), f"prompt with a NaN {where}")
+    ctx.close()
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("where", ["query", "key"])
+@pytest.mark.parametrize("mib", [0, 64])
+def test_a_token_that_meets_a_nan_in_the_cache_says_so(mib, where, D, codes):
+    for pairs in ([(5000, 1), (300, 6), (40, 1)], [(5000, 150), (300, 6), (40, 1)]):
+        lens, counts = [r for r, _ in pairs], [n for _, n in pairs]
+        off, g = offsets(counts), torch.Generator().manual_seed(D)
+        Kp, Vp, table, keys, values = make_cache(g, lens, 2, D, 64, codes)
+        T = int(off[-1])
+        Q = rand(g, T, 4, D)
+        Oref, Lref = plain.attention(Q, off, keys, values, lens)
+        if where == "query":
+            lost = torch.tensor([0, int(off[1]) + 2, T - 1])
+            Q[lost] = NAN
+        else:      # one that all tokens of two sequences see
+            lost = torch.cat([torch.arange(0, counts[0]), torch.arange(int(off[1]), int(off[2]))])
+            for b, j in ((0, 3000), (1, 70)):
+                Kp[int(table[b, j // 64]) * 64 + j % 64] = 0x7F if codes else NAN
+        kept = torch.ones(T, dtype=torch.bool)
+        kept[lost] = False
+        kv = hb.PagedKV(K=Kp, V=Vp, page_table=table, page_size=64, kv_format=hb.HG_KV_E4M3 if codes else hb.HG_KV_BF16, k_scale=0.02, v_scale=0.015)
+        O, L = torch.empty(T, 4, D, device=DEV), torch.empty(T, 4, device=DEV)
+        ctx = context(mib)
+        hb.hg_chunk_attn_paged(ctx, Q.to(DEV), i32(off), kv, i32(lens), max(counts), max(lens), O, L)
+        O, L = O.cpu().double(), L.cpu().double()
+        assert torch.isnan(O[~kept]).all() and torch.isnan(L[~kept]).all()
+        check(O[kept].numpy(), L[kept].numpy(), Oref[kept].numpy(), Lref[kept].numpy(), f"chunks with a NaN {where}")
+        ctx.close()
