@@ -39,7 +39,7 @@ EXPORTS = (
     "hg_create", "hg_destroy", "hg_set_stream", "hg_set_option", "hg_workspace_bytes", "hg_prefix_attn",
     "hg_prefix_attn_grouped", "hg_suffix_attn", "hg_merge", "hg_hydragen_attn", "hg_naive_attn", "hg_read_stage_timings",
     "hg_strerror", "hg_suffix_attn_paged", "hg_hydragen_attn_paged", "hg_kv_append", "hg_kv_append_paged",
-    "hg_debug_wide_plan", "hg_debug_wide_ranges", "hg_debug_wide_team", "hg_debug_item_runs", "hg_debug_suffix_plan", "hg_debug_fused_plan", "hg_debug_single_work", "hg_suffix_attn_fp8", "hg_hydragen_attn_fp8", "hg_kv_append_fp8",
+    "hg_debug_wide_plan", "hg_debug_wide_ranges", "hg_debug_wide_team", "hg_debug_item_runs", "hg_debug_suffix_plan", "hg_debug_fused_plan", "hg_debug_single_work", "hg_debug_ragged_plan", "hg_suffix_attn_fp8", "hg_hydragen_attn_fp8", "hg_kv_append_fp8",
     "hg_prompt_attn", "hg_chunk_attn_paged", "hg_page_slots", "hg_kv_write_paged",
     "hg_hydragen_attn_static", "hg_debug_mfma_loop", "hg_debug_stream_read", "hg_debug_xcd_of_workgroups",
 )
@@ -142,6 +142,8 @@ def lib() -> ctypes.CDLL:
         L.hg_debug_fused_plan.restype = ci
         L.hg_debug_single_work.argtypes = [ci] * 4 + [ctypes.POINTER(ci)]
         L.hg_debug_single_work.restype = ci
+        L.hg_debug_ragged_plan.argtypes = [ci] * 9 + [cs, ctypes.POINTER(i64)]
+        L.hg_debug_ragged_plan.restype = ci
         L.hg_debug_mfma_loop.argtypes = [vp, ci, ci, vp, vp]
         L.hg_debug_mfma_loop.restype = ci
         L.hg_debug_stream_read.argtypes = [vp, vp, cs, vp]
@@ -696,6 +698,16 @@ def hg_debug_fused_plan(levels, B: int, nq: int, Hq: int, Hkv: int, D: int, max_
         plan["wavefronts"], plan["slots"] = plan["slots"], 0
         plan["dealt"], plan["nchunks"] = bool(plan["nchunks"]), 0
     return plan
+
+
+def hg_debug_ragged_plan(rows: int, max_len: int, B: int, Hq: int, Hkv: int, D: int, max_new: Optional[int] = None, codes: bool = False, workspace_bytes: int = 0):
+    """dict of how hg_prompt_attn (max_new None) or hg_chunk_attn_paged would run, or the error code it would return (host only)."""
+    out = (ctypes.c_int64 * 14)()
+    rc = lib().hg_debug_ragged_plan(int(max_new is not None), int(codes), rows, max_new or 0, max_len, B, Hq, Hkv, D, workspace_bytes, out)
+    if rc != HG_OK:
+        return rc
+    return dict(zip(("tiles", "few_rows", "few_most", "nsplit", "chunk", "tile_nsplit", "tile_chunk", "part_O", "part_L", "tile_part_O", "tile_part_L", "workgroups", "threads",
+                     "join"), list(out)))
 
 
 def hg_debug_mfma_loop(ctx: Context, random_operands: bool, iters: int, clocks: torch.Tensor, sink: torch.Tensor) -> None:

@@ -62,6 +62,18 @@ inline int64_t rows_grid(const RaggedArgs& a) {
     return a.paired ? (n + 15) / 16 * 16 : n;
 }
 
+// Workgroups that take tiles
+inline int64_t tiles_grid(const RaggedArgs& a) { return (int64_t)a.tiles_all * a.Hkv * a.tile_nsplit; }
+// ... and of a launch that has tiles: over a paged cache both kinds by turns, 256 of each
+inline int64_t ragged_grid(const RaggedArgs& a) { return a.few_rows == 0 ? tiles_grid(a) : ((tiles_grid(a) + 255) / 256 + (rows_grid(a) + 255) / 256) * 256; }
+// Workgroups of the join of parts: groups of D / 8 lanes to a row, and of a token's heads
+inline int join_groups(const RaggedArgs& a) { return a.nsplit > 8 || a.tile_nsplit > 8 ? 8 : 1; }
+inline int join_per_token(const RaggedArgs& a, int D) { const int rows = 2048 / D / join_groups(a); return a.tile_nsplit > 1 ? (a.Hq + rows - 1) / rows : 0; }
+inline int64_t join_grid(const RaggedArgs& a, int D) {
+    const int rows = 2048 / D / join_groups(a);
+    return (int64_t)a.rows * join_per_token(a, D) + (a.nsplit > 1 ? (a.part_rows + rows - 1) / rows : 0);
+}
+
 // ---- launchers ----
 hipError_t launch_ragged_rows(const RaggedArgs& a, int D, bool codes, hipStream_t s);       // ragged_rows.hip: what remains, or all there is
 hipError_t launch_ragged_wide(const RaggedArgs& a, bool codes, hipStream_t s);           // ragged_wide.hip, D = 128: tiles, and what remains in the same launch

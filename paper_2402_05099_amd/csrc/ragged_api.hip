@@ -5,6 +5,7 @@
 
 #include "context.h"
 #include "hydragen.h"
+#include "hydragen_debug.h"
 #include "ragged.h"
 
 namespace {
@@ -24,13 +25,23 @@ int page_shift(int page_size) {
     return -1;
 }
 
-// Shapes and row distances that both attention calls have.
-int check_ragged(const hg_ctx* c, const void* Q, int64_t q_stride, const int32_t* q_off, int rows, int max_new, int B, int Hq, int Hkv, int D,
-                 const void* O, int o_dtype) {
-    if (!c || (o_dtype != HG_F32 && o_dtype != HG_BF16) || rows < 0 || max_new < 0 || B < 0 || Hq <= 0 || Hkv <= 0) return HG_ERR_INVALID_ARG;
+// Sizes that both attention calls have.
+int check_sizes(int rows, int max_new, int B, int Hq, int Hkv, int D) {
+    if (rows < 0 || max_new < 0 || B < 0 || Hq <= 0 || Hkv <= 0) return HG_ERR_INVALID_ARG;
     if (D != 64 && D != 128) return HG_ERR_UNSUPPORTED;
     if (Hq % Hkv != 0) return HG_ERR_UNSUPPORTED;
     if ((int64_t)rows * Hq >= (1LL << 31) || B >= (1 << 24) || ((int64_t)rows * (Hq / Hkv) + 256LL * B) * Hkv >= (1LL << 31)) return HG_ERR_UNSUPPORTED;
+    return HG_OK;
+}
+// ... and those of keys in a cache.
+int check_cache_sizes(int max_len, int Hkv, int D) { return max_len >= kAllKeys || (int64_t)Hkv * D * 32 >= (1LL << 31) ? HG_ERR_UNSUPPORTED : HG_OK; }
+
+// Shapes and row distances that both attention calls have.
+int check_ragged(const hg_ctx* c, const void* Q, int64_t q_stride, const int32_t* q_off, int rows, int max_new, int B, int Hq, int Hkv, int D,
+                 const void* O, int o_dtype) {
+    if (!c || (o_dtype != HG_F32 && o_dtype != HG_BF16)) return HG_ERR_INVALID_ARG;
+    const int rc = check_sizes(rows, max_new, B, Hq, Hkv, D);
+    if (rc) return rc;
     if (rows > 0 && B > 0 && max_new > 0) {
         if (!Q || !q_off || !O) return HG_ERR_INVALID_ARG;
         if (q_stride < (int64_t)Hq * D || q_stride % 8 != 0 ||
@@ -83,7 +94,7 @@ void split_keys(int64_t want, int max_len, int least, int step, int64_t rows, in
     const int64_t most = std::min<int64_t>({want, max_len / least, (int64_t)(per ? room.floats / per : 0), 256});
     if (most <= 1 || rows >= (1LL << 31)) return;
     chunk = (int)(((max_len + most - 1) / most + step - 1) / step * step);
-    nsplit = (max_len + chunk - 1) / chunk;
+    nsplit = (int)(((int64_t)max_len + chunk - 1) / chunk);
     O = room.take((size_t)nsplit * rows * D);
     L = room.take((size_t)nsplit * rows);
 }
@@ -134,6 +145,20 @@ void plan_tiles(RaggedArgs& a, int D, Room& room) {
     split_keys(best, a.max_len, 1024, 64, (int64_t)a.rows * a.Hq, D, room, a.tile_nsplit, a.tile_chunk, a.tile_part_O, a.tile_part_L);
 }
 
+// Choices of a call over packed rows, whose sequences have no more keys than there are tokens, whatever the caller's bound ...
+void plan_prompt(RaggedArgs& a, int max_len, int D, Room room) {
+    a.max_len = std::min(max_len, a.rows);
+    plan_tiles(a, D, room);
+}
+// ... and of one over a paged cache.  true: it has tiles
+bool plan_chunk(RaggedArgs& a, int max_len, int D, bool codes, Room room) {
+    a.max_len = max_len;
+    plan_few_rows(a, D, codes, room);
+    const bool tiles = (int64_t)std::min(a.max_new, a.rows) * a.G > a.few_rows;
+    if (tiles) plan_tiles(a, D, room);
+    return tiles;
+}
+
 // tiles: the call has any; what remains behind them, or is all there is, goes along
 int run(const hg_ctx* c, const RaggedArgs& a, int D, bool codes, bool tiles) {
     const int rc = rc_of(!tiles ? launch_ragged_rows(a, D, codes, c->stream) : D == 128 ? launch_ragged_wide(a, codes, c->stream) : launch_ragged_wide_d64(a, codes, c->stream));
@@ -158,9 +183,7 @@ int hg_prompt_attn(hg_ctx* c, const void* Q, const void* K, const void* V, int64
     a.K = static_cast<const unsigned char*>(K);
     a.V = static_cast<const unsigned char*>(V);
     a.kv_stride = 2 * kv_stride;
-    a.max_len = max_len;
-    Room room = room_of(c);
-    plan_tiles(a, D, room);
+    plan_prompt(a, max_len, D, room_of(c));
     return run(c, a, D, false, true);
 }
 
@@ -174,8 +197,7 @@ int hg_chunk_attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_
     if (codes && (!positive_scale(kv->k_scale) || !positive_scale(kv->v_scale))) return HG_ERR_INVALID_ARG;
     const int shift = page_shift(kv->page_size);
     if (shift < 0 || kv->n_pages < 0 || kv->table_stride < 0) return HG_ERR_INVALID_ARG;
-    if ((int64_t)kv->n_pages * kv->page_size >= (1LL << 31) || (int64_t)kv->table_stride * kv->page_size >= (1LL << 31) || max_len >= kAllKeys ||
-        (int64_t)Hkv * D * 32 >= (1LL << 31))
+    if ((int64_t)kv->n_pages * kv->page_size >= (1LL << 31) || (int64_t)kv->table_stride * kv->page_size >= (1LL << 31) || check_cache_sizes(max_len, Hkv, D))
         return HG_ERR_UNSUPPORTED;
     if (rows == 0 || B == 0 || max_new == 0) return HG_OK;
     if (!lengths || !kv->K || !kv->V || !kv->page_table || kv->n_pages < 1 || (int64_t)kv->table_stride * kv->page_size < std::max(max_len, 1) ||
@@ -190,15 +212,11 @@ int hg_chunk_attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_
     a.pg.shift = shift;
     a.pg.stride = kv->table_stride;
     a.pg.n_pages = kv->n_pages;
-    a.max_len = max_len;
     if (codes) {
         a.scale *= kv->k_scale;
         a.v_scale = kv->v_scale;
     }
-    Room room = room_of(c);
-    plan_few_rows(a, D, codes, room);
-    const bool tiles = (int64_t)std::min(max_new, rows) * a.G > a.few_rows;
-    if (tiles) plan_tiles(a, D, room);
+    const bool tiles = plan_chunk(a, max_len, D, codes, room_of(c));
     return run(c, a, D, codes, tiles);
 }
 
@@ -251,6 +269,27 @@ int hg_kv_write_paged(hg_ctx* c, const void* Knew, const void* Vnew, int64_t str
     a.k_scale = kv->k_scale;
     a.v_scale = kv->v_scale;
     return rc_of(launch_kv_write(a, c->stream));
+}
+
+int hg_debug_ragged_plan(int paged, int codes, int rows, int max_new, int max_len, int B, int Hq, int Hkv, int D, size_t workspace_bytes, int64_t out[14]) {
+    if (!out || max_len < 0) return HG_ERR_INVALID_ARG;
+    int rc = check_sizes(rows, paged ? max_new : max_len, B, Hq, Hkv, D);
+    if (!rc && paged) rc = check_cache_sizes(max_len, Hkv, D);
+    if (rc) return rc;
+    std::fill(out, out + 14, (int64_t)0);
+    if (rows == 0 || B == 0 || (paged ? max_new : max_len) == 0) return HG_OK;      // nothing is launched
+    RaggedArgs a = ragged_args(nullptr, 0, nullptr, rows, paged ? max_new : max_len, B, Hq, Hkv, D, 0.f, nullptr, HG_F32, nullptr);
+    float* const ws = reinterpret_cast<float*>(256);      // (only distances from it are looked at)
+    const Room room{ws, workspace_bytes / sizeof(float)};
+    bool tiles = true;
+    if (paged) tiles = plan_chunk(a, max_len, D, codes != 0, room);
+    else plan_prompt(a, max_len, D, room);
+    const auto at = [&](const float* p) { return p ? (int64_t)((reinterpret_cast<intptr_t>(p) - reinterpret_cast<intptr_t>(ws)) / (int64_t)sizeof(float)) : -1; };
+    const bool join = a.nsplit > 1 || a.tile_nsplit > 1;
+    const int64_t got[14] = {tiles, a.few_rows, a.few_most, a.nsplit, a.chunk, a.tile_nsplit, a.tile_chunk, at(a.part_O), at(a.part_L), at(a.tile_part_O), at(a.tile_part_L),
+                             tiles ? ragged_grid(a) : rows_grid(a), tiles ? 256 : 64 * a.wavefronts, join ? join_grid(a, D) : 0};
+    std::copy(got, got + 14, out);
+    return HG_OK;
 }
 
 }  // extern "C"

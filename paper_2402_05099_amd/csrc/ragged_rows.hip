@@ -164,16 +164,14 @@ hipError_t launch_ragged_rows(const RaggedArgs& a, int D, bool codes, hipStream_
 
 template <int D, int PG>
 static hipError_t launch_join_t(const RaggedArgs& a, hipStream_t s) {
-    constexpr int rows = 2048 / D / PG;
-    const int per_token = a.tile_nsplit > 1 ? (a.Hq + rows - 1) / rows : 0;
-    const int64_t grid = (int64_t)a.rows * per_token + (a.nsplit > 1 ? (a.part_rows + rows - 1) / rows : 0);
+    const int64_t grid = join_grid(a, D);
     if (grid >= (1LL << 31)) return hipErrorInvalidValue;
-    ragged_join_kernel<D, PG><<<(unsigned)grid, 256, 0, s>>>(a, per_token);
+    ragged_join_kernel<D, PG><<<(unsigned)grid, 256, 0, s>>>(a, join_per_token(a, D));
     return hipGetLastError();
 }
 
 hipError_t launch_ragged_join(const RaggedArgs& a, int D, hipStream_t s) {
-    const bool many = a.nsplit > 8 || a.tile_nsplit > 8;
+    const bool many = join_groups(a) > 1;
     if (D == 128) return many ? launch_join_t<128, 8>(a, s) : launch_join_t<128, 1>(a, s);
     return many ? launch_join_t<64, 8>(a, s) : launch_join_t<64, 1>(a, s);
 }

@@ -677,7 +677,7 @@ template <int MODE>
 static hipError_t launch_mode(const RaggedArgs& a, hipStream_t s) {
     constexpr int bytes = MODE == kDense ? lds_bytes(MODE) + 16 : std::max(lds_bytes(MODE) + 16, rr::rows_lds<D, MODE == kCodes, true>(NW));
     static_assert(bytes <= 81920, "two workgroups to a CU");
-    const int64_t tiles = (int64_t)a.tiles_all * a.Hkv * a.tile_nsplit, grid = MODE == kDense ? tiles : ((tiles + 255) / 256 + (rows_grid(a) + 255) / 256) * 256;
+    const int64_t grid = ragged_grid(a);
     if (grid >= (1LL << 31)) return hipErrorInvalidValue;
     static bool attr_set[64] = {};
     int dev = 0;

@@ -1,0 +1,97 @@
+"""Host choices of the calls between a prompt and its first decode step, checked without a GPU: key ranges cover what there can be and nothing else, partial results
+lie in the workspace and beside each other, launches have sizes that can be launched, whatever bounds and workspace the caller gives."""
+import random
+
+import pytest
+
+from paper_2402_05099_amd import binding as hb
+
+NO_BOUND = 2**31 - 1
+WORKSPACES = [0, 1 << 12, 1 << 20, 64 << 20, 512 << 20, 1 << 40]
+HEADS = [(1, 1), (4, 4), (8, 1), (16, 2), (32, 8), (40, 40), (64, 8), (12, 4), (9, 3), (80, 1)]
+
+
+def look(rows, max_len, B, Hq, Hkv, D, max_new=None, codes=False, ws=0):
+    what = f"rows {rows}, max_len {max_len}, B {B}, heads {Hq}/{Hkv}, D {D}, max_new {max_new}, workspace {ws}"
+    p = hb.hg_debug_ragged_plan(rows, max_len, B, Hq, Hkv, D, max_new, codes, ws)
+    assert isinstance(p, dict), f"{what}: error {p}"
+    keys = max_len if max_new is not None else min(max_len, rows)      # a sequence has no more, whatever its length
+    kinds = []
+    if p["tiles"]:
+        kinds.append((p["tile_nsplit"], p["tile_chunk"], rows * Hq, p["tile_part_O"], p["tile_part_L"]))
+    else:
+        assert p["tile_nsplit"] == 1
+    if max_new is not None:
+        kinds.append((p["nsplit"], p["chunk"], B * Hkv * p["few_most"], p["part_O"], p["part_L"]))
+        assert p["few_most"] <= p["few_rows"] and p["few_most"] <= max_new * (Hq // Hkv)
+        assert p["tiles"] or min(rows, max_new) * (Hq // Hkv) <= p["few_rows"], what
+    else:
+        assert p["tiles"] and p["nsplit"] == 1 and p["few_rows"] == 0, what
+    used = []
+    for n, chunk, part_rows, O, L in kinds:
+        assert 1 <= n <= 256 and chunk > 0 and n * chunk >= keys, f"{what}: {n} ranges of {chunk}"
+        if n == 1:
+            assert O == L == -1, what
+            continue
+        assert chunk % 64 == 0 and (n - 1) * chunk < keys, f"{what}: {n} ranges of {chunk}, the last has no key"
+        assert O % 4 == 0, f"{what}: rows are stored in pieces of 16 bytes"
+        used += [(O, O + n * part_rows * D), (L, L + n * part_rows)]
+    used.sort()
+    assert all(a >= 0 and z <= ws // 4 for a, z in used), f"{what}: parts {used} outside the workspace"
+    assert all(z <= a for (_, z), (a, _) in zip(used, used[1:])), f"{what}: parts {used} overlap"
+    assert p["workgroups"] > 0 and p["workgroups"] * p["threads"] < 2**32, f"{what}: {p['workgroups']} workgroups"
+    assert (p["join"] > 0) == bool(used) and p["join"] * 256 < 2**32, what
+    return p
+
+
+@pytest.mark.parametrize("ws", WORKSPACES)
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("D", [64, 128])
+def test_prompts_under_any_bound(D, heads, ws):
+    for rows in (1, 64, 130, 1024, 4096, 5000, 16384, 70000):
+        for max_len in (1, 100, rows, rows + 1, 4096, 8192, 1 << 20, 1 << 30, NO_BOUND - 1, NO_BOUND):
+            for B in (1, 2, 8, 9, 512):
+                look(rows, max_len, B, *heads, D, ws=ws)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_prompt_s_bound_beyond_its_tokens_changes_nothing(D):
+    for rows in (1, 130, 1024, 4096):
+        want = look(rows, rows, 2, 8, 8, D, ws=512 << 20)
+        for max_len in (rows + 1, 8 * rows, 1 << 30, NO_BOUND):
+            assert look(rows, max_len, 2, 8, 8, D, ws=512 << 20) == want
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("ws", WORKSPACES)
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("D", [64, 128])
+def test_chunks_under_any_bound(D, heads, ws, codes):
+    for rows in (1, 45, 256, 3000, 20000):
+        for max_new in (1, 3, 8, 64, 2048, NO_BOUND):
+            for max_len in (0, 1, 515, 1280, 1281, 4096, 32768, 65536 + 33, (1 << 30) - 2):
+                for B in (1, 3, 45, 512):
+                    look(rows, max_len, B, *heads, D, max_new, codes, ws)
+
+
+def test_drawn_calls():
+    rng = random.Random(5)
+
+    def size(most):
+        return min(most, int(2 ** rng.uniform(0, most.bit_length())))
+
+    for _ in range(20000):
+        Hq, Hkv = rng.choice(HEADS)
+        B, rows, ws = size(4096), size(200000), rng.choice(WORKSPACES + [size(1 << 30)])
+        paged = rng.random() < 0.6
+        look(rows, size((1 << 30) - 2) if paged else size(NO_BOUND), B, Hq, Hkv, rng.choice([64, 128]), size(NO_BOUND) if paged else None, rng.random() < 0.5, ws)
+
+
+def test_nothing_to_do_and_refusals():
+    assert hb.hg_debug_ragged_plan(0, 5, 1, 4, 4, 64)["workgroups"] == 0
+    assert hb.hg_debug_ragged_plan(5, 0, 1, 4, 4, 64)["workgroups"] == 0
+    assert hb.hg_debug_ragged_plan(5, 5, 0, 4, 4, 64, 1)["workgroups"] == 0
+    assert hb.hg_debug_ragged_plan(5, 5, 1, 4, 3, 64) == hb.HG_ERR_UNSUPPORTED
+    assert hb.hg_debug_ragged_plan(5, 5, 1, 4, 4, 32) == hb.HG_ERR_UNSUPPORTED
+    assert hb.hg_debug_ragged_plan(5, -1, 1, 4, 4, 64) == hb.HG_ERR_INVALID_ARG
+    assert hb.hg_debug_ragged_plan(5, (1 << 30) - 1, 1, 4, 4, 64, 1) == hb.HG_ERR_UNSUPPORTED
