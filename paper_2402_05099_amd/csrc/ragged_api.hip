@@ -13,6 +13,7 @@ namespace {
 using namespace hg;
 
 constexpr int kAllKeys = 0x3fffffff;      // longer than any key range
+constexpr int64_t kMostWorkgroups = (1LL << 24) - 1024;      // of 256 threads: a launch has fewer than 2^32, and either kind of workgroup is rounded up to whole 256
 
 int rc_of(hipError_t e) { return e == hipSuccess ? HG_OK : HG_ERR_HIP; }
 
@@ -30,7 +31,8 @@ int check_sizes(int rows, int max_new, int B, int Hq, int Hkv, int D) {
     if (rows < 0 || max_new < 0 || B < 0 || Hq <= 0 || Hkv <= 0) return HG_ERR_INVALID_ARG;
     if (D != 64 && D != 128) return HG_ERR_UNSUPPORTED;
     if (Hq % Hkv != 0) return HG_ERR_UNSUPPORTED;
-    if ((int64_t)rows * Hq >= (1LL << 31) || B >= (1 << 24) || ((int64_t)rows * (Hq / Hkv) + 256LL * B) * Hkv >= (1LL << 31)) return HG_ERR_UNSUPPORTED;
+    // (the last: with one range of keys to each, tiles and what remains are fewer than kMostWorkgroups)
+    if ((int64_t)rows * Hq >= (1LL << 31) || B >= (1 << 24) || ((int64_t)rows * (Hq / Hkv) + 256LL * B) * Hkv >= 128 * kMostWorkgroups) return HG_ERR_UNSUPPORTED;
     return HG_OK;
 }
 // ... and those of keys in a cache.
@@ -136,7 +138,7 @@ void plan_tiles(RaggedArgs& a, int D, Room& room) {
     const double part = 8.0 * a.rows * a.Hq * (D + 1) / 4.5e6;
     int best = 1;
     double least = 1e300;
-    const int most = std::max(1, (int)std::min<int64_t>({64, a.max_len / 1024, (1LL << 30) / std::max<int64_t>(1, (int64_t)a.tiles_all * a.Hkv)}));      // (a grid of 32 bits)
+    const int most = std::max(1, (int)std::min<int64_t>({64, a.max_len / 1024, (kMostWorkgroups - (int64_t)a.row_wgs) / std::max<int64_t>(1, (int64_t)a.tiles_all * a.Hkv)}));
     for (int s = 1; s <= most; ++s) {
         const double n = 0.75 * wgs * s, us = std::max(1.0, ceil(n / 512.0)) * (stages / s * (n <= 256.0 ? 0.6 : 0.95) + 8.0) + (s > 1 ? part * s + (a.nsplit > 1 ? 1.0 : 6.0) : 0.0);
         if (us < (best == 1 ? 0.9 : 1.0) * least) { least = us; best = s; }      // (a tenth at least, or there is nothing to join)

@@ -95,3 +95,25 @@ def test_nothing_to_do_and_refusals():
     assert hb.hg_debug_ragged_plan(5, 5, 1, 4, 4, 32) == hb.HG_ERR_UNSUPPORTED
     assert hb.hg_debug_ragged_plan(5, -1, 1, 4, 4, 64) == hb.HG_ERR_INVALID_ARG
     assert hb.hg_debug_ragged_plan(5, (1 << 30) - 1, 1, 4, 4, 64, 1) == hb.HG_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("ws", [0, 512 << 20, 1 << 40])
+@pytest.mark.parametrize("heads", [(8, 1), (32, 8), (64, 8)])
+@pytest.mark.parametrize("B", [20000, 100000, 1000000])
+def test_many_sequences_of_which_few_bring_tokens(B, heads, ws):
+    """A launch has fewer than 2^32 threads: the places for tiles are as many as there are sequences, whatever the tokens."""
+    for rows in (1, 200, 4000):
+        for max_len in (515, 4096, 65536):
+            look(rows, max_len, B, *heads, 128, 200, ws=ws)
+            look(rows, max_len, B, *heads, 64, 1, ws=ws)
+            look(rows, max_len, B, *heads, 128, ws=ws)
+
+
+def test_the_most_sequences():
+    B = (1 << 20) - 1
+    while not isinstance(hb.hg_debug_ragged_plan(100, 4096, B, 8, 8, 64, 200), dict):
+        B -= 1
+    assert B > 1000000
+    look(100, 4096, B, 8, 8, 64, 200, ws=1 << 40)
+    look(100, 4096, B, 8, 8, 64, 1, ws=1 << 40)
+    look(100, 100, B, 8, 8, 64, ws=1 << 40)
