@@ -31,6 +31,7 @@ int check_sizes(int rows, int max_new, int B, int Hq, int Hkv, int D) {
     if (rows < 0 || max_new < 0 || B < 0 || Hq <= 0 || Hkv <= 0) return HG_ERR_INVALID_ARG;
     if (D != 64 && D != 128) return HG_ERR_UNSUPPORTED;
     if (Hq % Hkv != 0) return HG_ERR_UNSUPPORTED;
+    if ((int64_t)Hq * D > (1LL << 30)) return HG_ERR_UNSUPPORTED;      // (a head lies within 32 bits of its token's first)
     // (the last: with one range of keys to each, tiles and what remains are fewer than kMostWorkgroups)
     if ((int64_t)rows * Hq >= (1LL << 31) || B >= (1 << 24) || ((int64_t)rows * (Hq / Hkv) + 256LL * B) * Hkv >= 128 * kMostWorkgroups) return HG_ERR_UNSUPPORTED;
     return HG_OK;

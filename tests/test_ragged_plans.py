@@ -117,3 +117,12 @@ def test_the_most_sequences():
     look(100, 4096, B, 8, 8, 64, 200, ws=1 << 40)
     look(100, 4096, B, 8, 8, 64, 1, ws=1 << 40)
     look(100, 100, B, 8, 8, 64, ws=1 << 40)
+
+
+@pytest.mark.parametrize("max_new", [None, 1])
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_token_s_heads_lie_within_two_gibibytes(D, max_new):
+    """The kernels find a head's query in its token's row by 32-bit distances."""
+    most = (1 << 30) // D
+    look(1, 1, 1, most, 1, D, max_new)
+    assert hb.hg_debug_ragged_plan(1, 1, 1, most + 1, 1, D, max_new) == hb.HG_ERR_UNSUPPORTED
