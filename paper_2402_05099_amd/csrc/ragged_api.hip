@@ -249,7 +249,8 @@ int hg_kv_write_paged(hg_ctx* c, const void* Knew, const void* Vnew, int64_t str
     if (!codes && kv->kv_format != HG_KV_BF16) return HG_ERR_INVALID_ARG;
     if (codes && (!positive_scale(kv->k_scale) || !positive_scale(kv->v_scale))) return HG_ERR_INVALID_ARG;
     if (page_shift(kv->page_size) < 0 || kv->n_pages < 0) return HG_ERR_INVALID_ARG;
-    if ((int64_t)kv->n_pages * kv->page_size >= (1LL << 31) || (int64_t)rows * Hkv * D >= (1LL << 33)) return HG_ERR_UNSUPPORTED;
+    if ((int64_t)kv->n_pages * kv->page_size >= (1LL << 31) || (int64_t)rows * Hkv * D >= (1LL << 33) || (int64_t)Hkv * D >= (1LL << 31))
+        return HG_ERR_UNSUPPORTED;
     if (rows == 0) return HG_OK;
     if (!Knew || !Vnew || !slots || stride < (int64_t)Hkv * D || stride % 8 != 0 ||
         (reinterpret_cast<uintptr_t>(Knew) | reinterpret_cast<uintptr_t>(Vnew)) % 16 != 0) return HG_ERR_INVALID_ARG;

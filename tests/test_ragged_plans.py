@@ -126,3 +126,16 @@ def test_a_token_s_heads_lie_within_two_gibibytes(D, max_new):
     most = (1 << 30) // D
     look(1, 1, 1, most, 1, D, max_new)
     assert hb.hg_debug_ragged_plan(1, 1, 1, most + 1, 1, D, max_new) == hb.HG_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("codes", [0, 1])
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_of_a_write_lie_within_32_bits(D, codes):
+    """A pool without pages: the sizes are checked, and nothing would be written."""
+    import ctypes
+    some = ctypes.create_string_buffer(4096)      # (stands for a context and for tensors, which are not looked into)
+    at = ctypes.c_void_p((ctypes.addressof(some) + 255) // 256 * 256)
+    kv = hb.hg_paged_kv(at, at, at, 16, 1, 0, codes, 1.0, 1.0)
+    most = (1 << 31) // D
+    for Hkv, want in ((8, hb.HG_OK), (most - 1, hb.HG_OK), (most, hb.HG_ERR_UNSUPPORTED), (2 * most, hb.HG_ERR_UNSUPPORTED)):
+        assert hb.lib().hg_kv_write_paged(at, at, at, Hkv * D, at, 1, ctypes.byref(kv), Hkv, D) == want
