@@ -638,6 +638,8 @@ def hg_kv_write_paged(ctx: Context, Knew, Vnew, slots, kv: PagedKV) -> None:
     _want(slots, torch.int32, (T,), "slots")
     dt = torch.uint8 if kv.kv_format == HG_KV_E4M3 else torch.bfloat16
     _want(kv.K, dt, (kv.K.shape[0], Hkv, D), "paged K"); _want(kv.V, dt, kv.K.shape, "paged V")
+    if kv.K.shape[0] % kv.page_size:
+        raise ValueError("paged cache: K must be [n_pages * page_size, Hkv, D]")
     st = kv.c_struct()
     _check(lib().hg_kv_write_paged(ctx.h, _p(Knew), _p(Vnew), step, _p(slots), T, ctypes.byref(st), Hkv, D), "hg_kv_write_paged")
 
