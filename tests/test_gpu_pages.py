@@ -1,10 +1,12 @@
 """Block tables, slots and the write into a paged cache: refusals, the checks in Python, calls of many sequences, a list of free pages that is too short."""
 import numpy as np
+import numpy as np
 import pytest
 import torch
 
+import oracle.fp8 as fp8
 from paper_2402_05099_amd import binding as hb
-from test_gpu_ragged import DEV, context, i32
+from test_gpu_ragged import DEV, context, i32, rand, run_slots
 
 pytestmark = pytest.mark.gpu
 
@@ -23,4 +25,51 @@ def test_a_pool_that_ends_inside_a_page_is_refused():
             hb.hg_chunk_attn_paged(ctx, new, i32([0, 3]), kv, i32([3]), 3, 3, new.clone())
         torch.cuda.synchronize()
         assert torch.all(K == 5) and torch.all(V == 5)
+    ctx.close()
+
+
+@pytest.mark.parametrize("ps", [16, 128])
+@pytest.mark.parametrize("B", [1023, 1024, 1025, 2048, 2049, 2500])
+def test_slots_of_more_requests_than_a_pass_looks_at(B, ps):
+    print(f"slots: B {B}, page {ps}", flush=True)
+    g = np.random.default_rng(B)
+    lengths, counts = g.integers(0, 300, B).tolist(), g.integers(0, 12, B).tolist()
+    run_slots(lengths, counts, ps, 2 * B, 24)
+    run_slots(lengths, counts, ps, B // 40, 24)                          # the list ends in the first pass
+    run_slots(lengths, [0] * (B - 20) + [700] * 20, ps, 1000, 24)         # ... or in the last; tables too narrow for some
+    run_slots(lengths, counts, ps, 2 * B, 24, rows=sum(counts[:900]))    # tokens without a place in `slots`, in every pass but the first
+    run_slots(lengths, counts, ps, 2 * B, 24, rows=sum(counts) + 3000)
+    run_slots([0] * B, [1] + [0] * (B - 2) + [40], ps, 5, 24)
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_the_write_is_the_same_through_the_checks_in_python(D, codes, monkeypatch):
+    T, Hkv, pages, scales = 77, 3, 9, (0.01, 0.03)
+    g = torch.Generator().manual_seed(D)
+    x = rand(g, T, 2 * Hkv + 4, D, gain=3.0)
+    x[0, 1, :3] = torch.tensor([float("nan"), float("inf"), -float("inf")])
+    xd = x.to(DEV)
+    K, V = xd[:, 1:1 + Hkv], xd[:, 1 + Hkv:1 + 2 * Hkv]      # rows lie further apart than they are long
+    assert K.stride(0) > Hkv * D
+    slots = torch.randperm(pages * 16, generator=g)[:T].int()
+    slots[5], slots[9] = -1, pages * 16
+    ok = (slots >= 0) & (slots < pages * 16)
+    dt = torch.uint8 if codes else torch.bfloat16
+    want = []
+    for first, scale in ((1, scales[0]), (1 + Hkv, scales[1])):
+        new, pool = x[:, first:first + Hkv], torch.full((pages * 16, Hkv, D), 5, dtype=dt)
+        if codes:
+            new = torch.from_numpy(fp8.quantize(new.float().numpy(), np.float32(scale)))
+        pool[slots[ok].long()] = new[ok]
+        want.append(pool)
+    ctx = context()
+    for native in (hb.native(), hb._PythonOnly):
+        monkeypatch.setattr(hb, "_native", native)
+        pools = [torch.full((pages * 16, Hkv, D), 5, dtype=dt, device=DEV) for _ in range(2)]
+        kv = hb.PagedKV(K=pools[0], V=pools[1], page_table=i32([[0]]), page_size=16, kv_format=int(codes), k_scale=scales[0], v_scale=scales[1])
+        hb.hg_kv_write_paged(ctx, K, V, slots.to(DEV), kv)
+        for a, z in zip(want, pools):
+            a, z = (a, z.cpu()) if codes else (a.view(torch.int16), z.cpu().view(torch.int16))
+            assert torch.equal(a, z), native
     ctx.close()
