@@ -9,7 +9,7 @@ Every step is the same five calls, whatever the requests bring (whole prompts, t
   hg_prefix_attn       ... and over the system prompt, which is stored once: all tokens of all requests in one matrix
   hg_merge             the two parts into the exact result
 
-The system prompt itself is a prompt like any other: hg_prompt_attn.  Nothing is read back between the calls; the host looks at `pages_used` once a step, to know
+The system prompt itself is a prompt like any other: hg_prompt_attn.  Nothing is read back between the calls; the host looks once a step, to know
 how many pages of its free list are gone.
 
 usage: prompts_to_decode.py [--requests N] [--steps K] [--system P] [--heads 32/8] [--dim 128] [--codes]
@@ -58,17 +58,19 @@ class Server:
         Q, K, V = qkv[:, :self.Hq], qkv[:, self.Hq:self.Hq + self.Hkv], qkv[:, self.Hq + self.Hkv:]
         q_off, slots = torch.empty(self.B + 1, dtype=torch.int32, device=dev), torch.empty(T, dtype=torch.int32, device=dev)
         hb.hg_page_slots(self.ctx, self.lengths, counts, self.free, self.page_size, self.kv.page_table, q_off, slots, self.grown, self.used)
-        self.lengths, self.grown = self.grown, self.lengths
         hb.hg_kv_write_paged(self.ctx, K, V, slots, self.kv)
         O = [torch.empty(T, self.Hq, self.D, dtype=torch.float32, device=dev) for _ in range(2)]
         L = [torch.empty(T, self.Hq, dtype=torch.float32, device=dev) for _ in range(2)]
-        hb.hg_chunk_attn_paged(self.ctx, Q, q_off, self.kv, self.lengths, most, self.row_capacity, O[0], L[0])
+        hb.hg_chunk_attn_paged(self.ctx, Q, q_off, self.kv, self.grown, most, self.row_capacity, O[0], L[0])
         hb.hg_prefix_attn(self.ctx, Q.contiguous(), *self.system, O[1], L[1])
         out = torch.empty(T, self.Hq, self.D, dtype=torch.bfloat16, device=dev)
         hb.hg_merge(self.ctx, O, L, out)
-        taken = int(self.used)      # (the one look at the device)
+        # The one look at the device.  A step that wants more pages than there are is not taken: lengths and free pages stay, and what it has written lies behind the requests' rows
+        # or in pages that are still free, so it may be made again, with other counts or with more pages.
+        taken = int(self.used)
         if taken > self.free.numel():
             raise RuntimeError(f"{taken} pages are wanted, {self.free.numel()} are free: admit fewer requests, or take pages back first")
+        self.lengths, self.grown = self.grown, self.lengths
         self.free = self.free[taken:]
         return out
 
