@@ -10,7 +10,7 @@ Every step is the same five calls, whatever the requests bring (whole prompts, t
   hg_merge             the two parts into the exact result
 
 The system prompt itself is a prompt like any other: hg_prompt_attn.  Nothing is read back between the calls; the host looks once a step, to know
-how many pages of its free list are gone.
+how many pages of its free list are gone and whether every token had a place.
 
 usage: prompts_to_decode.py [--requests N] [--steps K] [--system P] [--heads 32/8] [--dim 128] [--codes]
 """
@@ -65,11 +65,13 @@ class Server:
         hb.hg_prefix_attn(self.ctx, Q.contiguous(), *self.system, O[1], L[1])
         out = torch.empty(T, self.Hq, self.D, dtype=torch.bfloat16, device=dev)
         hb.hg_merge(self.ctx, O, L, out)
-        # The one look at the device.  A step that wants more pages than there are is not taken: lengths and free pages stay, and what it has written lies behind the requests' rows
+        # The one look at the device.  A step in which some token has no place is not taken: lengths and free pages stay, and what it has written lies behind the requests' rows
         # or in pages that are still free, so it may be made again, with other counts or with more pages.
-        taken = int(self.used)
+        taken, unplaced = torch.cat([self.used, (self.lengths + counts - self.grown).sum(0, keepdim=True, dtype=torch.int32)]).tolist()
         if taken > self.free.numel():
             raise RuntimeError(f"{taken} pages are wanted, {self.free.numel()} are free: admit fewer requests, or take pages back first")
+        if unplaced:
+            raise RuntimeError(f"{unplaced} tokens lie past the {self.row_capacity} rows that a request may have")
         self.lengths, self.grown = self.grown, self.lengths
         self.free = self.free[taken:]
         return out

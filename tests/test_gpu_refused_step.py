@@ -14,7 +14,8 @@ sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(
 
 
 @pytest.mark.parametrize("codes", [False, True])
-@pytest.mark.parametrize("pages,capacity,refused,message", [(4, 128, [30, 50], "pages are wanted, 2 are free"), (4, 128, [0, 44], "3 pages are wanted, 2 are free")])
+@pytest.mark.parametrize("pages,capacity,refused,message", [(4, 128, [30, 50], "pages are wanted, 2 are free"), (4, 128, [0, 44], "3 pages are wanted, 2 are free"),
+                                                            (9, 32, [20, 28], "1 tokens lie past the 32 rows")])
 def test_a_refused_step_changes_nothing(pages, capacity, refused, message, codes):
     from prompts_to_decode import Server
     B, Hq, Hkv, D, P = 2, 4, 2, 64, 20
