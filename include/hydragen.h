@@ -311,7 +311,10 @@ int hg_kv_append_fp8(hg_ctx* ctx, const void* Knew, const void* Vnew, void* Ks8,
  * lengths[b] + counts[b] - 1 need beyond those in use are taken from free_pages (DEVICE int32[n_free]) in order, sequence after sequence, and entered.
  * Out: q_off, the running sum of counts; slots (DEVICE int32[rows]), the pool row of each packed token, -1 behind the last one; new_lengths =
  * lengths + counts; pages_used (DEVICE int32[1]), how many pages of the list were wanted.  More than n_free: the list was too short; the missing pages are entered as -1,
- * their tokens have slot -1, and new_lengths counts only rows with a place.  Rows from table_stride * page_size on have none either.  Nothing but
+ * their tokens have slot -1, and new_lengths counts only rows with a place.  Rows from table_stride * page_size on have none either.  A sequence with such tokens has
+ * new_lengths < lengths + counts, while q_off still counts all of them: hg_chunk_attn_paged, which takes a sequence's tokens to be its last rows, then gives ALL of its tokens the wrong
+ * rows, those with a place among them (the other sequences' results are right).  So whoever lets the calls follow each other without a look at pages_used, in a graph for instance, looks
+ * afterwards, and where it is above n_free makes the step again from the same lengths.  Nothing but
  * the new entries of page_table changes, so a call may be made again with a longer list.  new_lengths and q_off must not be lengths or counts.
  *
  * hg_kv_write_paged: pool row slots[i] = new row i, as bf16 or as codes (as in hg_kv_append_fp8); slots outside the pool are skipped.  No two tokens may

@@ -607,7 +607,8 @@ def hg_chunk_attn_paged(ctx: Context, Q, q_off, kv: PagedKV, lengths, max_new: i
 
 
 def hg_page_slots(ctx: Context, lengths, counts, free_pages, page_size: int, page_table, q_off, slots, new_lengths, pages_used) -> None:
-    """Places for counts[b] new tokens of every sequence: fills in page_table, q_off [B + 1], slots [T], new_lengths [B] and pages_used [1]."""
+    """Places for counts[b] new tokens of every sequence: fills in page_table, q_off [B + 1], slots [T], new_lengths [B] and pages_used [1].
+    pages_used above free_pages.numel(): the step has to be made again, from the same lengths, with more pages (see include/hydragen.h)."""
     rc = (_native or native()).slots(ctx, lengths, counts, free_pages, page_size, page_table, q_off, slots, new_lengths, pages_used)
     if rc is not None:
         if rc:

@@ -5,6 +5,8 @@ import pytest
 import torch
 
 import oracle.fp8 as fp8
+import ragged_plain as plain
+from parity import check
 from paper_2402_05099_amd import binding as hb
 from test_gpu_ragged import DEV, context, i32, rand, run_slots
 
@@ -72,4 +74,54 @@ def test_the_write_is_the_same_through_the_checks_in_python(D, codes, monkeypatc
         for a, z in zip(want, pools):
             a, z = (a, z.cpu()) if codes else (a.view(torch.int16), z.cpu().view(torch.int16))
             assert torch.equal(a, z), native
+    ctx.close()
+
+
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("codes", [False, True])
+def test_a_step_that_ran_out_of_pages_is_made_again(codes, captured):
+    """slots, write and attention one after another: sequences whose tokens all have a place are right, and made again with a longer list all are"""
+    g = torch.Generator().manual_seed(3)
+    Hq, Hkv, D, ps, stride, counts, scales = 8, 2, 128, 16, 8, [20, 0, 70, 1, 40], (0.0125, 0.0125)
+    T, B = sum(counts), len(counts)
+    off = np.concatenate([[0], np.cumsum(counts)])
+    x = rand(g, T, Hq + 2 * Hkv, D)
+    xd = x.to(DEV)
+    dt = torch.uint8 if codes else torch.bfloat16
+    kv = hb.PagedKV(K=torch.zeros(20 * ps, Hkv, D, dtype=dt, device=DEV), V=torch.zeros(20 * ps, Hkv, D, dtype=dt, device=DEV),
+                    page_table=torch.full((B, stride), -1, dtype=torch.int32, device=DEV), page_size=ps, kv_format=int(codes), k_scale=scales[0], v_scale=scales[1])
+    pages = torch.randperm(20, generator=g).int().to(DEV)
+    lengths, n = i32([0] * B), i32(counts)
+    q_off, slots, new, used = (torch.zeros(k, dtype=torch.int32, device=DEV) for k in (B + 1, T, B, 1))
+    O, L = torch.zeros(T, Hq, D, dtype=torch.bfloat16, device=DEV), torch.zeros(T, Hq, device=DEV)
+    stream = torch.cuda.Stream()
+    ctx = hb.Context(0, 16 << 20, stream=stream)
+
+    def step(free):
+        hb.hg_page_slots(ctx, lengths, n, free, ps, kv.page_table, q_off, slots, new, used)
+        hb.hg_kv_write_paged(ctx, xd[:, Hq:Hq + Hkv], xd[:, Hq + Hkv:], slots, kv)
+        hb.hg_chunk_attn_paged(ctx, xd[:, :Hq], q_off, kv, new, 70, stride * ps, O, L)
+
+    def stored(v):
+        return (v.float() / np.float32(0.0125)).clamp(-448, 448).to(torch.float8_e4m3fn).double() * float(np.float32(0.0125)) if codes else v.double()
+
+    K, V = ([stored(x[a:z, h:h + Hkv]) for a, z in zip(off, off[1:])] for h in (Hq, Hq + Hkv))
+    Oref, Lref = plain.attention(x[:, :Hq], off, K, V, counts)
+    for n_free, right in ((8, (0, 2, 3)), (11, (0, 2, 3, 4))):      # 2 + 5 + 1 + 3 pages are wanted
+        free = pages[:n_free].contiguous()
+        torch.cuda.synchronize()
+        if captured:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                step(free)
+            torch.cuda.synchronize()
+            for _ in range(3):
+                graph.replay()
+        else:
+            step(free)
+        torch.cuda.synchronize()
+        assert used.item() == 11 and lengths.tolist() == [0] * B and q_off.tolist() == off.tolist()
+        assert [b for b in range(B) if new[b] == counts[b] > 0] == list(right)
+        at = torch.cat([torch.arange(off[b], off[b + 1]) for b in right])
+        check(O.cpu()[at].double().numpy(), L.cpu()[at].double().numpy(), Oref[at].numpy(), Lref[at].numpy(), f"{n_free} pages", out_bf16=True)
     ctx.close()
