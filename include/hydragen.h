@@ -302,9 +302,12 @@ int hg_kv_append_fp8(hg_ctx* ctx, const void* Knew, const void* Vnew, void* Ks8,
  * hg_chunk_attn_paged: the n = q_off[b+1] - q_off[b] new tokens of a sequence are the last n of its lengths[b] rows in the paged cache, already written
  * there; token t attends to rows [0, lengths[b] - (n-1-t)).  n = 1 is decode; a token that sees no row gets O = 0, LSE = -inf.  Rows above
  * max_len are ignored (min(lengths[b], max_len) takes the place of lengths[b]); tokens of a sequence from max_new (a host upper bound) on are not computed.  The
- * pool may hold 2^31 - 1 rows, bf16 or codes (weights are rounded to bf16 over either); pool rows that no sequence owns may hold anything, NaN included.
- * In both, the key and value rows that a token does not see may hold anything, infinities and NaN included, its own sequence's later rows among them.
- * Both use the workspace, where there is one, to split long key ranges over more workgroups, and run without it.
+ * pool may hold 2^31 - 1 rows, bf16 or codes; pool rows that no sequence owns may hold anything, NaN included.
+ * In both, the key and value rows that a token does not see may hold anything, infinities and NaN included, its own sequence's later rows among them.  Softmax weights are rounded
+ * to bf16 before they are multiplied with the values, over bf16 rows and codes, for bf16 results and fp32 ones; scores, sums and LSE are fp32.
+ * Both use the workspace, where there is one, to split long key ranges over more workgroups, and run without it.  A range of keys that tiles of 128 rows have takes rows * Hq, one of
+ * single and drafted tokens at most B * Hkv * 64 rows of D + 1 floats; what does not fit makes for fewer ranges, which is slower and nothing else.  65 MiB hold all that
+ * calls of single and drafted tokens take, 384 MiB those of any call with contexts up to 131072 rows (hg_debug_ragged_plan tells for given sizes).
  *
  * hg_page_slots: places for the new tokens.  lengths, counts: DEVICE int32[B], rows that sequence b has in the cache and new tokens that it brings
  * (negative ones count as 0).  Row j of the sequence lives in page page_table[b * table_stride + j / page_size]; the pages that rows lengths[b] ..

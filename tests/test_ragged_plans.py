@@ -139,3 +139,16 @@ def test_rows_of_a_write_lie_within_32_bits(D, codes):
     most = (1 << 31) // D
     for Hkv, want in ((8, hb.HG_OK), (most - 1, hb.HG_OK), (most, hb.HG_ERR_UNSUPPORTED), (2 * most, hb.HG_ERR_UNSUPPORTED)):
         assert hb.lib().hg_kv_write_paged(at, at, at, Hkv * D, at, 1, ctypes.byref(kv), Hkv, D) == want
+
+
+def test_the_workspace_that_calls_take_at_most():
+    """the figures of include/hydragen.h"""
+    rng = random.Random(1)
+    for _ in range(30000):
+        Hq, Hkv = rng.choice(HEADS + [(128, 1), (128, 8), (96, 96)])
+        D, rows, max_len = rng.choice([64, 128]), min(400000, int(2 ** rng.uniform(0, 19))), min(131072, int(2 ** rng.uniform(0, 18)))
+        B, max_new = min(2048, 2 * rows, int(2 ** rng.uniform(0, 12))), rng.choice([None, int(2 ** rng.uniform(0, 13))])
+        p = look(rows, max_len, B, Hq, Hkv, D, max_new, ws=1 << 44)
+        few = 4 * (D + 1) * (p["nsplit"] * B * Hkv * p["few_most"] if p["nsplit"] > 1 else 0)
+        tiles = 4 * (D + 1) * (p["tile_nsplit"] * rows * Hq if p["tile_nsplit"] > 1 else 0)
+        assert few <= 65 << 20 and few + tiles <= 384 << 20
