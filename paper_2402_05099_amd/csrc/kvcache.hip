@@ -9,24 +9,6 @@
 
 namespace hg {
 
-// E4M3 codes of eight bf16 values divided by `scale`: the fp32 quotient (correctly rounded division), magnitudes
-// above 448 saturated, then the hardware's round-to-nearest-even conversion; NaN stays NaN.
-__device__ __forceinline__ uint2 quantize8(const uint4& r, float scale) {
-    const float f[8] = {bf16_lo(r.x), bf16_hi(r.x), bf16_lo(r.y), bf16_hi(r.y), bf16_lo(r.z), bf16_hi(r.z), bf16_lo(r.w), bf16_hi(r.w)};
-    float q[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float x = f[i] / scale;
-        q[i] = x != x ? x : fminf(fmaxf(x, -448.0f), 448.0f);
-    }
-    int lo = 0, hi = 0;
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], lo, false);
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], lo, true);
-    hi = __builtin_amdgcn_cvt_pk_fp8_f32(q[4], q[5], hi, false);
-    hi = __builtin_amdgcn_cvt_pk_fp8_f32(q[6], q[7], hi, true);
-    return make_uint2((unsigned)lo, (unsigned)hi);
-}
-
 // What bounds it: a chain of loads (arguments, length, page, each 0.4 - 0.8 us), so whatever does not depend on the length is requested
 // with it: a thread's first piece of the new rows, the sequence's offset.  One thread per 16-byte piece of K and V, up to
 // 1024: a workgroup must cover its sequence, for the length may only be advanced when all have read it.

@@ -135,25 +135,6 @@ hipError_t launch_page_slots(const SlotArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-namespace {
-// As in kvcache.hip: code = nearest E4M3 value to the fp32 quotient, ties to even, magnitudes above 448 saturated, NaN stays NaN.
-__device__ __forceinline__ uint2 codes8(const uint4& r, float scale) {
-    const float f[8] = {bf16_lo(r.x), bf16_hi(r.x), bf16_lo(r.y), bf16_hi(r.y), bf16_lo(r.z), bf16_hi(r.z), bf16_lo(r.w), bf16_hi(r.w)};
-    float q[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float x = f[i] / scale;
-        q[i] = x != x ? x : fminf(fmaxf(x, -448.0f), 448.0f);
-    }
-    int lo = 0, hi = 0;
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], lo, false);
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], lo, true);
-    hi = __builtin_amdgcn_cvt_pk_fp8_f32(q[4], q[5], hi, false);
-    hi = __builtin_amdgcn_cvt_pk_fp8_f32(q[6], q[7], hi, true);
-    return make_uint2((unsigned)lo, (unsigned)hi);
-}
-}
-
 // A thread takes a piece of eight elements of K and of V.  Bound by HBM: 16.8 thousand tokens, 40 heads of 128, as codes 91 us, 5.5 TB/s of 503 MB (a large copy
 // reaches 4.8); a decode step's rows 4.1 us, a launch.
 template <bool CODES>
@@ -169,8 +150,8 @@ __global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a) {
     if (slot < 0 || slot >= a.pool_rows) return;      // a token without a place
     const int64_t dst = (int64_t)slot * a.vec + c;
     if constexpr (CODES) {
-        reinterpret_cast<Piece*>(a.K)[dst] = codes8(k, a.k_scale);
-        reinterpret_cast<Piece*>(a.V)[dst] = codes8(v, a.v_scale);
+        reinterpret_cast<Piece*>(a.K)[dst] = quantize8(k, a.k_scale);
+        reinterpret_cast<Piece*>(a.V)[dst] = quantize8(v, a.v_scale);
     } else {
         reinterpret_cast<Piece*>(a.K)[dst] = k;
         reinterpret_cast<Piece*>(a.V)[dst] = v;
