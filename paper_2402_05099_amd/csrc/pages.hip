@@ -19,7 +19,7 @@ constexpr int kTokens = 1024;                    // tokens that a workgroup find
 // for itself, so that one launch does: 8 bytes per sequence out of L2 instead of a second launch.  A new page begins with a new token, so the
 // page's entry in the table is written where that token's slot is found.
 // What bounds it is latency: loads, two scans, the search of a token's sequence (ten looks into LDS), its page, 4.1 us for four sequences with 125 tokens, of which
-// the launch is most; 512 sequences with 131 thousand tokens 6.1 us, 0.6 MB in and out.  (256 sequences at a time, the pages of a sequence entered by the one
+// the launch is most (3.5 to 4.4 on different boxes); 512 sequences with 131 thousand tokens 6.1 us, 0.6 MB in and out.  (256 sequences at a time, the pages of a sequence entered by the one
 // workgroup that has it, 20.5 us.)
 __global__ __launch_bounds__(kThreads) void page_slots_kernel(SlotArgs a) {
     __shared__ int s_q0[kSeqs], s_len[kSeqs], s_have[kSeqs], s_first[kSeqs], s_sum[2][kThreads / 64];
@@ -135,8 +135,8 @@ hipError_t launch_page_slots(const SlotArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// A thread takes a piece of eight elements of K and of V.  Bound by HBM: 16.8 thousand tokens, 40 heads of 128, as codes 91 us, 5.5 TB/s of 503 MB (a large copy
-// reaches 4.8); a decode step's rows 4.1 us, a launch.
+// A thread takes a piece of eight elements of K and of V.  Bound by HBM: 16.8 thousand tokens, 40 heads of 128, as codes 91 us, 5.5 TB/s of 503 MB, two thirds of
+// them reads (an addition of the same bytes, two reads to a write, 85); a decode step's rows 4.1 us, a launch.
 template <bool CODES>
 __global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a) {
     using Piece = std::conditional_t<CODES, uint2, uint4>;

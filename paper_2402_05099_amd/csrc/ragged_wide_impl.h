@@ -19,7 +19,7 @@
 // What bounds it: the matrix pipes, and in calls of a millisecond the board's power.  One prompt of 8192 tokens, 64/8 heads: 0.95-1.01 ms, 1.10-1.16 PFLOP/s of what the mask leaves, at
 // 1.67 GHz with the matrix pipes 67 % busy (1417 cycles a stage and workgroup, 1024 of them products; without exponentials, or with half the LDS reads, 5 % less).  16 prompts of up to 2048
 // tokens, 40 heads 315-335 us (237 GFLOP; 43 % busy): a tile takes 7.6 us beside its 24 stages of 0.8, half of it until Q and the first rows are there.  45 prompts of up to 515 tokens,
-// 16/2 heads 46 us: the same 7 us beside seven stages.  2K tokens of two prompts over 8K to 16K keys, 64/8 heads 1.26-1.32 ms, 1.11-1.16 PFLOP/s.
+// 16/2 heads 44-47 us: the same 7 us beside seven stages.  2K tokens of two prompts over 8K to 16K keys, 64/8 heads 1.26-1.32 ms, 1.11-1.16 PFLOP/s.
 #include <algorithm>
 #include <type_traits>
 
