@@ -1,0 +1,469 @@
+"""A decode step over trees of drafted tokens: the operators that such a step needs beside slots and the write into the pages, through the public binding.
+
+Four operators; a case names one by `op`:
+  "masks"   which drafted tokens each one follows from, as bits, and how many, from their parents (hg_tree_masks)
+  "attn"    attention of every request's tree over its paged cache: all rows before the tree, and of the tree what the masks say (hg_tree_attn_paged)
+  "verify"  which drafted tokens stand, from the target's probabilities, the drafts' and given random numbers, and the token behind them (hg_tree_verify)
+  "keep"    the accepted tokens' rows moved together behind the context, in the pages of all layers, and the lengths after it (hg_tree_keep_paged)
+Fields: B requests; new_lo .. new_hi tokens of their trees; width: a token's parent is one of as many tokens before it (1: a chain); Hq, Hkv, D heads and head dimension;
+ctx_lo .. ctx_hi rows a request has in the cache before the step; page rows per page; cache "bf16" or "e4m3"; fused: Q is a view of the projection's output; V tokens of the
+vocabulary; probs "fp32" or "bf16"; drafts: the drafts' probabilities are given (else each drafted token counts as certain); layers of the cache; deep: tokens accepted at most.
+A case's lengths are evenly spread over their ranges, whatever the seed, which orders the requests and draws trees and values.
+"""
+import math
+
+import torch
+
+own = False
+
+K_SCALE, V_SCALE = 0.0125, 0.011      # one step of the codes: 448 times this covers N(0, 1) with room
+
+
+def _case(name, op, **more):
+    c = dict(name=name, op=op, B=1, new_lo=1, new_hi=1, width=1, Hq=1, Hkv=1, D=128, ctx_lo=0, ctx_hi=0, page=16, cache="bf16", fused=False,
+             V=0, probs="fp32", drafts=False, layers=1, deep=1)
+    c.update(more)
+    return c
+
+
+def listed():
+    return [
+        # four requests with a handful of drafted tokens: the smallest call, all latency
+        _case("masks_small", "masks", B=4, new_lo=1, new_hi=8, width=2),
+        # many requests, trees of up to 1024 tokens: long ancestries
+        _case("masks_large", "masks", B=64, new_lo=64, new_hi=1024, width=16),
+        # a small model's four short contexts: launches and a chain of loads
+        _case("attn_tiny", "attn", B=4, Hq=4, Hkv=4, D=64, ctx_lo=1, ctx_hi=64, new_lo=1, new_hi=8, width=3),
+        # a ragged batch with grouped heads, trees of odd sizes
+        _case("attn_ragged", "attn", B=45, Hq=16, Hkv=2, D=128, ctx_lo=1, ctx_hi=515, new_lo=1, new_hi=33, width=4, fused=True),
+        # a 13b-class layer without grouped heads, 8-bit cache
+        _case("attn_mha_codes", "attn", B=16, Hq=40, Hkv=40, D=128, ctx_lo=256, ctx_hi=4096, new_lo=8, new_hi=26, width=4, cache="e4m3"),
+        # trees of 64 tokens behind long documents
+        _case("attn_long", "attn", B=3, Hq=64, Hkv=8, D=128, ctx_lo=16384, ctx_hi=65536, new_lo=64, new_hi=64, width=8, page=64),
+        # a busy server: trees of all sizes behind contexts of all lengths
+        _case("attn_batch", "attn", B=48, Hq=32, Hkv=8, D=128, ctx_lo=512, ctx_hi=4096, new_lo=1, new_hi=96, width=6),
+        # chains of a few tokens over a small vocabulary
+        _case("verify_chain", "verify", B=4, new_lo=1, new_hi=6, width=1, V=1000, drafts=True),
+        # trees with the drafts' probabilities, a vocabulary of 32 thousand
+        _case("verify_trees", "verify", B=32, new_lo=1, new_hi=32, width=4, V=32000, drafts=True),
+        # few requests, larger trees of drafts taken as certain, the largest vocabulary
+        _case("verify_vocabulary", "verify", B=8, new_lo=64, new_hi=64, width=8, V=131072, probs="bf16"),
+        # one layer of a small batch
+        _case("keep_layer", "keep", B=4, Hkv=2, D=128, ctx_lo=16, ctx_hi=150, new_lo=1, new_hi=8, deep=4),
+        # all layers of a model at once
+        _case("keep_layers", "keep", B=64, Hkv=8, D=128, ctx_lo=1, ctx_hi=128, new_lo=8, new_hi=32, deep=8, layers=32),
+    ]
+
+
+# ---- what a case is made of --------------------------------------------------------------------------------------------------
+
+def _spread(n, lo, hi):
+    return [lo + (hi - lo) * i // max(n - 1, 1) if n > 1 else hi for i in range(n)]
+
+
+def _requests(c):
+    """[(rows in the cache, drafted tokens)] in a fixed order"""
+    B = c["B"]
+    ctx, new = _spread(B, c["ctx_lo"], c["ctx_hi"]), _spread(B, c["new_lo"], c["new_hi"])
+    step = next(s for s in range(max(1, int(B * 0.618)), 2 * B + 2) if math.gcd(s, B) == 1)      # long contexts with small and with large trees
+    return [(ctx[i * step % B], new[i]) for i in range(B)]
+
+
+def _pages(n, ps):
+    return -(-n // ps)
+
+
+def _kept(c, n):
+    """Tokens that stand of n, in a "keep" case: at most half of what follows the first, so that the places they move to are nobody's source"""
+    return min(n, 1 + min((n - 1) // 2, c["deep"] - 1)) if n else 0
+
+
+def work(case):
+    c, rq = case, _requests(case)
+    T, B, kv, es = sum(n for _, n in rq), c["B"], c["Hkv"] * c["D"], 1 if c["cache"] == "e4m3" else 2
+    if c["op"] == "masks":
+        return {"bytes": 4.0 * T * (2 + _pages(c["new_hi"], 32)) + 4 * (B + 1), "flops": 0.0}
+    if c["op"] == "verify":      # one row of each kind decides the next token; of the others a number for every drafted token
+        ep = 4 if c["probs"] == "fp32" else 2
+        some = sum(n > 0 for _, n in rq)
+        kinds = 2 if c["drafts"] else 1
+        return {"bytes": float(some * c["V"] * ep * kinds + T * (4 * 4 + ep * kinds) + 4 * (B + 1) + 12 * B), "flops": 0.0}
+    if c["op"] == "keep":
+        moved = sum(max(_kept(c, n) - 1, 0) for _, n in rq)
+        return {"bytes": 4.0 * moved * c["layers"] * kv * es + 4 * T + 16 * B, "flops": 0.0}
+    rows = sum(x + n for x, n in rq)
+    return {"bytes": T * c["Hq"] * (4.0 * c["D"] + 4) + 2.0 * es * rows * kv + 4.0 * T * _pages(c["new_hi"], 32)
+            + 4.0 * sum(_pages(x + n, c["page"]) for x, n in rq) + 8 * B,
+            "flops": 4.0 * c["D"] * c["Hq"] * sum(n * (x + 1) for x, n in rq)}      # (the context and the token itself; its ancestors are few)
+
+
+def draw(rng):
+    heads = [(4, 4), (8, 1), (16, 2), (32, 8), (40, 40), (64, 8), (12, 4), (10, 2)]
+
+    def log_int(lo, hi):
+        return min(hi, int(math.exp(rng.uniform(math.log(lo), math.log(hi + 1)))))
+
+    cost = lambda c: work(c)["bytes"] / 5e12 + work(c)["flops"] / 1e15  # noqa: E731
+    most = {op: max(cost(c) for c in listed() if c["op"] == op) for op in ("masks", "attn", "verify", "keep")}
+    while True:
+        op = rng.choice(["masks", "attn", "attn", "attn", "verify", "verify", "keep"])
+        Hq, Hkv = rng.choice(heads)
+        new_hi = log_int(1, 1024) if op == "masks" else log_int(1, 128)
+        ctx_hi = log_int(1, 65536) if op == "attn" else log_int(1, 512)
+        c = _case("", op, B=log_int(1, 256), new_lo=rng.randint(0, new_hi), new_hi=new_hi, width=rng.choice([1, 2, 3, 5, 8, 16]), Hq=Hq, Hkv=Hkv, D=rng.choice([64, 128, 128]),
+                  ctx_lo=log_int(1, ctx_hi), ctx_hi=ctx_hi, page=rng.choice([16, 32, 64, 128]), cache=rng.choice(["bf16", "bf16", "e4m3"]) if op in ("attn", "keep") else "bf16",
+                  fused=rng.random() < 0.5, V=log_int(100, 131072) if op == "verify" else 0, probs=rng.choice(["fp32", "bf16"]), drafts=rng.random() < 0.6,
+                  layers=log_int(1, 48) if op == "keep" else 1, deep=rng.randint(1, 12))
+        del c["name"]
+        rq = _requests(c)
+        T, rows, pool = sum(n for _, n in rq), sum(x + n for x, n in rq), sum(_pages(x + n, c["page"]) for x, n in rq) * c["page"]
+        fits = {"masks": c["B"] * new_hi * new_hi <= 7e7, "attn": c["B"] * Hq * new_hi * (ctx_hi + new_hi) <= 2e9 and c["B"] * (ctx_hi + new_hi) * Hkv * c["D"] < 1 << 30,
+                "verify": T * c["V"] <= 7e7, "keep": pool * Hkv * c["D"] * c["layers"] < 1 << 28}[op]
+        if T and cost(c) <= most[op] and fits and rows * Hkv * c["D"] < 1 << 29:
+            return c
+
+
+# ---- inputs ------------------------------------------------------------------------------------------------------------------
+
+def _values(g, *shape):
+    return torch.randn(*shape, generator=g, device="cuda", dtype=torch.float32).to(torch.bfloat16)
+
+
+def _i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def _parents(c, counts, g):
+    """Packed parents: that of token t is one of the `width` tokens before it; the first has none (-1)"""
+    T = sum(counts)
+    t = torch.cat([torch.arange(n) for n in counts]) if counts else torch.zeros(0, dtype=torch.int64)
+    back = (torch.rand(T, generator=g) * torch.clamp(t, max=c["width"])).long()
+    return torch.where(t > 0, t - 1 - back, -torch.ones_like(t)).to(torch.int32).cuda()
+
+
+def _pool(c, g, *shape):
+    if c["cache"] == "e4m3":
+        return (_values(g, *shape).float() / K_SCALE).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+    return _values(g, *shape)
+
+
+def _owner(off, T):
+    """(request, position in it) of each of T packed tokens"""
+    i = torch.arange(T, device=off.device)
+    b = torch.searchsorted(off.long(), i, right=True) - 1
+    return b, i - off.long()[b]
+
+
+def _padded(x, off, n, fill):
+    """Packed values as [B, n]"""
+    at = off[:-1].long()[:, None] + torch.arange(n, device=x.device)
+    here = at < off[1:].long()[:, None]
+    return torch.where(here, x[at.clamp(max=max(x.shape[0] - 1, 0))], torch.full((), fill, dtype=x.dtype, device=x.device))
+
+
+def _words(bits):
+    """Truth values [T, n] as int32 words, bit j % 32 of word j / 32"""
+    T, n = bits.shape
+    wide = torch.zeros(T, _pages(n, 32) * 32, dtype=torch.int64, device=bits.device)
+    wide[:, :n] = bits
+    w = (wide.view(T, -1, 32) << torch.arange(32, device=bits.device)).sum(-1)
+    return torch.where(w >= 1 << 31, w - (1 << 32), w).to(torch.int32)
+
+
+def _inputs(c, seed):
+    """Everything a case's operator reads, as tensors by name"""
+    g = torch.Generator(device="cuda").manual_seed(seed * 7919 + 23)
+    cpu = torch.Generator().manual_seed(seed)
+    rq = _requests(c)
+    rq = [rq[i] for i in torch.randperm(len(rq), generator=cpu).tolist()]
+    B, ps, ctx, new = c["B"], c["page"], [x for x, _ in rq], [n for _, n in rq]
+    off = [0]
+    for n in new:
+        off.append(off[-1] + n)
+    T = off[-1]
+    s = {"q_off": _i32(off), "T": T, "max_new": max(new), "max_len": max(x + n for x, n in rq)}
+    if c["op"] == "keep":
+        path, kept = torch.full((T,), -1, dtype=torch.int32), []
+        for b, n in enumerate(new):      # the first token, and others that lie behind all places they move to: a pass may be made again
+            a = _kept(c, n)
+            kept.append(a)
+            if a:
+                path[off[b]] = 0
+                path[off[b] + 1:off[b] + a] = (a + torch.randperm(n - a, generator=cpu)[:a - 1].sort().values).to(torch.int32)
+        s["path"], s["kept"] = path.cuda(), _i32(kept)
+    else:
+        s["parents"] = _parents(c, new, cpu)
+    if c["op"] == "masks":
+        return s
+    if c["op"] == "verify":
+        V = c["V"]
+        z = torch.randn(T, V, generator=g, device="cuda") * 6
+        target = torch.softmax(z, 1)
+        draft = torch.softmax(z + torch.randn(T, V, generator=g, device="cuda") * 1.5, 1)
+        b, t = _owner(s["q_off"], T)
+        row = s["q_off"].long()[b] + s["parents"].long().clamp(min=0)
+        s["tokens"] = torch.empty(T, dtype=torch.int32, device="cuda")
+        for i in range(0, T, 64):      # each token as its parent's drafts have it
+            s["tokens"][i:i + 64] = torch.multinomial(draft[row[i:i + 64]], 1, generator=g)[:, 0].to(torch.int32)
+        dtype = torch.float32 if c["probs"] == "fp32" else torch.bfloat16
+        s["target"], s["draft"] = target.to(dtype), draft.to(dtype) if c["drafts"] else None
+        s["u"], s["u_next"] = torch.rand(T, generator=g, device="cuda"), torch.rand(B, generator=g, device="cuda")
+        return s
+    # pages of the pool in a random order
+    need = [_pages(x + n, ps) for x, n in rq]
+    stride, n_pages = max(need), sum(need) + 3
+    order = torch.randperm(n_pages, generator=cpu).to(torch.int32)
+    table = torch.full((B, stride), -1, dtype=torch.int32)
+    at = 0
+    for b, w in enumerate(need):
+        table[b, :w] = order[at:at + w]
+        at += w
+    s["table"], s["len"] = table.cuda(), _i32([x + n for x, n in rq])
+    lead = (c["layers"],) if c["op"] == "keep" else ()
+    s["Kp"], s["Vp"] = (_pool(c, g, *lead, n_pages * ps, c["Hkv"], c["D"]) for _ in range(2))
+    if c["op"] == "attn":
+        x = _values(g, T, c["Hq"] + 2 * c["Hkv"] if c["fused"] else c["Hq"], c["D"])
+        s["Q"] = x[:, :c["Hq"]]
+        s["masks"] = _plain_masks(s)["masks"]
+    return s
+
+
+def prepare(case, seed):
+    """The step's tensors and the results', as a serving program keeps them"""
+    s = _inputs(case, seed)
+    s["case"] = case
+    T, B = s["T"], case["B"]
+    if case["op"] == "attn":
+        s["O"] = torch.empty(T, case["Hq"], case["D"], dtype=torch.bfloat16, device="cuda")
+        s["LSE"] = torch.empty(T, case["Hq"], dtype=torch.float32, device="cuda")
+    ints = {"masks": {"masks": (T, _pages(s["max_new"], 32)), "depth": (T,)}, "verify": {"path": (T,), "kept": (B,), "next": (B,)}, "keep": {"grown": (B,)}}
+    for name, shape in ints.get(case["op"], {}).items():
+        s[name] = torch.empty(shape, dtype=torch.int32, device="cuda")
+    return s
+
+
+# ---- the plain forms ---------------------------------------------------------------------------------------------------------
+
+def _plain_masks(s):
+    """Ancestors by doubling: those of a token so far, and of the token that many steps up"""
+    n, T = s["max_new"], s["T"]
+    up = _padded(s["parents"], s["q_off"], n, -1).long()
+    follows = torch.eye(n, dtype=torch.bool, device=up.device).expand(up.shape[0], n, n).clone()
+    at = torch.arange(n, device=up.device)
+    up = torch.where((up >= 0) & (up < at), up, n)
+    for _ in range(max(n - 1, 1).bit_length()):
+        more = torch.gather(torch.cat([follows, torch.zeros_like(follows[:, :1])], 1), 1, up[:, :, None].expand(-1, -1, n))
+        follows = follows | more
+        up = torch.gather(torch.cat([up, torch.full_like(up[:, :1], n)], 1), 1, up)
+    b, t = _owner(s["q_off"], T)
+    follows = follows[b, t]
+    return {"masks": _words(follows), "depth": (follows.sum(1) - 1).to(torch.int32)}
+
+
+def _cache_rows(s, c, dtype):
+    """K and V of every request's rows, padded to the longest: [B, longest, Hkv, D]"""
+    j = torch.arange(s["max_len"], device="cuda")
+    rows = s["table"][:, j // c["page"]].long().clamp(min=0) * c["page"] + j % c["page"]
+    here = (j < s["len"][:, None])[:, :, None, None]
+    out = []
+    for pool, scale in ((s["Kp"], K_SCALE), (s["Vp"], V_SCALE)):
+        x = pool[rows]
+        x = x.view(torch.float8_e4m3fn).to(dtype) * scale if c["cache"] == "e4m3" else x.to(dtype)
+        out.append(torch.where(here, x, torch.zeros((), dtype=dtype, device="cuda")))
+    return out
+
+
+def _plain_attn(s, c):
+    k, v = _cache_rows(s, c, torch.float32)
+    B, L, Hkv, D = k.shape
+    T, Hq, G, n = s["T"], c["Hq"], c["Hq"] // c["Hkv"], s["max_new"]
+    at = (s["q_off"][:-1].long()[:, None] + torch.arange(n, device="cuda")).clamp(max=T - 1)
+    q = s["Q"].float()[at].view(B, n, Hkv, G, D).permute(0, 2, 3, 1, 4).reshape(B * Hkv, G * n, D)
+    sc = torch.matmul(q, k.permute(0, 2, 3, 1).reshape(B * Hkv, D, L)).view(B, Hkv, G, n, L).mul_(1.0 / math.sqrt(D))
+    j = torch.arange(L, device="cuda") - (s["len"] - (s["q_off"][1:] - s["q_off"][:-1]))[:, None]      # [B, L]: place in the tree, below 0 before it
+    words = s["masks"][at]
+    word = torch.gather(words, 2, (j // 32).clamp(0, words.shape[2] - 1)[:, None, :].expand(B, n, L))
+    seen = (j < 0)[:, None, :] | ((word >> (j % 32)[:, None, :]) & 1).bool()
+    seen &= (torch.arange(L, device="cuda") < s["len"][:, None])[:, None, :]
+    sc.masked_fill_(~seen[:, None, None], -math.inf)
+    m = sc.amax(-1, keepdim=True)
+    p = sc.sub_(m).exp_()
+    l = p.sum(-1, keepdim=True)
+    o = torch.matmul(p.view(B * Hkv, G * n, L), v.permute(0, 2, 1, 3).reshape(B * Hkv, L, D)).view(B, Hkv, G, n, D) / l
+    lse = (m + l.log())[..., 0]
+    b, t = _owner(s["q_off"], T)
+    return {"O": o.permute(0, 3, 1, 2, 4).reshape(B, n, Hq, D)[b, t].to(torch.bfloat16), "LSE": lse.permute(0, 3, 1, 2).reshape(B, n, Hq)[b, t]}
+
+
+def _plain_verify(s, c):
+    """Token after token: one whose parent is the last that stands is looked at.  With drafts, what is left of the target's weights after rejections is
+    max(0, p - take q), `left` in sum; without, p but for the rejected tokens.  In 64 bits: a sum over the vocabulary next to a random number."""
+    off, n, B = s["q_off"], s["max_new"], c["B"]
+    V, dev = c["V"], off.device
+    up, tok, u = _padded(s["parents"], off, n, -1).long(), _padded(s["tokens"], off, n, 0).long(), _padded(s["u"], off, n, 0.0).double()
+    first, count = off[:-1].long().clamp(max=s["T"] - 1), (off[1:] - off[:-1]).long()
+    cur = torch.zeros(B, dtype=torch.int64, device=dev)
+    take, left = torch.zeros(B, dtype=torch.float64, device=dev), torch.ones(B, dtype=torch.float64, device=dev)
+    path = torch.full((B, n + 1), -1, dtype=torch.int64, device=dev)
+    path[:, 0] = torch.where(count > 0, 0, -1)
+    kept = (count > 0).long()
+    refused = torch.zeros(B, n, dtype=torch.bool, device=dev)
+    for t in range(1, n):
+        live = (t < count) & (up[:, t] == cur)
+        row, x = first + cur, tok[:, t]
+        p = s["target"][row, x].double()
+        if c["drafts"]:
+            q = s["draft"][row, x].double()
+            yes = live & (u[:, t] * q * left < (p - take * q).clamp(min=0))
+        else:
+            p = torch.where((refused & (tok == x[:, None])).any(1), torch.zeros_like(p), p)
+            yes = live & (u[:, t] * left < p)
+        no = live & ~yes
+        if c["drafts"]:
+            take = torch.where(no, take + left, take)
+            rest = (s["target"][row].double() - take[:, None] * s["draft"][row].double()).clamp(min=0).sum(1)
+        else:
+            rest = left - p
+            refused[:, t] = no
+            refused = refused & ~yes[:, None]
+        left = torch.where(yes, torch.ones_like(left), torch.where(no, rest, left))
+        take = torch.where(yes, torch.zeros_like(take), take)
+        cur = torch.where(yes, t, cur)
+        path.scatter_(1, kept[:, None], torch.where(yes, t, path.gather(1, kept[:, None])[:, 0])[:, None])
+        kept = kept + yes
+    w = s["target"][first + cur].double()
+    if c["drafts"]:
+        lower = (w - take[:, None] * s["draft"][first + cur].double()).clamp(min=0)
+    else:
+        lower = torch.cat([w, torch.zeros_like(w[:, :1])], 1).scatter_(1, torch.where(refused, tok, V), 0.0)[:, :V]
+    w = torch.where(lower.sum(1, keepdim=True) > 0, lower, w)
+    reached = (w > 0) & (torch.cumsum(w, 1) > (s["u_next"].double() * w.sum(1))[:, None])
+    y = torch.arange(V, device=dev)
+    nxt = torch.where(reached, y, V).amin(1)
+    nxt = torch.where(nxt == V, torch.where(w > 0, y, -1).amax(1), nxt)
+    b, t = _owner(off, s["T"])
+    return {"path": path[b, t].to(torch.int32), "kept": kept.to(torch.int32), "next": torch.where(count > 0, nxt, -1).to(torch.int32)}
+
+
+def _moves(s, c):
+    """(pool rows, pool rows they move to) of the accepted tokens"""
+    b, i = _owner(s["q_off"], s["T"])
+    b, i, t = (x[i < s["kept"][b]] for x in (b, i, s["path"].long()))
+    before = (s["len"] - (s["q_off"][1:] - s["q_off"][:-1])).long()[b]
+    return [s["table"][b, j // c["page"]].long() * c["page"] + j % c["page"] for j in (before + t, before + i)]
+
+
+def _plain_keep(s, c):
+    src, dst = _moves(s, c)
+    rows = torch.arange(s["Kp"].shape[1], device="cuda")
+    rows[dst] = src
+    return {"K": s["Kp"][:, rows], "V": s["Vp"][:, rows], "lengths": s["len"] - (s["q_off"][1:] - s["q_off"][:-1]) + s["kept"]}
+
+
+def _as_values(out, c):
+    return {k: v.view(torch.float8_e4m3fn) if k in "KV" and c["cache"] == "e4m3" else v for k, v in out.items()}
+
+
+def run(s):
+    c = s["case"]
+    if own:
+        return _run_own(s, c)
+    if c["op"] == "masks":
+        return _plain_masks(s)
+    if c["op"] == "attn":
+        return _plain_attn(s, c)
+    if c["op"] == "verify":
+        return _plain_verify(s, c)
+    return _as_values(_plain_keep(s, c), c)
+
+
+_handle = None
+
+
+def _library():
+    """The binding and the program's one context, with a workspace that fits every case"""
+    global _handle
+    from paper_2402_05099_amd import binding as hb
+    if _handle is None:
+        _handle = hb.Context(0, 512 << 20)
+    return hb, _handle
+
+
+def _run_own(s, c):
+    hb, h = _library()
+    if "Kp" in s and "kv" not in s:      # the cache as a program keeps it: an object for each layer
+        pools = zip(s["Kp"], s["Vp"]) if c["op"] == "keep" else [(s["Kp"], s["Vp"])]
+        s["kv"] = [hb.PagedKV(K=k, V=v, page_table=s["table"], page_size=c["page"], kv_format=hb.HG_KV_E4M3 if c["cache"] == "e4m3" else hb.HG_KV_BF16,
+                              k_scale=K_SCALE, v_scale=V_SCALE) for k, v in pools]
+    if c["op"] == "masks":
+        hb.hg_tree_masks(h, s["parents"], s["q_off"], s["max_new"], s["masks"], s["depth"])
+        return {"masks": s["masks"], "depth": s["depth"]}
+    if c["op"] == "attn":
+        hb.hg_tree_attn_paged(h, s["Q"], s["q_off"], s["masks"], s["kv"][0], s["len"], s["max_new"], s["max_len"], s["O"], s["LSE"])
+        return {"O": s["O"], "LSE": s["LSE"]}
+    if c["op"] == "verify":
+        hb.hg_tree_verify(h, s["tokens"], s["parents"], s["q_off"], s["max_new"], s["target"], s["draft"], s["u"], s["u_next"], s["path"], s["kept"], s["next"])
+        return {"path": s["path"], "kept": s["kept"], "next": s["next"]}
+    hb.hg_tree_keep_paged(h, s["kv"], s["q_off"], s["path"], s["kept"], s["len"], s["max_new"], s["grown"])
+    return _as_values({"K": s["Kp"], "V": s["Vp"], "lengths": s["grown"]}, c)
+
+
+# ---- the definitions in 64 bits ----------------------------------------------------------------------------------------------
+
+def _e4m3_values():
+    """The 256 values of the format: sign, 4 exponent bits with bias 7, 3 mantissa bits, NaN where all of them are set"""
+    v = []
+    for code in range(256):
+        e, f = (code >> 3) & 15, code & 7
+        x = math.nan if (code & 127) == 127 else f * 2.0 ** -9 if e == 0 else (8 + f) * 2.0 ** (e - 10)
+        v.append(-x if code & 128 else x)
+    return torch.tensor(v, dtype=torch.float64, device="cuda")
+
+
+def exact(case, seed):
+    if case["op"] in ("masks", "verify"):
+        return None      # whole numbers
+    s, c = _inputs(case, seed), case
+    val, off, table, lens = _e4m3_values(), s["q_off"].tolist(), s["table"].tolist(), s["len"].tolist()
+    if c["op"] == "keep":
+        path, kept, out = s["path"].tolist(), s["kept"].tolist(), {"lengths": None}
+        place = lambda b, j: table[b][j // c["page"]] * c["page"] + j % c["page"]  # noqa: E731
+        for name in ("K", "V"):
+            pool = s[name + "p"]
+            if c["cache"] == "e4m3":
+                pool = val.float()[pool.long()]      # (codes are fp32 numbers, and there are many)
+            moved = pool.clone()
+            for b in range(c["B"]):
+                before = lens[b] - (off[b + 1] - off[b])
+                for i in range(1, kept[b]):
+                    moved[:, place(b, before + i)] = pool[:, place(b, before + path[off[b] + i])]
+            out[name] = moved
+        return out
+    T, Hq, Hkv, D = s["T"], c["Hq"], c["Hkv"], c["D"]
+    O = torch.empty(T, Hq, D, dtype=torch.float64, device="cuda")
+    LSE = torch.empty(T, Hq, dtype=torch.float64, device="cuda")
+    parents = s["parents"].tolist()
+    for b in range(c["B"]):
+        n, rows = off[b + 1] - off[b], lens[b]
+        if n == 0:
+            continue
+        unseen = torch.ones(n, rows, dtype=torch.bool)
+        for t in range(n):
+            unseen[t, :rows - n] = False
+            a = t
+            while a >= 0:
+                unseen[t, rows - n + a] = False
+                a = parents[off[b] + a]
+        unseen = unseen.cuda()
+        at = torch.cat([torch.arange(c["page"], device="cuda") + p * c["page"] for p in table[b] if p >= 0])[:rows]
+        for kvh in range(Hkv):
+            if c["cache"] == "e4m3":
+                k, v = val[s["Kp"][at, kvh].long()] * K_SCALE, val[s["Vp"][at, kvh].long()] * V_SCALE
+            else:
+                k, v = s["Kp"][at, kvh].double(), s["Vp"][at, kvh].double()
+            for h in range(kvh * (Hq // Hkv), (kvh + 1) * (Hq // Hkv)):
+                z = s["Q"][off[b]:off[b + 1], h].double() @ k.T.contiguous() / math.sqrt(D)
+                z = z.masked_fill(unseen, -math.inf)
+                LSE[off[b]:off[b + 1], h] = torch.logsumexp(z, 1)
+                O[off[b]:off[b + 1], h] = torch.softmax(z, 1) @ v
+    return {"O": O, "LSE": LSE}
