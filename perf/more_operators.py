@@ -199,7 +199,7 @@ def _inputs(c, seed):
         V = c["V"]
         z = torch.randn(T, V, generator=g, device="cuda") * 6
         target = torch.softmax(z, 1)
-        draft = torch.softmax(z + torch.randn(T, V, generator=g, device="cuda") * 1.5, 1)
+        draft = torch.softmax(z + torch.randn(T, V, generator=g, device="cuda") * 0.8, 1)
         b, t = _owner(s["q_off"], T)
         row = s["q_off"].long()[b] + s["parents"].long().clamp(min=0)
         s["tokens"] = torch.empty(T, dtype=torch.int32, device="cuda")
