@@ -73,9 +73,10 @@ extern "C" {
 typedef struct hg_ctx hg_ctx;
 
 enum { HG_OK = 0, HG_ERR_INVALID_ARG = 1, HG_ERR_UNSUPPORTED = 2, HG_ERR_WORKSPACE = 3, HG_ERR_HIP = 4, HG_ERR_STATIC_LIMIT = 5 };
-enum { HG_F32 = 0, HG_BF16 = 1 };
+enum { HG_F32 = 0, HG_BF16 = 1, HG_TOKENS = 2 }; /* HG_TOKENS: of hg_tree_verify alone */
 enum { HG_KV_BF16 = 0, HG_KV_E4M3 = 1 }; /* element format of a paged suffix cache (hg_paged_kv.kv_format) */
 enum { HG_MAX_LEVELS = 4, HG_MAX_PARTS = 64 };
+enum { HG_MAX_TREE = 1024, HG_MAX_LAYERS = 128 }; /* drafted tokens of a sequence, and layers of a cache, in one call */
 enum { HG_STATIC_SCRATCH_BYTES = 67108864 }; /* 64 MiB: partial-result memory of hg_hydragen_attn_static */
 
 /* Tunables for hg_set_option (0 = library default). */
@@ -334,6 +335,49 @@ int hg_page_slots(hg_ctx* ctx, const int32_t* lengths, const int32_t* counts, co
                   int32_t* q_off, int32_t* slots, int32_t* new_lengths, int32_t* pages_used);
 int hg_kv_write_paged(hg_ctx* ctx, const void* Knew, const void* Vnew, int64_t stride, const int32_t* slots, int rows,
                       const hg_paged_kv* kv, int Hkv, int D);
+
+/*
+ * A decode step over trees of drafted tokens (Sec. 2.2's step, of which App. B's num_queries > 1 is the form for one chain): a drafting model proposes several continuations of every sequence,
+ * the target model looks at all of them at once, and what it would have said itself stands.  Tokens are packed as above (q_off, rows).  The n tokens of a sequence are its tree: token 0 is the one
+ * that the last step ended with, whose row the cache does not have yet; every other token t has a parent, parents[t] in [0, t) counted within the sequence, after which it would come.  A token whose
+ * parents[t] is outside [0, t) has none.  A step: hg_page_slots and hg_kv_write_paged give all of the tree rows behind the context; hg_tree_masks; hg_tree_attn_paged in every layer;
+ * hg_tree_verify; hg_tree_keep_paged, whose new lengths are those of the next step.  Pages behind them are free again (the caller's business, as ever).
+ *
+ * hg_tree_masks: what each token follows from.  Bit j % 32 of masks[i * mask_words + j / 32], i = q_off[b] + t: 1 where j is t or one of its ancestors; depth[i] (may be NULL): how
+ * many ancestors it has, so its position is that of the context's end + depth.  mask_words >= ceil(min(max_new, rows) / 32); words behind the tokens' are 0.  max_new, a host upper bound on the tokens of a
+ * sequence, is at most HG_MAX_TREE; tokens from max_new on are left as they are, and have no bit.
+ *
+ * hg_tree_attn_paged: hg_chunk_attn_paged but for what the n new tokens, the last n of the sequence's lengths[b] rows, see of each other: token t sees all rows [0, lengths[b] - n) and of its sequence's n
+ * rows those with a bit in its row of masks (DEVICE, mask_words words to a row, bits as above, from hg_tree_masks or any others: bits from n on count for nothing, tokens without a bit are not
+ * seen, and a token without a row to see has O = 0, LSE = -inf).  max_new has no limit here.  Everything else is as there: strides, bounds, the workspace, what rows that are not seen may hold.
+ *
+ * hg_tree_verify: which tokens stand, and the token behind them, so that what comes out is distributed as if the target had been asked token by token (for drafts that are drawn from `draft`, or that are
+ * told apart among siblings).  Token 0 stands.  The others are looked at in order, each if its parent is the last one that stands; with x the token (tokens[i]), p and q row
+ * `parent` of target and draft (DEVICE [rows, V] of p_dtype, HG_F32 or HG_BF16, row distances in elements: row i has the probabilities of what comes behind token i, the target's, and
+ * those that its children were drawn with), u[i] a random number from [0, 1):
+ *   with draft: p_0 = p; x stands if u q(x) < p_k(x), k being the siblings refused before; a refusal leaves p_k+1 = max(0, p_k - q) / its sum.
+ *   draft NULL (each drafted token counts as certain): x stands if u < p_k(x); a refusal leaves p_k+1 = p_k without x, / its sum.
+ * next_tokens[b] is drawn from the p_k that is left at the last token that stands: the smallest y with p_k(0) + .. + p_k(y) > u_next[b] (times the sum as it is: rows need not sum to one exactly).
+ * Sums are taken in 64 bits.  The kernels use p_k = max(0, p - c_k q) / S_k, c_0 = 0, S_0 = 1, c_k+1 = c_k + S_k, S_k+1 = sum of max(0, p - c_k+1 q), which is the same.  Entries that are not positive finite
+ * numbers count as 0, so do tokens outside [0, V).  Where nothing is left (rounding), the draw is from p; where p has nothing either, next_tokens[b] is -1.
+ *   p_dtype = HG_TOKENS (greedy decoding): target is int32 [rows], what the target says behind each token; a token stands if it is what its parent's row says, next_tokens[b] is what the last
+ * one's says.  V, draft, u and u_next are not looked at.
+ * Out: accepted[b], how many stand (0 for a sequence without tokens, whose next_tokens is -1); path, DEVICE int32[rows]: path[q_off[b] + i], i < accepted[b], the i-th that stands (ascending, the first 0),
+ * -1 behind them.  max_new at most HG_MAX_TREE; tokens from max_new on are not looked at, their places in path are left as they are.  Outputs must not be inputs.
+ *
+ * hg_tree_keep_paged: the tokens that stand become part of the context: row lengths[b] - n + i = row lengths[b] - n + path[q_off[b] + i] for i < accepted[b], K and V, in the pages of n_layers (at most
+ * HG_MAX_LAYERS) caches that differ in K and V only, and new_lengths[b] = max(lengths[b] - n + accepted[b], 0).  accepted above n counts as n; a path that is not ascending gives wrong rows; rows that the table has no place
+ * for, or whose page is not in the pool, are not moved, nor is anything from or to a place outside the sequence's n rows.  new_lengths must not be any of the inputs; no pool may be there twice.
+ */
+int hg_tree_masks(hg_ctx* ctx, const int32_t* parents, const int32_t* q_off, int rows, int max_new, int B, uint32_t* masks, int mask_words, int32_t* depth);
+int hg_tree_attn_paged(hg_ctx* ctx, const void* Q, int64_t q_stride, const int32_t* q_off, int rows, const uint32_t* masks, int mask_words,
+                       const hg_paged_kv* kv, const int32_t* lengths, int max_new, int max_len,
+                       int B, int Hq, int Hkv, int D, float scale, void* O, int o_dtype, float* LSE);
+int hg_tree_verify(hg_ctx* ctx, const int32_t* tokens, const int32_t* parents, const int32_t* q_off, int rows, int max_new, int B, int V,
+                   const void* target, int64_t target_stride, const void* draft, int64_t draft_stride, int p_dtype,
+                   const float* u, const float* u_next, int32_t* path, int32_t* accepted, int32_t* next_tokens);
+int hg_tree_keep_paged(hg_ctx* ctx, int n_layers, const hg_paged_kv* kv, const int32_t* q_off, int rows, const int32_t* path, const int32_t* accepted,
+                       const int32_t* lengths, int max_new, int B, int Hkv, int D, int32_t* new_lengths);
 
 /*
  * Non-decomposed comparison (the behaviour Sec. 1 and Sec. 2.3 attribute to per-sequence decode kernels):

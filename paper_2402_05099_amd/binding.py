@@ -1,5 +1,5 @@
 """Thin ctypes binding of libhydragen.so: same names as include/hydragen.h, argument marshalling only.  The calls of a decode step and those before it
-(fused attention, cache update, prompts and chunks, slots and the write into the pages) are marshalled by a native extension (csrc/marshal.cpp); what it does not take comes
+(fused attention, cache update, prompts and chunks, slots and the write into the pages, drafted trees) are marshalled by a native extension (csrc/marshal.cpp); what it does not take comes
 back here, to the same checks in Python.
 
 PyTorch is used for device memory and streams; every step of the attention path runs in the HIP kernels of
@@ -19,8 +19,9 @@ import torch
 
 HG_OK, HG_ERR_INVALID_ARG, HG_ERR_UNSUPPORTED, HG_ERR_WORKSPACE, HG_ERR_HIP, HG_ERR_STATIC_LIMIT = 0, 1, 2, 3, 4, 5
 HG_STATIC_SCRATCH_BYTES = 64 << 20
-HG_F32, HG_BF16 = 0, 1
+HG_F32, HG_BF16, HG_TOKENS = 0, 1, 2
 HG_MAX_LEVELS, HG_MAX_PARTS = 4, 64
+HG_MAX_TREE, HG_MAX_LAYERS = 1024, 128
 HG_OPT_PREFIX_SPLITS, HG_OPT_SUFFIX_CHUNK, HG_OPT_OVERLAP, HG_OPT_NAIVE_CHUNK, HG_OPT_STAGE_TIMING, HG_OPT_PREFIX_KERNEL = 1, 2, 3, 4, 5, 6
 HG_OPT_WIDE_SLOTS = 7
 HG_OPT_NUM_QUERIES = 8
@@ -41,6 +42,7 @@ EXPORTS = (
     "hg_strerror", "hg_suffix_attn_paged", "hg_hydragen_attn_paged", "hg_kv_append", "hg_kv_append_paged",
     "hg_debug_wide_plan", "hg_debug_wide_ranges", "hg_debug_wide_team", "hg_debug_item_runs", "hg_debug_suffix_plan", "hg_debug_fused_plan", "hg_debug_single_work", "hg_debug_ragged_plan", "hg_suffix_attn_fp8", "hg_hydragen_attn_fp8", "hg_kv_append_fp8",
     "hg_prompt_attn", "hg_chunk_attn_paged", "hg_page_slots", "hg_kv_write_paged",
+    "hg_tree_masks", "hg_tree_attn_paged", "hg_tree_verify", "hg_tree_keep_paged",
     "hg_hydragen_attn_static", "hg_debug_mfma_loop", "hg_debug_stream_read", "hg_debug_xcd_of_workgroups",
 )
 
@@ -128,6 +130,14 @@ def lib() -> ctypes.CDLL:
         L.hg_page_slots.restype = ci
         L.hg_kv_write_paged.argtypes = [vp, vp, vp, i64, vp, ci, ctypes.POINTER(hg_paged_kv), ci, ci]
         L.hg_kv_write_paged.restype = ci
+        L.hg_tree_masks.argtypes = [vp, vp, vp, ci, ci, ci, vp, ci, vp]
+        L.hg_tree_masks.restype = ci
+        L.hg_tree_attn_paged.argtypes = [vp, vp, i64, vp, ci, vp, ci, ctypes.POINTER(hg_paged_kv), vp, ci, ci, ci, ci, ci, ci, cf, vp, ci, vp]
+        L.hg_tree_attn_paged.restype = ci
+        L.hg_tree_verify.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, vp, i64, vp, i64, ci, vp, vp, vp, vp, vp]
+        L.hg_tree_verify.restype = ci
+        L.hg_tree_keep_paged.argtypes = [vp, ci, ctypes.POINTER(hg_paged_kv), vp, ci, vp, vp, vp, ci, ci, ci, ci, vp]
+        L.hg_tree_keep_paged.restype = ci
         L.hg_debug_wide_plan.argtypes = [ci] * 8 + [ctypes.POINTER(ci)]
         L.hg_debug_wide_plan.restype = ci
         L.hg_debug_wide_ranges.argtypes = [ci] * 8 + [ctypes.POINTER(ci), ctypes.POINTER(ci)]
@@ -172,6 +182,7 @@ class _PythonOnly:
         return None
 
     attn = attn_fp8 = attn_paged = append = append_fp8 = append_paged = prompt = chunk = slots = write = _none
+    tree_masks = tree_attn = tree_verify = tree_keep = _none
 
 
 def native():
@@ -191,7 +202,8 @@ def native():
             m = _PythonOnly
         else:
             fns = (L.hg_hydragen_attn, L.hg_hydragen_attn_fp8, L.hg_hydragen_attn_paged, L.hg_kv_append, L.hg_kv_append_fp8, L.hg_kv_append_paged,
-                   L.hg_prompt_attn, L.hg_chunk_attn_paged, L.hg_page_slots, L.hg_kv_write_paged)
+                   L.hg_prompt_attn, L.hg_chunk_attn_paged, L.hg_page_slots, L.hg_kv_write_paged,
+                   L.hg_tree_masks, L.hg_tree_attn_paged, L.hg_tree_verify, L.hg_tree_keep_paged)
             m.setup([ctypes.cast(f, ctypes.c_void_p).value for f in fns], Level, PagedKV)
         _native = m
     return _native
@@ -643,6 +655,102 @@ def hg_kv_write_paged(ctx: Context, Knew, Vnew, slots, kv: PagedKV) -> None:
         raise ValueError("paged cache: K must be [n_pages * page_size, Hkv, D]")
     st = kv.c_struct()
     _check(lib().hg_kv_write_paged(ctx.h, _p(Knew), _p(Vnew), step, _p(slots), T, ctypes.byref(st), Hkv, D), "hg_kv_write_paged")
+
+
+def hg_tree_masks(ctx: Context, parents, q_off, max_new: int, masks, depth=None) -> None:
+    """Which drafted tokens each one follows from: parents int32 [T], q_off int32 [B + 1], masks int32 [T, words] (bits), depth int32 [T]."""
+    rc = (_native or native()).tree_masks(ctx, parents, q_off, max_new, masks, depth)
+    if rc is not None:
+        if rc:
+            _check(rc, "hg_tree_masks")
+        return
+    T = parents.numel()
+    _want(parents, torch.int32, (T,), "parents"); _want(q_off, torch.int32, (q_off.numel(),), "q_off")
+    words = _mask_words(masks, T)
+    if depth is not None:
+        _want(depth, torch.int32, (T,), "depth")
+    _check(lib().hg_tree_masks(ctx.h, _p(parents), _p(q_off), T, max_new, q_off.numel() - 1, _p(masks), words, _p(depth)), "hg_tree_masks")
+
+
+def _mask_words(masks, T) -> int:
+    _want(masks, torch.int32, name="masks")
+    if masks.ndim != 2 or masks.shape[0] != T:
+        raise ValueError(f"masks: need [{T}, words], got {tuple(masks.shape)}")
+    return masks.shape[1]
+
+
+def hg_tree_attn_paged(ctx: Context, Q, q_off, masks, kv: PagedKV, lengths, max_new: int, max_len: int, O, LSE=None, scale: float = 0.0) -> None:
+    """hg_chunk_attn_paged of trees: a token sees all rows before its sequence's new ones, and of those what its row of masks (int32 [T, words]) says."""
+    rc = (_native or native()).tree_attn(ctx, Q, q_off, masks, kv, lengths, max_new, max_len, O, LSE, scale)
+    if rc is not None:
+        if rc:
+            _check(rc, "hg_tree_attn_paged")
+        return
+    T, Hq, D, q_step = _rows_of(Q, torch.bfloat16, "Q")
+    B = q_off.numel() - 1
+    Hkv = _want_paged(kv, B, D)
+    _want(q_off, torch.int32, (B + 1,), "q_off"); _want(lengths, torch.int32, (B,), "lengths")
+    words = _mask_words(masks, T)
+    _packed_out(O, LSE, (T, Hq), D)
+    st = kv.c_struct()
+    _check(lib().hg_tree_attn_paged(ctx.h, _p(Q), q_step, _p(q_off), T, _p(masks), words, ctypes.byref(st), _p(lengths), max_new, max_len, B, Hq, Hkv, D, scale,
+                                    _p(O), _dtype_code(O), _p(LSE)), "hg_tree_attn_paged")
+
+
+def _probs(t, dtype, T, V, name):
+    """Row distance of probabilities [T, V]"""
+    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != (T, V) or (V > 1 and t.stride(1) != 1) or (T > 1 and t.stride(0) < V):
+        raise ValueError(f"{name}: need a device tensor [{T}, {V}] of {dtype} with packed rows, got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+    return t.stride(0) if T > 1 else V
+
+
+def hg_tree_verify(ctx: Context, tokens, parents, q_off, max_new: int, target, draft, u, u_next, path, accepted, next_tokens) -> None:
+    """Which drafted tokens stand, and the token behind them.  target: the target's probabilities [T, V] (float32 or bfloat16, rows may lie further apart), or its tokens (int32 [T],
+    greedy decoding; draft, u and u_next are then None); draft: the drafts' probabilities, or None; u float32 [T], u_next float32 [B]; out: path int32 [T], accepted and next_tokens int32 [B]."""
+    rc = (_native or native()).tree_verify(ctx, tokens, parents, q_off, max_new, target, draft, u, u_next, path, accepted, next_tokens)
+    if rc is not None:
+        if rc:
+            _check(rc, "hg_tree_verify")
+        return
+    T, B = tokens.numel(), q_off.numel() - 1
+    for t, n, name in ((tokens, T, "tokens"), (parents, T, "parents"), (q_off, B + 1, "q_off"), (path, T, "path"), (accepted, B, "accepted"), (next_tokens, B, "next_tokens")):
+        _want(t, torch.int32, (n,), name)
+    V = t_step = d_step = 0
+    if target.ndim == 1:
+        _want(target, torch.int32, (T,), "target")
+        if draft is not None or u is not None or u_next is not None:
+            raise ValueError("draft, u and u_next are None where the target's tokens are given")
+        kind = HG_TOKENS
+    else:
+        if target.dtype not in (torch.float32, torch.bfloat16) or target.ndim != 2:
+            raise TypeError(f"target: need [T, V] of float32 or bfloat16, or int32 [T], got {target.dtype} {tuple(target.shape)}")
+        V, kind = target.shape[1], HG_F32 if target.dtype == torch.float32 else HG_BF16
+        t_step = _probs(target, target.dtype, T, V, "target")
+        if draft is not None:
+            d_step = _probs(draft, target.dtype, T, V, "draft")
+        _want(u, torch.float32, (T,), "u"); _want(u_next, torch.float32, (B,), "u_next")
+    _check(lib().hg_tree_verify(ctx.h, _p(tokens), _p(parents), _p(q_off), T, max_new, B, V, _p(target), t_step, _p(draft), d_step, kind, _p(u), _p(u_next),
+                                _p(path), _p(accepted), _p(next_tokens)), "hg_tree_verify")
+
+
+def hg_tree_keep_paged(ctx: Context, kvs: Sequence[PagedKV], q_off, path, accepted, lengths, max_new: int, new_lengths) -> None:
+    """The accepted tokens' rows moved together behind the context in every layer's cache (kvs: PagedKV of one table and geometry), and the lengths afterwards."""
+    rc = (_native or native()).tree_keep(ctx, kvs, q_off, path, accepted, lengths, max_new, new_lengths)
+    if rc is not None:
+        if rc:
+            _check(rc, "hg_tree_keep_paged")
+        return
+    T, B = path.numel(), q_off.numel() - 1
+    for t, n, name in ((q_off, B + 1, "q_off"), (path, T, "path"), (accepted, B, "accepted"), (lengths, B, "lengths"), (new_lengths, B, "new_lengths")):
+        _want(t, torch.int32, (n,), name)
+    if not kvs:
+        raise ValueError("kvs: need the cache of one layer at least")
+    D = kvs[0].K.shape[-1]
+    Hkv = [_want_paged(kv, B, D) for kv in kvs][0]
+    if any(kv.K.shape != kvs[0].K.shape for kv in kvs):
+        raise ValueError("kvs: the layers' caches must have one shape")
+    st = (hg_paged_kv * len(kvs))(*[kv.c_struct() for kv in kvs])
+    _check(lib().hg_tree_keep_paged(ctx.h, len(kvs), st, _p(q_off), T, _p(path), _p(accepted), _p(lengths), max_new, B, Hkv, D, _p(new_lengths)), "hg_tree_keep_paged")
 
 
 def hg_debug_wide_plan(n_blocks: int, max_rows: int, max_seqs: int, Hkv: int, rows_per_seq: int, max_parts: int, slots_per_xcd: int,

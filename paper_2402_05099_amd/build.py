@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libhydragen.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")
-SOURCES = ["api.hip", "prefix.hip", "prefix_wide.hip", "prefix_wide_d64.hip", "combined_tiles.hip", "combined.hip", "combined_d64.hip", "combined_tiles_d64.hip", "decode.hip", "merge.hip", "kvcache.hip", "decode_mfma.hip", "fused_small.hip", "ragged_api.hip", "ragged_wide.hip", "ragged_wide_d64.hip", "ragged_rows.hip", "pages.hip", "ceilings.hip"]
+SOURCES = ["api.hip", "prefix.hip", "prefix_wide.hip", "prefix_wide_d64.hip", "combined_tiles.hip", "combined.hip", "combined_d64.hip", "combined_tiles_d64.hip", "decode.hip", "merge.hip", "kvcache.hip", "decode_mfma.hip", "fused_small.hip", "ragged_api.hip", "ragged_wide.hip", "ragged_wide_d64.hip", "ragged_rows.hip", "tree_rows.hip", "tree_wide.hip", "tree_wide_d64.hip", "tree.hip", "tree_api.hip", "pages.hip", "ceilings.hip"]
 
 # packed fp32 VALU forms are switched off for every device compile of this library
 HIPCC_FLAGS = [

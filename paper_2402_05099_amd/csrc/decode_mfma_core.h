@@ -250,6 +250,22 @@ struct MfmaTile {
         }
     }
 
+    // stage rows whose bit is not set get the score -inf
+    __device__ __forceinline__ void mask_bits(Scores& r, unsigned bits) const {
+        const unsigned mine = bits >> (TR == 16 ? 4 * lg : 4 * hl);
+        if constexpr (TR == 16) {
+#pragma unroll
+            for (int kg = 0; kg < 2; ++kg)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!(mine >> (16 * kg + i) & 1u)) r.S4[kg][i] = -INFINITY;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (!(mine >> (8 * (i >> 2) + (i & 3)) & 1u)) r.S[i] = -INFINITY;
+        }
+    }
+
     // online softmax: scores -> weights as B operand of the value product (k-slot order), row sums, lazy rescaling
     __device__ __forceinline__ void softmax(const Scores& r, uintx4 (&pb)[2]) {
         float tmax;

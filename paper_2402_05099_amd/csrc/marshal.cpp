@@ -1,5 +1,5 @@
 // The argument marshalling of the decode-step calls (fused attention, cache update) and of those that lead to it (prompts, chunks, slots, the write
-// into the pages) as a CPython extension: the checks of
+// into the pages, drafted trees) as a CPython extension: the checks of
 // binding.py on the tensors, their device pointers, and the call into libhydragen.so, whose functions it is handed as addresses.
 //
 // Why native: such a call is one to three kernel launches of a few microseconds each, and checking a dozen tensors
@@ -29,6 +29,10 @@ decltype(&hg_prompt_attn) f_prompt;
 decltype(&hg_chunk_attn_paged) f_chunk;
 decltype(&hg_page_slots) f_slots;
 decltype(&hg_kv_write_paged) f_write;
+decltype(&hg_tree_masks) f_tree_masks;
+decltype(&hg_tree_attn_paged) f_tree_attn;
+decltype(&hg_tree_verify) f_tree_verify;
+decltype(&hg_tree_keep_paged) f_tree_keep;
 PyObject *level_type, *paged_type;
 
 PyObject *s_h, *s_value, *s_nq, *s_K, *s_V, *s_n_blocks, *s_kv_off, *s_seq_off, *s_max_rows, *s_max_seqs, *s_page_table, *s_page_size,
@@ -416,14 +420,138 @@ PyObject* write(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-constexpr int kFunctions = 10;
+// int32 [T, words]
+struct Masks {
+    void* p;
+    int words;
+    Masks(PyObject* o, int64_t T) {
+        const at::Tensor& t = device_tensor(o, at::kInt);
+        require(t.dim() == 2 && t.size(0) == T && t.size(1) <= INT_MAX);
+        p = t.data_ptr();
+        words = (int)t.size(1);
+    }
+};
+// (ctx, parents, q_off, max_new, masks, depth)
+PyObject* tree_masks(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 6, [&]() {
+        const Ints up(a[1]), off(a[2]);
+        require(off.n > 0);
+        const int max_new = to_int(a[3]);
+        const Masks m(a[4], up.n);
+        const void* depth = a[5] == Py_None ? nullptr : vector_of(a[5], up.n);
+        hg_ctx* const c = context(a[0]);
+        return without_gil([&]() { return f_tree_masks(c, up.p, off.p, up.n, max_new, off.n - 1, (uint32_t*)m.p, m.words, (int32_t*)depth); });
+    });
+}
+// (ctx, Q, q_off, masks, kv, lengths, max_new, max_len, O, LSE, scale)
+PyObject* tree_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 11, [&]() {
+        const Tokens q(a[1]);
+        const Ints off(a[2]);
+        require(off.n > 0);
+        const Masks m(a[3], q.T);
+        const Paged kv(a[4], off.n - 1, q.D);
+        const void* len = vector_of(a[5], off.n - 1);
+        const int max_new = to_int(a[6]), max_len = to_int(a[7]);
+        const Outputs out(a[8], a[9], q);
+        const float scale = to_float(a[10]);
+        hg_ctx* const c = context(a[0]);
+        return without_gil([&]() {
+            return f_tree_attn(c, q.t.data_ptr(), q.step, off.p, (int)q.T, (const uint32_t*)m.p, m.words, &kv.kv, (const int32_t*)len, max_new, max_len, off.n - 1, (int)q.H,
+                               (int)kv.Hkv, (int)q.D, scale, out.O, out.dtype, out.lse);
+        });
+    });
+}
+// Probabilities [T, V] whose rows may lie further apart than they are long
+struct Probs {
+    const void* p;
+    int64_t V, step;
+    Probs(PyObject* o, at::ScalarType type, int64_t T) {
+        const at::Tensor& t = tensor(o);
+        require(t.is_cuda() && t.scalar_type() == type && t.dim() == 2 && t.size(0) == T && t.size(1) <= INT_MAX);
+        V = t.size(1);
+        step = T > 1 ? t.stride(0) : V;
+        require((V <= 1 || t.stride(1) == 1) && step >= V);
+        p = t.data_ptr();
+    }
+};
+const void* floats_of(PyObject* o, int64_t n) {      // float32 [n]
+    const at::Tensor& t = device_tensor(o, at::kFloat);
+    require(t.dim() == 1 && t.size(0) == n);
+    return t.data_ptr();
+}
+// (ctx, tokens, parents, q_off, max_new, target, draft, u, u_next, path, accepted, next_tokens)
+PyObject* tree_verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 12, [&]() {
+        const Ints tok(a[1]), off(a[3]);
+        require(off.n > 0);
+        const int T = tok.n, B = off.n - 1;
+        const void* up = vector_of(a[2], T);
+        const int max_new = to_int(a[4]);
+        const void *path = vector_of(a[9], T), *kept = vector_of(a[10], B), *next = vector_of(a[11], B);
+        const at::ScalarType type = tensor(a[5]).scalar_type();
+        hg_ctx* const c = context(a[0]);
+        if (type == at::kInt) {
+            const void* says = vector_of(a[5], T);
+            require(a[6] == Py_None && a[7] == Py_None && a[8] == Py_None);
+            return without_gil([&]() {
+                return f_tree_verify(c, tok.p, (const int32_t*)up, off.p, T, max_new, B, 0, says, 0, nullptr, 0, HG_TOKENS, nullptr, nullptr, (int32_t*)path, (int32_t*)kept,
+                                     (int32_t*)next);
+            });
+        }
+        require(type == at::kFloat || type == at::kBFloat16);
+        const Probs p(a[5], type, T);
+        const void *q = nullptr, *u = floats_of(a[7], T), *u_next = floats_of(a[8], B);
+        int64_t q_step = 0;
+        if (a[6] != Py_None) {
+            const Probs d(a[6], type, T);
+            require(d.V == p.V);
+            q = d.p;
+            q_step = d.step;
+        }
+        return without_gil([&]() {
+            return f_tree_verify(c, tok.p, (const int32_t*)up, off.p, T, max_new, B, (int)p.V, p.p, p.step, q, q_step, type == at::kFloat ? HG_F32 : HG_BF16, (const float*)u,
+                                 (const float*)u_next, (int32_t*)path, (int32_t*)kept, (int32_t*)next);
+        });
+    });
+}
+// (ctx, kvs, q_off, path, accepted, lengths, max_new, new_lengths)
+PyObject* tree_keep(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 8, [&]() {
+        require(PyList_CheckExact(a[1]) && PyList_GET_SIZE(a[1]) > 0 && PyList_GET_SIZE(a[1]) <= HG_MAX_LAYERS);
+        const Ints off(a[2]), path(a[3]);
+        require(off.n > 0);
+        const int B = off.n - 1, layers = (int)PyList_GET_SIZE(a[1]);
+        const void *kept = vector_of(a[4], B), *len = vector_of(a[5], B), *grown = vector_of(a[7], B);
+        const int max_new = to_int(a[6]);
+        hg_paged_kv kv[HG_MAX_LAYERS];
+        int64_t Hkv = 0, D = 0, n_pages = 0;
+        for (int i = 0; i < layers; ++i) {
+            const Ref l(Py_NewRef(PyList_GET_ITEM(a[1], i)));
+            const Ref k(PyObject_GetAttr(l.p, s_K));
+            const at::Tensor& K = tensor(k.p);
+            require(K.dim() == 3 && K.size(2) <= INT_MAX);
+            if (i == 0) D = K.size(2);
+            const Paged p(l.p, B, D);
+            if (i == 0) { Hkv = p.Hkv; n_pages = p.kv.n_pages; }
+            require(p.Hkv == Hkv && p.kv.n_pages == n_pages && Hkv <= INT_MAX);
+            kv[i] = p.kv;
+        }
+        hg_ctx* const c = context(a[0]);
+        return without_gil([&]() {
+            return f_tree_keep(c, layers, kv, off.p, path.n, path.p, (const int32_t*)kept, (const int32_t*)len, max_new, B, (int)Hkv, (int)D, (int32_t*)grown);
+        });
+    });
+}
+
+constexpr int kFunctions = 14;
 // ([addresses of the functions, in the order above], Level, PagedKV)
 PyObject* setup(PyObject*, PyObject* args) {
     PyObject *list, *lt, *pt;
     if (!PyArg_ParseTuple(args, "O!OO", &PyList_Type, &list, &lt, &pt)) return nullptr;
     void* f[kFunctions];
     if (PyList_GET_SIZE(list) != kFunctions) {
-        PyErr_SetString(PyExc_ValueError, "ten addresses are wanted");
+        PyErr_SetString(PyExc_ValueError, "fourteen addresses are wanted");
         return nullptr;
     }
     for (int i = 0; i < kFunctions; ++i) {
@@ -440,6 +568,10 @@ PyObject* setup(PyObject*, PyObject* args) {
     f_chunk = (decltype(f_chunk))f[7];
     f_slots = (decltype(f_slots))f[8];
     f_write = (decltype(f_write))f[9];
+    f_tree_masks = (decltype(f_tree_masks))f[10];
+    f_tree_attn = (decltype(f_tree_attn))f[11];
+    f_tree_verify = (decltype(f_tree_verify))f[12];
+    f_tree_keep = (decltype(f_tree_keep))f[13];
     Py_INCREF(lt);
     Py_INCREF(pt);
     level_type = lt;
@@ -449,7 +581,8 @@ PyObject* setup(PyObject*, PyObject* args) {
 
 #define HG_FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HG_FAST(attn), HG_FAST(attn_fp8), HG_FAST(attn_paged), HG_FAST(append), HG_FAST(append_fp8), HG_FAST(append_paged),
-                         HG_FAST(prompt), HG_FAST(chunk), HG_FAST(slots), HG_FAST(write), {"setup", setup, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         HG_FAST(prompt), HG_FAST(chunk), HG_FAST(slots), HG_FAST(write), HG_FAST(tree_masks), HG_FAST(tree_attn), HG_FAST(tree_verify), HG_FAST(tree_keep),
+                         {"setup", setup, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -49,6 +49,11 @@ struct RaggedArgs {
     int tile_nsplit, tile_chunk;        // key ranges of a tile and their length (a multiple of 64)
     float* tile_part_O;       // tile_nsplit > 1: partial results [tile_nsplit][rows * Hq][D], [tile_nsplit][rows * Hq]
     float* tile_part_L;
+
+    // Trees of drafted tokens (hg_tree_attn_paged; null: none): a sequence's n tokens are the last n of its rows, and which of those token t sees says row t of the masks, a bit
+    // for each; it sees all rows before them.
+    const uint32_t* masks;
+    int mask_words;           // of a row of the masks
 };
 constexpr int kTile = 128;        // rows of a tile
 constexpr int kFewRows = 32;      // a remainder of more rows is a tile: beside tiles, and wherever a read of the cache for every 32 rows is what costs
@@ -79,6 +84,11 @@ hipError_t launch_ragged_rows(const RaggedArgs& a, int D, bool codes, hipStream_
 hipError_t launch_ragged_wide(const RaggedArgs& a, bool codes, hipStream_t s);           // ragged_wide.hip, D = 128: tiles, and what remains in the same launch
 hipError_t launch_ragged_wide_d64(const RaggedArgs& a, bool codes, hipStream_t s);          // ragged_wide_d64.hip
 hipError_t launch_ragged_join(const RaggedArgs& a, int D, hipStream_t s);                   // ragged_rows.hip: the parts of either (nsplit > 1, tile_nsplit > 1)
+// ... and the same for trees: tree_rows.hip, tree_wide.hip, tree_wide_d64.hip
+hipError_t launch_tree_rows(const RaggedArgs& a, int D, bool codes, hipStream_t s);
+hipError_t launch_tree_wide(const RaggedArgs& a, bool codes, hipStream_t s);
+hipError_t launch_tree_wide_d64(const RaggedArgs& a, bool codes, hipStream_t s);
+hipError_t launch_tree_join(const RaggedArgs& a, int D, hipStream_t s);
 
 // ---- block tables, slots and the write into a paged cache (pages.hip) ----
 struct SlotArgs {
@@ -161,13 +171,25 @@ __device__ __forceinline__ float value_if_not_finite(const unsigned char* e) {
     }
 }
 
+// Of a tree's tokens, those that one of them sees, whose row of the masks has `n` words: bit i of the result stands for the i-th row from `j` on, counted from the tree's first.  Rows
+// before it are the context, which is seen; those that the masks have no bit for are not.
+__device__ __forceinline__ unsigned tree_bits(const uint32_t* words, int n, int j) {
+    if (j <= -32) return ~0u;
+    const int w = j >> 5;
+    const unsigned lo = w < 0 ? ~0u : w < n ? words[w] : 0u, hi = w + 1 < n ? words[w + 1] : 0u;
+    return __builtin_amdgcn_alignbit(hi, lo, (unsigned)j & 31u);
+}
+__device__ __forceinline__ unsigned first_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
+
 // What a tile's kernel knows of its sequence; uniform over the workgroup.
 struct RaggedSeq {
     int b;
     int q0, n;        // first token, tokens
     int take;         // tokens that are computed (n, or max_new)
     int len;          // keys
-    __device__ __forceinline__ int seen(int t) const { return len - (n - 1 - t); }      // keys that token t sees (none if <= 0)
+    // keys that token t sees (none if <= 0); of a tree: that it may see
+    template <bool TREE = false>
+    __device__ __forceinline__ int seen(int t) const { return TREE ? len : len - (n - 1 - t); }
 };
 __device__ __forceinline__ RaggedSeq ragged_seq(const RaggedArgs& a, int b) {
     RaggedSeq s;
@@ -185,12 +207,13 @@ __device__ __forceinline__ RaggedSeq ragged_seq(const RaggedArgs& a, int b) {
 // Tiles of sequence b are numbered from floor(q_off[b] * G / kTile) + b on, which leaves room for each of its at most ceil(n * G / kTile) tiles before the next
 // sequence's: no table is needed, and the sequence is found with a look at 64 at a time.  Up to eight sequences are taken in the order of their largest tiles
 // instead (lane i holds sequence i and adds up the tiles of those before it: 0.09 us a sequence, 5 us of the 16 that a workgroup had with 45 short prompts).
+template <bool TREE = false>
 __device__ __forceinline__ bool tile_of_rank(const RaggedArgs& a, int rank, RaggedSeq& seq, int& tile) {
     const int lane = threadIdx.x & 63;
     if (a.B <= 8) {
         const RaggedSeq own = ragged_seq(a, min(lane, a.B - 1));
         const int tiles = lane < a.B ? (rows_in_tiles(own.take * a.G, a.few_rows) + kTile - 1) / kTile : 0;
-        const int size = (max(own.seen(0), 0) / kTile) * a.G + tiles;      // of the largest tile, in units of a tile's tokens
+        const int size = (max(own.template seen<TREE>(0), 0) / kTile) * a.G + tiles;      // of the largest tile, in units of a tile's tokens
         int start = 0;
         for (int i = 0; i < a.B; ++i) {
             const int other = __builtin_amdgcn_readlane(size, i);

@@ -1,5 +1,5 @@
-// Host side of the calls between a prompt and its first decode step: argument checks and the choice of kernels for hg_prompt_attn,
-// hg_chunk_attn_paged, hg_page_slots and hg_kv_write_paged.  As in api.hip: no device allocation, no host synchronisation, no copies.
+// Host side of the calls between a prompt and its first decode step, and of the attention of drafted trees: argument checks and the choice of kernels for hg_prompt_attn,
+// hg_chunk_attn_paged, hg_tree_attn_paged, hg_page_slots and hg_kv_write_paged.  As in api.hip: no device allocation, no host synchronisation, no copies.
 #include <math.h>
 #include <algorithm>
 
@@ -164,9 +164,48 @@ bool plan_chunk(RaggedArgs& a, int max_len, int D, bool codes, Room room) {
 
 // tiles: the call has any; what remains behind them, or is all there is, goes along
 int run(const hg_ctx* c, const RaggedArgs& a, int D, bool codes, bool tiles) {
-    const int rc = rc_of(!tiles ? launch_ragged_rows(a, D, codes, c->stream) : D == 128 ? launch_ragged_wide(a, codes, c->stream) : launch_ragged_wide_d64(a, codes, c->stream));
+    const bool tree = a.masks != nullptr;
+    const auto few = tree ? launch_tree_rows : launch_ragged_rows;
+    const auto wide = D == 128 ? (tree ? launch_tree_wide : launch_ragged_wide) : tree ? launch_tree_wide_d64 : launch_ragged_wide_d64;
+    const int rc = rc_of(tiles ? wide(a, codes, c->stream) : few(a, D, codes, c->stream));
     if (rc || (a.nsplit == 1 && a.tile_nsplit == 1)) return rc;
-    return rc_of(launch_ragged_join(a, D, c->stream));
+    return rc_of((tree ? launch_tree_join : launch_ragged_join)(a, D, c->stream));
+}
+
+// hg_chunk_attn_paged, and with masks hg_tree_attn_paged
+int attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_t* q_off, int rows, const hg_paged_kv* kv, const int32_t* lengths, const uint32_t* masks,
+               int mask_words, int max_new, int max_len, int B, int Hq, int Hkv, int D, float scale, void* O, int o_dtype, float* LSE) {
+    const int rc = check_ragged(c, Q, q_stride, q_off, rows, max_new, B, Hq, Hkv, D, O, o_dtype);
+    if (rc) return rc;
+    if (!kv || max_len < 0) return HG_ERR_INVALID_ARG;
+    const bool codes = kv->kv_format == HG_KV_E4M3;
+    if (!codes && kv->kv_format != HG_KV_BF16) return HG_ERR_INVALID_ARG;
+    if (codes && (!positive_scale(kv->k_scale) || !positive_scale(kv->v_scale))) return HG_ERR_INVALID_ARG;
+    const int shift = page_shift(kv->page_size);
+    if (shift < 0 || kv->n_pages < 0 || kv->table_stride < 0) return HG_ERR_INVALID_ARG;
+    if ((int64_t)kv->n_pages * kv->page_size >= (1LL << 31) || (int64_t)kv->table_stride * kv->page_size >= (1LL << 31) || check_cache_sizes(max_len, Hkv, D))
+        return HG_ERR_UNSUPPORTED;
+    if (rows == 0 || B == 0 || max_new == 0) return HG_OK;
+    if (!lengths || !kv->K || !kv->V || !kv->page_table || kv->n_pages < 1 || (int64_t)kv->table_stride * kv->page_size < std::max(max_len, 1) ||
+        (reinterpret_cast<uintptr_t>(kv->K) | reinterpret_cast<uintptr_t>(kv->V)) % 16 != 0) return HG_ERR_INVALID_ARG;
+    if (hipSetDevice(c->device) != hipSuccess) return HG_ERR_HIP;
+    RaggedArgs a = ragged_args(Q, q_stride, q_off, rows, max_new, B, Hq, Hkv, D, scale, O, o_dtype, LSE);
+    a.K = static_cast<const unsigned char*>(kv->K);
+    a.V = static_cast<const unsigned char*>(kv->V);
+    a.kv_stride = (int64_t)Hkv * D * (codes ? 1 : 2);
+    a.lengths = lengths;
+    a.masks = masks;
+    a.mask_words = mask_words;
+    a.pg.table = kv->page_table;
+    a.pg.shift = shift;
+    a.pg.stride = kv->table_stride;
+    a.pg.n_pages = kv->n_pages;
+    if (codes) {
+        a.scale *= kv->k_scale;
+        a.v_scale = kv->v_scale;
+    }
+    const bool tiles = plan_chunk(a, max_len, D, codes, room_of(c));
+    return run(c, a, D, codes, tiles);
 }
 
 }  // namespace
@@ -192,35 +231,14 @@ int hg_prompt_attn(hg_ctx* c, const void* Q, const void* K, const void* V, int64
 
 int hg_chunk_attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_t* q_off, int rows, const hg_paged_kv* kv, const int32_t* lengths,
                         int max_new, int max_len, int B, int Hq, int Hkv, int D, float scale, void* O, int o_dtype, float* LSE) {
-    const int rc = check_ragged(c, Q, q_stride, q_off, rows, max_new, B, Hq, Hkv, D, O, o_dtype);
-    if (rc) return rc;
-    if (!kv || max_len < 0) return HG_ERR_INVALID_ARG;
-    const bool codes = kv->kv_format == HG_KV_E4M3;
-    if (!codes && kv->kv_format != HG_KV_BF16) return HG_ERR_INVALID_ARG;
-    if (codes && (!positive_scale(kv->k_scale) || !positive_scale(kv->v_scale))) return HG_ERR_INVALID_ARG;
-    const int shift = page_shift(kv->page_size);
-    if (shift < 0 || kv->n_pages < 0 || kv->table_stride < 0) return HG_ERR_INVALID_ARG;
-    if ((int64_t)kv->n_pages * kv->page_size >= (1LL << 31) || (int64_t)kv->table_stride * kv->page_size >= (1LL << 31) || check_cache_sizes(max_len, Hkv, D))
-        return HG_ERR_UNSUPPORTED;
-    if (rows == 0 || B == 0 || max_new == 0) return HG_OK;
-    if (!lengths || !kv->K || !kv->V || !kv->page_table || kv->n_pages < 1 || (int64_t)kv->table_stride * kv->page_size < std::max(max_len, 1) ||
-        (reinterpret_cast<uintptr_t>(kv->K) | reinterpret_cast<uintptr_t>(kv->V)) % 16 != 0) return HG_ERR_INVALID_ARG;
-    if (hipSetDevice(c->device) != hipSuccess) return HG_ERR_HIP;
-    RaggedArgs a = ragged_args(Q, q_stride, q_off, rows, max_new, B, Hq, Hkv, D, scale, O, o_dtype, LSE);
-    a.K = static_cast<const unsigned char*>(kv->K);
-    a.V = static_cast<const unsigned char*>(kv->V);
-    a.kv_stride = (int64_t)Hkv * D * (codes ? 1 : 2);
-    a.lengths = lengths;
-    a.pg.table = kv->page_table;
-    a.pg.shift = shift;
-    a.pg.stride = kv->table_stride;
-    a.pg.n_pages = kv->n_pages;
-    if (codes) {
-        a.scale *= kv->k_scale;
-        a.v_scale = kv->v_scale;
-    }
-    const bool tiles = plan_chunk(a, max_len, D, codes, room_of(c));
-    return run(c, a, D, codes, tiles);
+    return attn_paged(c, Q, q_stride, q_off, rows, kv, lengths, nullptr, 0, max_new, max_len, B, Hq, Hkv, D, scale, O, o_dtype, LSE);
+}
+
+int hg_tree_attn_paged(hg_ctx* c, const void* Q, int64_t q_stride, const int32_t* q_off, int rows, const uint32_t* masks, int mask_words, const hg_paged_kv* kv,
+                       const int32_t* lengths, int max_new, int max_len, int B, int Hq, int Hkv, int D, float scale, void* O, int o_dtype, float* LSE) {
+    if (mask_words < 0 || (rows > 0 && B > 0 && max_new > 0 && (!masks || 32LL * mask_words < std::min(max_new, rows)))) return HG_ERR_INVALID_ARG;
+    if (mask_words >= (1 << 26)) return HG_ERR_UNSUPPORTED;      // (bits are counted in 32 bits)
+    return attn_paged(c, Q, q_stride, q_off, rows, kv, lengths, masks, mask_words, max_new, max_len, B, Hq, Hkv, D, scale, O, o_dtype, LSE);
 }
 
 int hg_page_slots(hg_ctx* c, const int32_t* lengths, const int32_t* counts, const int32_t* free_pages, int n_free, int page_size, int B, int rows,

@@ -50,7 +50,7 @@ __device__ __forceinline__ void store_row8(const OutDev& out, int64_t row, int c
 }
 
 // What workgroup `id` does for a sequence whose tiles have TR rows; everything up to the tile is known to the caller.
-template <int D, bool CODES, int TR, int NW>
+template <int D, bool CODES, int TR, int NW, bool TREE>
 __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, int sp, int kvh, int q0, int n, int len, int row0, int nrows) {
     using Tile = MfmaTile<D, CODES, TR>;
     using G_ = Geo<D>;
@@ -61,11 +61,11 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
 
     const int r0 = row0 + rt * TR;      // the tile's first row; the sequence's rows are [0, nrows), those from row0 on are taken here
     if (r0 >= nrows) return;
-    const auto seen_by = [&](int t) { return len - (n - 1 - t); };
+    const auto seen_by = [&](int t) { return TREE ? len : len - (n - 1 - t); };
     const int t_first = (int)a.by_group.of((unsigned)r0), t_last = (int)a.by_group.of((unsigned)(min(r0 + TR, nrows) - 1));
     const int k0 = sp * a.chunk, ke = min(seen_by(t_last), k0 + a.chunk);      // keys [k0, ke)
     if (sp > 0 && k0 >= ke) return;      // (the join looks at no part that starts behind a row's keys)
-    const int all_see = seen_by(t_first);       // every row of the tile sees the keys below
+    const int all_see = TREE ? len - n : seen_by(t_first);       // every row of the tile sees the keys below
     const bool in_parts = seen_by((int)a.by_group.of((unsigned)(nrows - 1))) > a.chunk;      // the sequence has several ranges
     const int nst = ke > k0 ? (ke - k0 + KT - 1) / KT : 0;
 
@@ -76,6 +76,8 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
     const bool rv = r < nrows;
     const int tok = (int)a.by_group.of((unsigned)(rv ? r : r0)), g = (rv ? r : r0) - tok * a.G;
     const int seen = rv ? seen_by(tok) : 0;
+    const uint32_t* const words = TREE ? a.masks + (int64_t)(q0 + tok) * a.mask_words : nullptr;
+    const auto bits_from = [&](int key0) { return tree_bits(words, a.mask_words, key0 - all_see); };      // (TREE) of 32 keys from key0 on
     {
         const unsigned char* const qp = reinterpret_cast<const unsigned char*>(a.Q) + (int64_t)(q0 + tok) * a.q_stride + (kvh * a.G + g) * (D * 2);
         if constexpr (TR == 16) {
@@ -161,7 +163,10 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
             if (((i + 1) & 31) == 0) look_up(i + 1);
             copy(a.K, voffK, i + 1, dst);
         }
-        if (key0 + KT > min(ke, all_see)) t.mask(S, 0, min(seen, ke) - key0);
+        if (key0 + KT > min(ke, all_see)) {
+            if constexpr (TREE) t.mask_bits(S, bits_from(key0) & first_bits(min(seen, ke) - key0));
+            else t.mask(S, 0, min(seen, ke) - key0);
+        }
         t.softmax(S, pb);
         if (more) wait_vm<CPS>();      // V has landed; the next K may be in flight
         else wait_vm<0>();
@@ -183,6 +188,7 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
         for (int i = spoiled; i < mine; ++i)
 #pragma unroll 1
             for (int key = k0 + (w + i * NW) * KT, end = min(key + KT, min(ke, seen)); key < end; ++key) {
+                if (TREE && !(bits_from(key) & 1u)) continue;
                 const int page = min(max(a.pg.table[(int64_t)b * a.pg.stride + min(key >> shift, a.pg.stride - 1)], 0), a.pg.n_pages - 1);
                 const unsigned char* const vr = a.V + (((int64_t)page << shift) + (key & ((1 << shift) - 1))) * a.kv_stride + (int64_t)kvh * (D * ES);
                 if constexpr (TR == 16) {
@@ -268,7 +274,7 @@ __device__ __forceinline__ void rows_tile(const RaggedArgs& a, int b, int rt, in
 // to 4096 rows, two and four ranges 122 and 123 us so, 114 with one).  At most 16 rows make a tile of 16, more of them tiles of 32 (`BOTH`: there may be more).
 // Codes of a row at D = 64 are half a line, and heads that follow each other on different XCDs fetched every line twice: 32 x 64/8 heads, 8192 keys 94 us, 40/40 heads, 2048 keys
 // 114; in pairs (Hkv even) 69 and 84.
-template <int D, bool CODES, bool BOTH, int NW>
+template <int D, bool CODES, bool BOTH, int NW, bool TREE = false>
 __device__ __forceinline__ void rows_workgroup(const RaggedArgs& a, unsigned id) {
     typedef const __attribute__((address_space(4))) int32_t* const_i32;
     int rest, kvh;
@@ -290,8 +296,8 @@ __device__ __forceinline__ void rows_workgroup(const RaggedArgs& a, unsigned id)
     const int len = max(min(((const_i32)(uintptr_t)a.lengths)[b], a.max_len), 0);
     const int nrows = min(n, a.max_new) * a.G;
     const int row0 = rows_in_tiles(nrows, a.few_rows);
-    if (!BOTH || nrows - row0 <= 16) rows_tile<D, CODES, 16, NW>(a, b, rt, sp, kvh, q0, n, len, row0, nrows);
-    else rows_tile<D, CODES, 32, NW>(a, b, rt, sp, kvh, q0, n, len, row0, nrows);
+    if (!BOTH || nrows - row0 <= 16) rows_tile<D, CODES, 16, NW, TREE>(a, b, rt, sp, kvh, q0, n, len, row0, nrows);
+    else rows_tile<D, CODES, 32, NW, TREE>(a, b, rt, sp, kvh, q0, n, len, row0, nrows);
 }
 
 }  // namespace rr

@@ -1,5 +1,6 @@
 // Causal attention of packed tokens on the matrix cores, 128 query rows to a workgroup: the body shared by ragged_wide.hip (D = 128) and
-// ragged_wide_d64.hip (D = 64), which define HG_RW_D.  Prompts, and long chunks but for what remains behind their tiles.
+// ragged_wide_d64.hip (D = 64), which define HG_RW_D and HG_RW_TREE.  Prompts, and long chunks but for what remains behind their tiles; as tree_wide.hip and
+// tree_wide_d64.hip trees of drafted tokens, whose rows see what their masks say of the last keys.
 //
 // Mathematics and pipeline are those of prefix_wide_impl.h (transposed products with v_mfma_f32_32x32x16_bf16, a lane owns one query row, weights
 // against a maximum that is only raised when their sum says so, one step = scores of stage j + 2, weights of stage j + 1 and P V of stage j, written out by
@@ -32,6 +33,7 @@ namespace rw {
 namespace {
 
 constexpr int D = HG_RW_D;
+constexpr bool TREE = HG_RW_TREE;
 constexpr int KT = D == 128 ? 32 : 64;  // keys per stage: 8 KiB of K and 8 KiB of V as bf16
 constexpr int KB = KT / 32;             // 32-key score tiles per stage
 constexpr int NW = 4;                   // wavefronts per workgroup
@@ -136,32 +138,36 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
         }
         const int rank = (int)(v / (unsigned)a.tile_nsplit);
         sp = (int)(v - (unsigned)rank * (unsigned)a.tile_nsplit);
-        if (!tile_of_rank(a, rank, sq, tile)) return;
+        if (!tile_of_rank<TREE>(a, rank, sq, tile)) return;
     }
     const int b = __builtin_amdgcn_readfirstlane(sq.b);
     const int nrows = __builtin_amdgcn_readfirstlane(rows_in_tiles(sq.take * a.G, a.few_rows)), row0 = tile * kTileRows;      // rows that tiles take
     const int q0 = __builtin_amdgcn_readfirstlane(sq.q0);
-    const int before = __builtin_amdgcn_readfirstlane(sq.len - (sq.n - 1));      // keys that the sequence's first token sees
+    // keys that the sequence's first token sees; of a tree, that all its tokens see
+    const int before = __builtin_amdgcn_readfirstlane(TREE ? max(sq.len - sq.n, 0) : sq.len - (sq.n - 1));
     const int tid = threadIdx.x, l = tid & 63, lq = l & 31, hl = l >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const auto token_of = [&](int r) { return (int)a.by_group.of((unsigned)r); };
     const int k0 = sp * a.tile_chunk;
-    const int k_all = __builtin_amdgcn_readfirstlane(before + token_of(min(row0 + kTileRows, nrows) - 1)), ke = min(k_all, k0 + a.tile_chunk);      // keys [k0, ke) of k_all
+    const int k_all = __builtin_amdgcn_readfirstlane(TREE ? sq.len : before + token_of(min(row0 + kTileRows, nrows) - 1)), ke = min(k_all, k0 + a.tile_chunk);      // keys [k0, ke) of k_all
     const int nst = ke > k0 ? (ke - k0 + KT - 1) / KT : 0, nfull = ke > k0 ? (ke - k0) / KT : 0;
     if (sp > 0 && nst == 0) return;      // (the join looks at no part that starts behind a row's keys)
     // stages from here on have keys that some row of the tile does not see
-    const int all_see = __builtin_amdgcn_readfirstlane(max(min(before + token_of(row0), ke), k0));
+    const int all_see = __builtin_amdgcn_readfirstlane(max(min(TREE ? before : before + token_of(row0), ke), k0));
     const int masked = all_see < ke ? (all_see - k0) / KT : nst;
     // this wavefront's rows, and this lane's
     const int wrow0 = row0 + 32 * w;
     const bool any = wrow0 < nrows;
-    const int w_least = __builtin_amdgcn_readfirstlane(any ? min(before + token_of(wrow0), ke) : 0);                              // every row of the wavefront sees the keys below
-    const int w_most = __builtin_amdgcn_readfirstlane(any ? min(before + token_of(min(wrow0 + 32, nrows) - 1), ke) : 0);          // ... and none those from here on
+    const int w_least = __builtin_amdgcn_readfirstlane(any ? min(TREE ? before : before + token_of(wrow0), ke) : 0);                              // every row of the wavefront sees the keys below
+    const int w_most = __builtin_amdgcn_readfirstlane(any ? min(TREE ? sq.len : before + token_of(min(wrow0 + 32, nrows) - 1), ke) : 0);          // ... and none those from here on
     const int mine = w_most > k0 ? (w_most - k0 + KT - 1) / KT : 0;      // stages that this wavefront multiplies
     const int r = wrow0 + lq;
     const bool rv = r < nrows;
     const int tok = token_of(rv ? r : row0), head = (rv ? r : row0) - tok * a.G + kvh * a.G;
-    const int seen = rv ? min(before + tok, ke) : 0;
+    const int seen = rv ? min(TREE ? sq.len : before + tok, ke) : 0;
+    const uint32_t* const words = TREE ? a.masks + (int64_t)(q0 + tok) * a.mask_words : nullptr;
+    const int tree0 = __builtin_amdgcn_readfirstlane(sq.len - sq.n);      // the tree's first row (below 0: rows that the cache does not have)
+    const auto bits_from = [&](int key) { return tree_bits(words, a.mask_words, key - tree0) & first_bits(seen - key); };      // (TREE) of 32 keys from `key` on, those this lane's row sees
 
     // ---- HBM -> LDS copies: wavefront w copies rows w RPW .. of a stage; the swizzle is applied on the global side ----
     const int64_t kv_stride = a.kv_stride;
@@ -315,6 +321,21 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
         return half_max(t);
     };
     const auto mask_stage = [&](STile& S, int s) {      // keys of stage s that this lane's row does not see
+        if constexpr (TREE) {
+#pragma unroll
+            for (int h = 0; h < KB; ++h) {
+                const unsigned bits = bits_from(k0 + s * KT + 32 * h) >> (4 * hl);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+#if HG_RW_D == 128
+                    if (!(bits >> (8 * (i >> 2) + (i & 3)) & 1u)) S[i] = -INFINITY;
+#else
+                    if (!(bits >> (8 * (i >> 2) + (i & 3)) & 1u)) (h == 0 ? S.a : S.b)[i] = -INFINITY;
+#endif
+                }
+            }
+            return;
+        }
         const int hi = seen - (k0 + s * KT) - 4 * hl;   // row i of this lane is 8 (i / 4) + i % 4 + 4 hl (+ 32 in the second tile)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -593,7 +614,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
             } else {
                 row = q0 + key;
             }
-            if (key >= seen) continue;
+            if (key >= seen || (TREE && !(bits_from(key) & 1u))) continue;
             const unsigned char* const vr = Vh + row * kv_stride + 4 * hl * ES;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
@@ -669,7 +690,7 @@ __global__ __launch_bounds__(64 * NW, 2) void HG_RW_KERNEL(RaggedArgs a) {
         const unsigned id = (block < 2u * both ? block >> 1 : block - both) * 256u + in;
         if (id >= (is_tile ? tiles : rows)) return;
         if (is_tile) tile_workgroup<MODE>(a, id);
-        else rr::rows_workgroup<D, MODE == kCodes, true, NW>(a, id);
+        else rr::rows_workgroup<D, MODE == kCodes, true, NW, TREE>(a, id);
     }
 }
 
@@ -693,7 +714,9 @@ static hipError_t launch_mode(const RaggedArgs& a, hipStream_t s) {
 }
 
 hipError_t HG_RW_LAUNCH(const RaggedArgs& a, bool codes, hipStream_t s) {
+#if !HG_RW_TREE
     if (!a.pg.table) return launch_mode<kDense>(a, s);
+#endif
     return codes ? launch_mode<kCodes>(a, s) : launch_mode<kPaged>(a, s);
 }
 
