@@ -1,6 +1,8 @@
 // Attention of packed tokens of several sequences, each with its own number of new tokens and of keys: whole prompts
 // (hg_prompt_attn) and chunks behind a paged cache (hg_chunk_attn_paged).  Arguments and what the kernels share (gfx950 only).
 #pragma once
+#include <type_traits>
+
 #include "hg_internal.h"
 
 namespace hg {
@@ -54,12 +56,20 @@ struct RaggedArgs {
     // for each; it sees all rows before them.
     const uint32_t* masks;
     int mask_words;           // of a row of the masks
+    int tile_wgs, tile_jobs;  // workgroups that take tiles, and how many of them a KV head has
+    int balanced;             // 1 (up to 64 sequences): the workgroups choose the key ranges from the lengths (tree_jobs), at most tile_nsplit to a sequence and none shorter than
+                              // tile_chunk; the first leaves what it has chosen for the join in
+    int* tile_choice;
 };
 constexpr int kTile = 128;        // rows of a tile
 constexpr int kFewRows = 32;      // a remainder of more rows is a tile: beside tiles, and wherever a read of the cache for every 32 rows is what costs
 constexpr int kFewRowsAlone = 64; // ... in small calls of no more rows than these, where a launch without tiles is over sooner (plan_few_rows)
-// Of a sequence's n G rows, those that tiles take.
-__host__ __device__ inline int rows_in_tiles(int nrows, int few_rows) { return nrows % kTile <= few_rows ? nrows - nrows % kTile : nrows; }
+// Of a sequence's n G rows, those that tiles take.  Of a tree: all, or none.
+template <bool TREE = false>
+__host__ __device__ inline int rows_in_tiles(int nrows, int few_rows) {
+    if (TREE) return nrows <= few_rows ? 0 : nrows;
+    return nrows % kTile <= few_rows ? nrows - nrows % kTile : nrows;
+}
 
 // Workgroups that take what remains (whole groups of sixteen where they come in pairs)
 inline int64_t rows_grid(const RaggedArgs& a) {
@@ -68,7 +78,7 @@ inline int64_t rows_grid(const RaggedArgs& a) {
 }
 
 // Workgroups that take tiles
-inline int64_t tiles_grid(const RaggedArgs& a) { return (int64_t)a.tiles_all * a.Hkv * a.tile_nsplit; }
+inline int64_t tiles_grid(const RaggedArgs& a) { return a.masks ? a.tile_wgs : (int64_t)a.tiles_all * a.Hkv * a.tile_nsplit; }
 // ... and of a launch that has tiles: over a paged cache both kinds by turns, 256 of each
 inline int64_t ragged_grid(const RaggedArgs& a) { return a.few_rows == 0 ? tiles_grid(a) : ((tiles_grid(a) + 255) / 256 + (rows_grid(a) + 255) / 256) * 256; }
 // Workgroups of the join of parts: groups of D / 8 lanes to a row, and of a token's heads
@@ -172,7 +182,7 @@ __device__ __forceinline__ float value_if_not_finite(const unsigned char* e) {
 }
 
 // Of a tree's tokens, those that one of them sees, whose row of the masks has `n` words: bit i of the result stands for the i-th row from `j` on, counted from the tree's first.  Rows
-// before it are the context, which is seen; those that the masks have no bit for are not.
+// before it are the context, which is seen; those that the masks have no bit for are not.  (Words kept in registers from the start made nothing faster.)
 __device__ __forceinline__ unsigned tree_bits(const uint32_t* words, int n, int j) {
     if (j <= -32) return ~0u;
     const int w = j >> 5;
@@ -212,7 +222,7 @@ __device__ __forceinline__ bool tile_of_rank(const RaggedArgs& a, int rank, Ragg
     const int lane = threadIdx.x & 63;
     if (a.B <= 8) {
         const RaggedSeq own = ragged_seq(a, min(lane, a.B - 1));
-        const int tiles = lane < a.B ? (rows_in_tiles(own.take * a.G, a.few_rows) + kTile - 1) / kTile : 0;
+        const int tiles = lane < a.B ? (rows_in_tiles<TREE>(own.take * a.G, a.few_rows) + kTile - 1) / kTile : 0;
         const int size = (max(own.template seen<TREE>(0), 0) / kTile) * a.G + tiles;      // of the largest tile, in units of a tile's tokens
         int start = 0;
         for (int i = 0; i < a.B; ++i) {
@@ -244,8 +254,88 @@ __device__ __forceinline__ bool tile_of_rank(const RaggedArgs& a, int rank, Ragg
     seq = RaggedSeq{lo + at, __builtin_amdgcn_readlane(own.q0, at), __builtin_amdgcn_readlane(own.n, at), __builtin_amdgcn_readlane(own.take, at),
                     __builtin_amdgcn_readlane(own.len, at)};
     tile = number - first(seq.q0, seq.b);
-    return tile >= 0 && tile * kTile < rows_in_tiles(seq.take * a.G, a.few_rows);      // (tile < 0: offsets out of order)
+    return tile >= 0 && tile * kTile < rows_in_tiles<TREE>(seq.take * a.G, a.few_rows);      // (tile < 0: offsets out of order)
 }
+
+// ---- trees of up to 64 sequences: which workgroup takes which tile and which keys ----
+// The key ranges of a sequence of `len` keys where none is to be longer than `most`: equal ones, multiples of 64.
+__device__ __forceinline__ int tree_range(int len, int most) {
+    if (len <= most) return max(len, 1);
+    const int parts = (len + most - 1) / most;
+    return ((len + parts - 1) / parts + 63) / 64 * 64;
+}
+// Running sums over the lanes of a wavefront, this one's included, and what comes out at the last lane.
+template <class T>
+__device__ __forceinline__ T lane_scan(T x) {
+    const auto add = [&](auto ctrl, auto rows) {
+        x += __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+    };
+    add(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});      // row_shr:1, 2, 4, 8: within 16 lanes
+    add(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    add(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    add(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});      // row_bcast:15, row_bcast:31
+    add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+    return x;
+}
+template <class T>
+__device__ __forceinline__ T last_lane(T x) { return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63)); }
+
+// Every lane of a wavefront must call these; lane i looks after sequence i.
+struct TreeJobs {
+    RaggedSeq own;
+    int tiles, range, most;      // of this lane's sequence; `most` is the same for all
+    __device__ __forceinline__ void load(const RaggedArgs& a) {
+        const int lane = threadIdx.x & 63;
+        own = ragged_seq(a, min(lane, a.B - 1));
+        tiles = lane < a.B ? (rows_in_tiles<true>(own.take * a.G, a.few_rows) + kTile - 1) / kTile : 0;
+    }
+    // The longest range: of the longest sequence's halves, thirds, .. those with which the call is estimated to be over first.  us: a stage of 32 keys takes 0.95, 0.6 where a workgroup has
+    // its CU to itself, a workgroup 7 beside its stages, 512 run at a time, the longest first; parts are written and read at 4.5 TB/s, their join takes 6.
+    __device__ __forceinline__ void choose(const RaggedArgs& a, int D) {
+        most = 0x3fffffff;
+        if (a.tile_nsplit > 1) {
+            int longest = tiles > 0 ? own.len : 0;
+#pragma unroll
+            for (int d = 32; d > 0; d /= 2) longest = max(longest, __shfl_xor(longest, d));
+            const float per_key = 0.95f / 32.f * (D == 64 ? 0.5f : 1.f), Hkv = (float)a.Hkv, stages = last_lane(lane_scan((float)tiles * (float)own.len)) * Hkv * per_key;
+            const float part = (float)own.take * (float)a.Hq * (float)(D + 1) * (8.f / 4.5e6f);
+            float best = 0.f;
+            for (int k = 1;; k += k < 12 ? 1 : k / 3) {
+                const int c = max(((longest + k - 1) / k + 63) / 64 * 64, a.tile_chunk);
+                int q = (int)((float)own.len * __builtin_amdgcn_rcpf((float)c)), r = own.len - q * c;      // off by one at most: there are 64 ranges at most
+                if (r < 0) { --q; r += c; }
+                if (r >= c) { ++q; r -= c; }
+                const int p = k == 1 ? 1 : max(q + (r > 0 ? 1 : 0), 1), n = last_lane(lane_scan(tiles * p));
+                const float wgs = (float)n * Hkv, parts = last_lane(lane_scan(tiles > 0 && p > 1 ? (float)p * part : 0.f));
+                const float job = (k == 1 ? (float)longest : (float)c) * per_key;
+                float us = wgs <= 512.f ? job * (wgs <= 256.f ? 0.63f : 1.f) + 7.f : fmaxf(job + 7.f, (stages + 7.f * wgs) * (1.f / 512.f) + stages * __builtin_amdgcn_rcpf(wgs));
+                if (parts > 0.f) us += 6.f + parts;
+                if (k == 1 || (us < best && n <= a.tile_jobs)) {
+                    best = us;
+                    most = k == 1 ? 0x3fffffff : c;
+                }
+                if (c <= a.tile_chunk || k >= a.tile_nsplit) break;
+            }
+        }
+        range = tree_range(own.len, most);
+    }
+    // First of this lane's sequence's `n` jobs, where those of long ranges come first: by eighths of the longest, sequence after sequence in each.
+    __device__ __forceinline__ int first_of(int n) const {
+        int longest = n > 0 ? range : 0;
+#pragma unroll
+        for (int d = 32; d > 0; d /= 2) longest = max(longest, __shfl_xor(longest, d));
+        const int eighth = n > 0 ? min((int)(8.f * (float)range * __builtin_amdgcn_rcpf((float)longest)), 7) : -1;
+        int start = 0, before = 0;
+#pragma unroll 1
+        for (int k = 7; k >= 0; --k) {
+            const int mine = eighth == k ? n : 0, run = lane_scan(mine);
+            if (eighth == k) start = before + run - mine;
+            before += last_lane(run);
+        }
+        return start;
+    }
+};
 #endif
 // Tile numbers of a call.
 inline int64_t ragged_tiles(int64_t rows, int G, int B) { return rows * G / kTile + B; }

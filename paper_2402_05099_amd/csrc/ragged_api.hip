@@ -148,6 +148,33 @@ void plan_tiles(RaggedArgs& a, int D, Room& room) {
     split_keys(best, a.max_len, 1024, 64, (int64_t)a.rows * a.Hq, D, room, a.tile_nsplit, a.tile_chunk, a.tile_part_O, a.tile_part_L);
 }
 
+// Tiles of trees.  Up to 64 sequences: their workgroups choose the key ranges from the lengths (TreeJobs), among as many workgroups as there are here; what is decided here is whether there may be
+// several ranges, and room for their parts.  More sequences: as above.
+void plan_tree_tiles(RaggedArgs& a, int D, Room& room) {
+    a.balanced = a.B <= 64;
+    if (!a.balanced) {
+        plan_tiles(a, D, room);
+        a.tile_wgs = a.tiles_all * a.Hkv * a.tile_nsplit;
+        return;
+    }
+    const int64_t one = (int64_t)a.tiles_all * a.Hkv;      // (a sequence's last tile may be all but empty: at most B of them)
+    a.tile_wgs = (int)one;
+    a.tile_jobs = a.tiles_all;
+    if (one - (int64_t)a.B * a.Hkv >= 512 || a.max_len < 1024) {
+        a.balanced = one > 256;      // (else each has a CU to itself)
+        return;
+    }
+    Room rest = room;
+    int* const choice = reinterpret_cast<int*>(rest.floats >= 64 ? rest.take(64) : nullptr);
+    if (!choice) return;
+    split_keys(64, a.max_len, 256, 64, (int64_t)a.rows * a.Hq, D, rest, a.tile_nsplit, a.tile_chunk, a.tile_part_O, a.tile_part_L);
+    if (a.tile_nsplit == 1) return;
+    room = rest;
+    a.tile_choice = choice;
+    a.tile_jobs = std::max(a.tiles_all, 512 / a.Hkv);
+    a.tile_wgs = a.tile_jobs * a.Hkv;
+}
+
 // Choices of a call over packed rows, whose sequences have no more keys than there are tokens, whatever the caller's bound ...
 void plan_prompt(RaggedArgs& a, int max_len, int D, Room room) {
     a.max_len = std::min(max_len, a.rows);
@@ -158,7 +185,8 @@ bool plan_chunk(RaggedArgs& a, int max_len, int D, bool codes, Room room) {
     a.max_len = max_len;
     plan_few_rows(a, D, codes, room);
     const bool tiles = (int64_t)std::min(a.max_new, a.rows) * a.G > a.few_rows;
-    if (tiles) plan_tiles(a, D, room);
+    if (tiles && a.masks) plan_tree_tiles(a, D, room);
+    else if (tiles) plan_tiles(a, D, room);
     return tiles;
 }
 

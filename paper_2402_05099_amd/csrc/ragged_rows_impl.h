@@ -295,7 +295,7 @@ __device__ __forceinline__ void rows_workgroup(const RaggedArgs& a, unsigned id)
     const int n = min(max(((const_i32)(uintptr_t)a.q_off)[b + 1], q0), a.rows) - q0;
     const int len = max(min(((const_i32)(uintptr_t)a.lengths)[b], a.max_len), 0);
     const int nrows = min(n, a.max_new) * a.G;
-    const int row0 = rows_in_tiles(nrows, a.few_rows);
+    const int row0 = rows_in_tiles<TREE>(nrows, a.few_rows);
     if (!BOTH || nrows - row0 <= 16) rows_tile<D, CODES, 16, NW, TREE>(a, b, rt, sp, kvh, q0, n, len, row0, nrows);
     else rows_tile<D, CODES, 32, NW, TREE>(a, b, rt, sp, kvh, q0, n, len, row0, nrows);
 }

@@ -89,10 +89,11 @@ __global__ __launch_bounds__(256) void HG_JOIN_KERNEL(RaggedArgs a, int per_toke
         const RaggedSeq sq = ragged_seq(a, __builtin_amdgcn_readfirstlane(lo));
         const int tok = token - sq.q0, g = h - (int)a.by_group.of((unsigned)h) * a.G;
         if (tok < 0 || tok >= sq.take) return;
-        const int in_tiles = rows_in_tiles(sq.take * a.G, a.few_rows), r = tok * a.G + g;
-        mine = h < a.Hq && r < in_tiles && sq.template seen<HG_ROWS_TREE>((int)a.by_group.of((unsigned)(min(r / kTile * kTile + kTile, in_tiles) - 1))) > a.tile_chunk;
+        const int in_tiles = rows_in_tiles<HG_ROWS_TREE>(sq.take * a.G, a.few_rows), r = tok * a.G + g;
+        const int chunk = HG_ROWS_TREE && a.balanced ? tree_range(sq.len, *a.tile_choice) : a.tile_chunk;
+        mine = h < a.Hq && r < in_tiles && sq.template seen<HG_ROWS_TREE>((int)a.by_group.of((unsigned)(min(r / kTile * kTile + kTile, in_tiles) - 1))) > chunk;
         const int seen = mine ? sq.template seen<HG_ROWS_TREE>(tok) : 0;
-        parts = seen > 0 ? min((seen + a.tile_chunk - 1) / a.tile_chunk, a.tile_nsplit) : 0;
+        parts = seen > 0 ? min((seen + chunk - 1) / chunk, a.tile_nsplit) : 0;
         O = a.tile_part_O;
         L = a.tile_part_L;
         stride = (int64_t)a.rows * a.Hq;
@@ -102,7 +103,7 @@ __global__ __launch_bounds__(256) void HG_JOIN_KERNEL(RaggedArgs a, int per_toke
         if (at < a.part_rows) {
             const int bh = (int)a.by_most.of((unsigned)at), b = (int)a.by_heads.of((unsigned)bh), kvh = bh - b * a.Hkv;
             const RaggedSeq sq = ragged_seq(a, b);
-            const int r = rows_in_tiles(sq.take * a.G, a.few_rows) + ((int)at - bh * a.few_most), tok = (int)a.by_group.of((unsigned)r);
+            const int r = rows_in_tiles<HG_ROWS_TREE>(sq.take * a.G, a.few_rows) + ((int)at - bh * a.few_most), tok = (int)a.by_group.of((unsigned)r);
             mine = r < sq.take * a.G && sq.template seen<HG_ROWS_TREE>(sq.take - 1) > a.chunk;
             const int seen = mine ? sq.template seen<HG_ROWS_TREE>(tok) : 0;
             parts = seen > 0 ? min((seen + a.chunk - 1) / a.chunk, a.nsplit) : 0;

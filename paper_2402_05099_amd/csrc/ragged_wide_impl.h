@@ -122,7 +122,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
     unsigned char* const smem = rw_smem;
 
     // ---- which tile, which keys ----
-    int tile, kvh, sp;
+    int tile, kvh, sp, chunk = a.tile_chunk;
     RaggedSeq sq;
     {
         // Workgroups whose ids are equal modulo 8 run on one XCD: the tiles of a KV head go to one of them, or to as few as there are heads for, so
@@ -136,20 +136,36 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
             v = a.by_heads.of(id);
             kvh = (int)(id - v * (unsigned)a.Hkv);
         }
-        const int rank = (int)(v / (unsigned)a.tile_nsplit);
-        sp = (int)(v - (unsigned)rank * (unsigned)a.tile_nsplit);
-        if (!tile_of_rank<TREE>(a, rank, sq, tile)) return;
+        if (TREE && a.balanced) {      // longest ranges first; the tiles that share one next to each other
+            TreeJobs jobs;
+            jobs.load(a);
+            jobs.choose(a, D);
+            if (id == 0 && a.tile_choice && threadIdx.x == 0) *a.tile_choice = jobs.most;
+            const int parts = (max(jobs.own.len, 1) + jobs.range - 1) / jobs.range, n = jobs.tiles * parts, start = jobs.first_of(n);
+            const unsigned long long at = __ballot((int)v >= start && (int)v < start + n);
+            if (at == 0) return;
+            const int b = __builtin_ctzll(at), t = __builtin_amdgcn_readlane(jobs.tiles, b), in = (int)v - __builtin_amdgcn_readlane(start, b);
+            sq = RaggedSeq{b, __builtin_amdgcn_readlane(jobs.own.q0, b), __builtin_amdgcn_readlane(jobs.own.n, b), __builtin_amdgcn_readlane(jobs.own.take, b),
+                           __builtin_amdgcn_readlane(jobs.own.len, b)};
+            chunk = __builtin_amdgcn_readlane(jobs.range, b);
+            sp = in / t;
+            tile = in - sp * t;
+        } else {
+            const int rank = (int)(v / (unsigned)a.tile_nsplit);
+            sp = (int)(v - (unsigned)rank * (unsigned)a.tile_nsplit);
+            if (!tile_of_rank<TREE>(a, rank, sq, tile)) return;
+        }
     }
     const int b = __builtin_amdgcn_readfirstlane(sq.b);
-    const int nrows = __builtin_amdgcn_readfirstlane(rows_in_tiles(sq.take * a.G, a.few_rows)), row0 = tile * kTileRows;      // rows that tiles take
+    const int nrows = __builtin_amdgcn_readfirstlane(rows_in_tiles<TREE>(sq.take * a.G, a.few_rows)), row0 = tile * kTileRows;      // rows that tiles take
     const int q0 = __builtin_amdgcn_readfirstlane(sq.q0);
     // keys that the sequence's first token sees; of a tree, that all its tokens see
     const int before = __builtin_amdgcn_readfirstlane(TREE ? max(sq.len - sq.n, 0) : sq.len - (sq.n - 1));
     const int tid = threadIdx.x, l = tid & 63, lq = l & 31, hl = l >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const auto token_of = [&](int r) { return (int)a.by_group.of((unsigned)r); };
-    const int k0 = sp * a.tile_chunk;
-    const int k_all = __builtin_amdgcn_readfirstlane(TREE ? sq.len : before + token_of(min(row0 + kTileRows, nrows) - 1)), ke = min(k_all, k0 + a.tile_chunk);      // keys [k0, ke) of k_all
+    const int k0 = sp * chunk;
+    const int k_all = __builtin_amdgcn_readfirstlane(TREE ? sq.len : before + token_of(min(row0 + kTileRows, nrows) - 1)), ke = min(k_all, k0 + chunk);      // keys [k0, ke) of k_all
     const int nst = ke > k0 ? (ke - k0 + KT - 1) / KT : 0, nfull = ke > k0 ? (ke - k0) / KT : 0;
     if (sp > 0 && nst == 0) return;      // (the join looks at no part that starts behind a row's keys)
     // stages from here on have keys that some row of the tile does not see
@@ -626,7 +642,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
     }
     const float ltot = half_sum(lsum), lr = half_sum(lround);
     const float inv = lr == 0.f ? 0.f : a.v_scale / lr;      // (a row whose scores are NaN stays NaN)
-    const bool in_parts = k_all > a.tile_chunk;      // (a tile of one range has the result itself)
+    const bool in_parts = k_all > chunk;      // (a tile of one range has the result itself)
     const int64_t row_at = (int64_t)(q0 + tok) * a.Hq + head;
     if (rv && hl == 0) {
         const float lse = ltot == 0.f ? -INFINITY : (mc + __log2f(ltot)) * kLn2;
@@ -684,7 +700,7 @@ __global__ __launch_bounds__(64 * NW, 2) void HG_RW_KERNEL(RaggedArgs a) {
     if constexpr (MODE == kDense) {
         tile_workgroup<MODE>(a, blockIdx.x);
     } else {
-        const unsigned tiles = (unsigned)a.tiles_all * (unsigned)a.Hkv * (unsigned)a.tile_nsplit, rows = a.row_wgs;
+        const unsigned tiles = TREE ? (unsigned)a.tile_wgs : (unsigned)a.tiles_all * (unsigned)a.Hkv * (unsigned)a.tile_nsplit, rows = a.row_wgs;
         const unsigned both = min((tiles + 255u) / 256u, (rows + 255u) / 256u), block = blockIdx.x >> 8, in = blockIdx.x & 255u;
         const bool is_tile = block < 2u * both ? (block & 1u) == 0u : tiles > rows;
         const unsigned id = (block < 2u * both ? block >> 1 : block - both) * 256u + in;

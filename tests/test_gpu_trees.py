@@ -169,6 +169,35 @@ def test_tokens_and_rows_behind_the_bounds(D, codes):
     run_attn([(300, 40), (20, 7), (90, 64)], (8, 2), D, codes=codes, max_len=100)
 
 
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B", [1, 2, 63, 64, 65, 130])
+def test_key_ranges_of_many_sequences(B, D, codes):
+    """Up to 64 sequences the workgroups choose the ranges from the lengths; long ones among short and empty ones, trees that are tiles among those that are few rows."""
+    pairs = [(max(n, (1500 if b % 7 == 0 else 40) + 13 * b % 300), n) for b in range(B) for n in [(40, 3, 0, 17, 64, 9, 33)[b % 7]]]
+    run_attn(pairs, (8, 2), D, codes=codes, mib=64)
+    if B < 64:
+        run_attn(pairs, (8, 2), D, codes=codes, mib=1, kind="any")
+
+
+def test_bounds_that_are_a_capacity():
+    """max_new and max_len far above what there is, as a captured step has them."""
+    pairs = [(2000, 40), (0, 0), (300, 33), (1100, 64), (5, 1)]
+    Q, Qd, off, T, lens, counts, sees, masks, kv, keys, values = tree_case(pairs, 16, 2, 128)
+    wide = torch.full((len(pairs), 8192), -1, dtype=torch.int32, device=DEV)
+    wide[:, :kv.page_table.shape[1]] = kv.page_table
+    kv = hb.PagedKV(K=kv.K, V=kv.V, page_table=wide, page_size=16)
+    Oref, Lref = plain.attention(Q, off, sees, keys, values, lens)
+    for mib in (0, 16, 256):
+        ctx = context(mib)
+        O, L = torch.full((T, 16, 128), 7.0, device=DEV), torch.full((T, 16), 7.0, device=DEV)
+        bits = torch.cat([masks, torch.zeros(T, 32 - masks.shape[1], dtype=torch.int32, device=DEV)], 1).contiguous()
+        hb.hg_tree_attn_paged(ctx, Qd, i32(off.tolist()), bits, kv, i32(lens), 1024, 131072, O, L)
+        torch.cuda.synchronize()
+        check_rows(O, L, Oref, Lref, f"bounds of a capacity, {mib} MiB", 7.0)
+        ctx.close()
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_results_in_fp32_without_lse_peaked(D):
     run_attn(MIXED, (8, 2), D, lse=False, scale=0.3)
