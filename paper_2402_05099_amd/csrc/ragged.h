@@ -292,17 +292,21 @@ struct TreeJobs {
     }
     // The longest range: of the longest sequence's halves, thirds, .. those with which the call is estimated to be over first.  us: a stage of 32 keys takes 0.95, 0.6 where a workgroup has
     // its CU to itself, a workgroup 7 beside its stages, 512 run at a time, the longest first; parts are written and read at 4.5 TB/s, their join takes 6.
-    __device__ __forceinline__ void choose(const RaggedArgs& a, int D) {
+    // Of a workgroup of four wavefronts, each of which looks at every fourth candidate (0.4 us each); `meet`: 32 bytes of LDS.
+    __device__ __forceinline__ void choose(const RaggedArgs& a, int D, unsigned char* meet) {
         most = 0x3fffffff;
         if (a.tile_nsplit > 1) {
+            const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
             int longest = tiles > 0 ? own.len : 0;
 #pragma unroll
             for (int d = 32; d > 0; d /= 2) longest = max(longest, __shfl_xor(longest, d));
             const float per_key = 0.95f / 32.f * (D == 64 ? 0.5f : 1.f), Hkv = (float)a.Hkv, stages = last_lane(lane_scan((float)tiles * (float)own.len)) * Hkv * per_key;
             const float part = (float)own.take * (float)a.Hq * (float)(D + 1) * (8.f / 4.5e6f);
-            float best = 0.f;
-            for (int k = 1;; k += k < 12 ? 1 : k / 3) {
-                const int c = max(((longest + k - 1) / k + 63) / 64 * 64, a.tile_chunk);
+            float best = 1e30f;
+            int last = 0x3fffffff;      // the candidate before
+            for (int i = w; i < 18 && last > a.tile_chunk; i += 4) {
+                const int k = i < 12 ? i + 1 : (int)(0x403125'1c1510ull >> (8 * (i - 12)) & 255u);
+                const int c = max(((int)((float)longest * __builtin_amdgcn_rcpf((float)k)) / 64 + 1) * 64, a.tile_chunk);
                 int q = (int)((float)own.len * __builtin_amdgcn_rcpf((float)c)), r = own.len - q * c;      // off by one at most: there are 64 ranges at most
                 if (r < 0) { --q; r += c; }
                 if (r >= c) { ++q; r -= c; }
@@ -311,12 +315,22 @@ struct TreeJobs {
                 const float job = (k == 1 ? (float)longest : (float)c) * per_key;
                 float us = wgs <= 512.f ? job * (wgs <= 256.f ? 0.63f : 1.f) + 7.f : fmaxf(job + 7.f, (stages + 7.f * wgs) * (1.f / 512.f) + stages * __builtin_amdgcn_rcpf(wgs));
                 if (parts > 0.f) us += 6.f + parts;
-                if (k == 1 || (us < best && n <= a.tile_jobs)) {
+                if (us < best && (k == 1 || n <= a.tile_jobs)) {
                     best = us;
                     most = k == 1 ? 0x3fffffff : c;
                 }
-                if (c <= a.tile_chunk || k >= a.tile_nsplit) break;
+                last = k == 1 ? last : c;
             }
+            float* const us_of = reinterpret_cast<float*>(meet);
+            int* const most_of = reinterpret_cast<int*>(meet + 16);
+            if ((threadIdx.x & 63) == 0) { us_of[w] = best; most_of[w] = most; }
+            __syncthreads();
+            best = us_of[0];
+            most = most_of[0];
+#pragma unroll
+            for (int i = 1; i < 4; ++i)
+                if (us_of[i] < best) { best = us_of[i]; most = most_of[i]; }
+            most = __builtin_amdgcn_readfirstlane(most);
         }
         range = tree_range(own.len, most);
     }

@@ -139,7 +139,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
         if (TREE && a.balanced) {      // longest ranges first; the tiles that share one next to each other
             TreeJobs jobs;
             jobs.load(a);
-            jobs.choose(a, D);
+            jobs.choose(a, D, smem + lds_bytes(MODE) + 16);
             if (id == 0 && a.tile_choice && threadIdx.x == 0) *a.tile_choice = jobs.most;
             const int parts = (max(jobs.own.len, 1) + jobs.range - 1) / jobs.range, n = jobs.tiles * parts, start = jobs.first_of(n);
             const unsigned long long at = __ballot((int)v >= start && (int)v < start + n);
@@ -712,7 +712,7 @@ __global__ __launch_bounds__(64 * NW, 2) void HG_RW_KERNEL(RaggedArgs a) {
 
 template <int MODE>
 static hipError_t launch_mode(const RaggedArgs& a, hipStream_t s) {
-    constexpr int bytes = MODE == kDense ? lds_bytes(MODE) + 16 : std::max(lds_bytes(MODE) + 16, rr::rows_lds<D, MODE == kCodes, true>(NW));
+    constexpr int bytes = MODE == kDense ? lds_bytes(MODE) + 16 : std::max(lds_bytes(MODE) + 16 + (TREE ? 32 : 0), rr::rows_lds<D, MODE == kCodes, true>(NW));
     static_assert(bytes <= 81920, "two workgroups to a CU");
     const int64_t grid = ragged_grid(a);
     if (grid >= (1LL << 31)) return hipErrorInvalidValue;
