@@ -180,6 +180,16 @@ def test_key_ranges_of_many_sequences(B, D, codes):
         run_attn(pairs, (8, 2), D, codes=codes, mib=1, kind="any")
 
 
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_tiles_of_sequences_without_enough_rows(D, codes):
+    """Trees of more tokens than the cache has rows (a step that ran out of pages): the rows that are there are the last tokens', some or all tokens see nothing."""
+    for kind in ("tree", "any"):
+        run_attn([(0, 64), (5, 64), (64, 64), (33, 100), (70, 64)], (8, 2), D, codes=codes, kind=kind)
+    run_attn([(0, 64), (5, 64), (1500, 64), (33, 100)], (8, 2), D, codes=codes, mib=64)
+    run_attn([(40, 9), (70, 64), (0, 3)], (8, 2), D, codes=codes, max_len=0)
+
+
 def test_bounds_that_are_a_capacity():
     """max_new and max_len far above what there is, as a captured step has them."""
     pairs = [(2000, 40), (0, 0), (300, 33), (1100, 64), (5, 1)]
@@ -284,6 +294,60 @@ def test_tree_attention_in_a_graph_and_on_a_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    ctx.close()
+
+
+def test_a_whole_step_in_a_graph():
+    """Masks, attention, verification and the move captured on a stream of their own, replayed with eager work and other lengths between: the results of eager calls."""
+    g, r = torch.Generator().manual_seed(5), np.random.default_rng(5)
+    Hq, Hkv, D, ps, V, B, n = 8, 2, 128, 16, 3000, 6, 70
+    T = B * n
+    Kp, Vp, table, _, _ = make_cache(g, [1300] * B, Hkv, D, ps, False)
+    first = [(Kp.clone(), Vp.clone()) for _ in range(2)]
+    Q = rand(g, T, Hq, D).to(DEV)
+    parents, off = i32(sum([random_parents(r, n, 4) for _ in range(B)], [])), i32(list(range(0, T + 1, n)))
+    target, draft = torch.softmax(4 * torch.randn(T, V, generator=g), 1).to(DEV), torch.softmax(4 * torch.randn(T, V, generator=g), 1).to(DEV)
+    tokens, u, un = torch.multinomial(draft, 1)[:, 0].to(torch.int32), torch.rand(T, generator=g).to(DEV), torch.rand(B, generator=g).to(DEV)
+    lens = [i32([n + int(x) for x in r.integers(0, 1230, B)]) for _ in range(4)]
+    ctx = context(64)
+
+    def step(kv, length, out):
+        hb.hg_tree_masks(ctx, parents, off, n, out[0], out[1])
+        hb.hg_tree_attn_paged(ctx, Q, off, out[0], kv[0], length, n, 1300, out[2], out[3])
+        hb.hg_tree_verify(ctx, tokens, parents, off, n, target, draft, u, un, out[4], out[5], out[6])
+        hb.hg_tree_keep_paged(ctx, kv, off, out[4], out[5], length, n, out[7])
+
+    def buffers():
+        e = lambda *shape, dtype=torch.int32: torch.zeros(*shape, dtype=dtype, device=DEV)  # noqa: E731
+        return [e(T, 3), e(T), e(T, Hq, D, dtype=torch.bfloat16), e(T, Hq, dtype=torch.float32), e(T), e(B), e(B), e(B)]
+
+    pools = [(k.clone(), v.clone()) for k, v in first]
+    kv = [hb.PagedKV(k, v, table, ps) for k, v in pools]
+    out, length = buffers(), lens[0].clone()
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    ctx.set_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        step(kv, length, out)
+    ctx.set_stream(None)
+    for x in lens:
+        again = [(k.clone(), v.clone()) for k, v in first]
+        want = buffers()
+        step([hb.PagedKV(k, v, table, ps) for k, v in again], x, want)
+        for (k, v), (k0, v0) in zip(pools, first):
+            k.copy_(k0)
+            v.copy_(v0)
+        length.copy_(x)
+        for o in out:
+            o.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b)
+        for a, b in zip(sum(pools, ()), sum(again, ())):
+            assert torch.equal(a.view(torch.int16), b.view(torch.int16))
     ctx.close()
 
 
