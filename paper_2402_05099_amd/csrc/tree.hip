@@ -112,12 +112,15 @@ struct Group;
 template <>
 struct Group<float> {
     unsigned v[8];
-    __device__ __forceinline__ void load(const float* row, int g, int V) {
+    __device__ __forceinline__ void load_full(const float* row, int g) {
         struct __attribute__((packed, aligned(4))) Piece { unsigned v[4]; };
-        if (kGroup * g + kGroup <= V) {
-            const Piece lo = *reinterpret_cast<const Piece*>(row + kGroup * g), hi = *reinterpret_cast<const Piece*>(row + kGroup * g + 4);
+        const Piece lo = *reinterpret_cast<const Piece*>(row + kGroup * g), hi = *reinterpret_cast<const Piece*>(row + kGroup * g + 4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i] = lo.v[i]; v[4 + i] = hi.v[i]; }
+        for (int i = 0; i < 4; ++i) { v[i] = lo.v[i]; v[4 + i] = hi.v[i]; }
+    }
+    __device__ __forceinline__ void load(const float* row, int g, int V) {
+        if (kGroup * g + kGroup <= V) {
+            load_full(row, g);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = kGroup * g + i < V ? bits_of(row[kGroup * g + i]) : 0u;
@@ -132,12 +135,15 @@ struct Group<float> {
 template <>
 struct Group<uint16_t> {
     unsigned v[4];
-    __device__ __forceinline__ void load(const uint16_t* row, int g, int V) {
+    __device__ __forceinline__ void load_full(const uint16_t* row, int g) {
         struct __attribute__((packed, aligned(2))) Piece { unsigned v[4]; };
-        if (kGroup * g + kGroup <= V) {
-            const Piece p = *reinterpret_cast<const Piece*>(row + kGroup * g);
+        const Piece p = *reinterpret_cast<const Piece*>(row + kGroup * g);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = p.v[i];
+        for (int i = 0; i < 4; ++i) v[i] = p.v[i];
+    }
+    __device__ __forceinline__ void load(const uint16_t* row, int g, int V) {
+        if (kGroup * g + kGroup <= V) {
+            load_full(row, g);
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -254,21 +260,40 @@ __global__ __launch_bounds__(NT) void tree_verify_kernel(TreeVerifyArgs a) {
     };
     const auto total = [](const double (&x)[kGroup]) -> double { return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7])); };
     const int groups = (V + kGroup - 1) / kGroup, piece = (groups + NW - 1) / NW;
+    const int full = V / kGroup;      // groups without an end of the row in them
     const auto sum_up = [&]() {      // this wavefront's piece
-        const int to = min((w + 1) * piece, groups);
+        const T* const prow = target + (int64_t)(sq.q0 + cur) * a.target_stride;
+        const T* const qrow = DRAFT ? draft + (int64_t)(sq.q0 + cur) * a.draft_stride : nullptr;
+        const int to = min((w + 1) * piece, full);
         double all = 0.0;
-        for (int g0 = w * piece + lane; g0 < to; g0 += 64 * U) {
+        for (int first = w * piece; first < to; first += 64 * U) {
             Group<T> p[U], q[U];
+            // (every lane loads, those past the end the last group once more: a load under a condition of a lane's own is waited for before the next)
 #pragma unroll
-            for (int k = 0; k < U; ++k)
-                if (g0 + 64 * k < to) load(g0 + 64 * k, p[k], q[k]);
+            for (int k = 0; k < U; ++k) p[k].load_full(prow, min(first + 64 * k + lane, to - 1));
+            if constexpr (DRAFT) {
+                if (c != 0.0) {
 #pragma unroll
-            for (int k = 0; k < U; ++k)
-                if (g0 + 64 * k < to) {
-                    double x[kGroup];
-                    weights(g0 + 64 * k, p[k], q[k], x);
-                    all += total(x);
+                    for (int k = 0; k < U; ++k) q[k].load_full(qrow, min(first + 64 * k + lane, to - 1));
+                } else {
+#pragma unroll
+                    for (int k = 0; k < U; ++k) q[k].clear();
                 }
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                if (first + 64 * k >= to) break;
+                double x[kGroup];
+                weights(min(first + 64 * k + lane, to - 1), p[k], q[k], x);
+                all += first + 64 * k + lane < to ? total(x) : 0.0;
+            }
+        }
+        if (full < groups && full / piece == w && lane == 0) {      // what is left behind them
+            Group<T> p, q;
+            double x[kGroup];
+            load(full, p, q);
+            weights(full, p, q, x);
+            all += total(x);
         }
         all = wave_sum(all);
         if (lane == 0) s_sum[w] = all;
