@@ -57,7 +57,7 @@
  *     at the same time, be they enqueued on two streams, replayed from a graph or on two branches of one: such calls
  *     spoil each other's results (but no later call's).  hg_set_stream does not order anything by itself.  A call whose
  *     result comes out in one piece uses no workspace and may run beside any other: hg_merge, hg_kv_append*, hg_page_slots,
- *     hg_kv_write_paged, hg_tree_masks, hg_tree_verify, hg_tree_keep_paged, and hg_hydragen_attn on packed bf16 rows with little work (see HG_OPT_FUSED_KERNEL), which also needs none.
+ *     hg_kv_write_paged, hg_tree_masks, hg_tree_keep_paged, hg_tree_verify over vocabularies below 98304, and hg_hydragen_attn on packed bf16 rows with little work (see HG_OPT_FUSED_KERNEL), which also needs none.
  *   - Calls in flight, and graphs that hold calls, may outlive their context (not the workspace they were given).
  */
 #ifndef HYDRAGEN_H
@@ -358,7 +358,8 @@ int hg_kv_write_paged(hg_ctx* ctx, const void* Knew, const void* Vnew, int64_t s
  *   with draft: p_0 = p; x stands if u q(x) < p_k(x), k being the siblings refused before; a refusal leaves p_k+1 = max(0, p_k - q) / its sum.
  *   draft NULL (each drafted token counts as certain): x stands if u < p_k(x); a refusal leaves p_k+1 = p_k without x, / its sum.
  * next_tokens[b] is drawn from the p_k that is left at the last token that stands: the smallest y with p_k(0) + .. + p_k(y) > u_next[b] (times the sum as it is: rows need not sum to one exactly).
- * Sums are taken in 64 bits.  The kernels use p_k = max(0, p - c_k q) / S_k, c_0 = 0, S_0 = 1, c_k+1 = c_k + S_k, S_k+1 = sum of max(0, p - c_k+1 q), which is the same.  Entries that are not positive finite
+ * Sums are taken in 64 bits; the first over a vocabulary of 98304 tokens or more by several workgroups, if the workspace has room for it (at most 2072 bytes a sequence; else it
+ * is not used).  The kernels use p_k = max(0, p - c_k q) / S_k, c_0 = 0, S_0 = 1, c_k+1 = c_k + S_k, S_k+1 = sum of max(0, p - c_k+1 q), which is the same.  Entries that are not positive finite
  * numbers count as 0, so do tokens outside [0, V).  Where nothing is left (rounding), the draw is from p; where p has nothing either, next_tokens[b] is -1.
  *   p_dtype = HG_TOKENS (greedy decoding): target is int32 [rows], what the target says behind each token; a token stands if it is what its parent's row says, next_tokens[b] is what the last
  * one's says.  V, draft, u and u_next are not looked at.

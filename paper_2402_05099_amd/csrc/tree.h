@@ -15,6 +15,11 @@ struct TreeMaskArgs {
 };
 hipError_t launch_tree_masks(const TreeMaskArgs& a, hipStream_t s);
 
+constexpr int kVerifySplits = 64;      // workgroups that share the first sum of a sequence, at most
+struct TreeVerifyState {               // where the walk stands when that sum is needed
+    int cur, t, kept, more;            // more: for the next sibling; else for the next token
+    double c;
+};
 struct TreeVerifyArgs {
     const int32_t* tokens;
     const int32_t* parents;
@@ -28,7 +33,12 @@ struct TreeVerifyArgs {
     int32_t* path;
     int32_t* accepted;
     int32_t* next;
+    int nsplit;               // > 1: so many workgroups to a sequence for the first sum
+    TreeVerifyState* state;   // [B]
+    double* parts;            // [B][4 nsplit]
 };
+// Bytes that it takes
+inline size_t verify_bytes(int B, int nsplit) { return (size_t)B * (sizeof(TreeVerifyState) + (size_t)nsplit * 4 * sizeof(double)); }
 hipError_t launch_tree_verify(const TreeVerifyArgs& a, int p_dtype, hipStream_t s);
 
 struct TreeKeepArgs {

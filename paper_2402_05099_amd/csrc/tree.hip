@@ -170,32 +170,46 @@ __device__ __forceinline__ double wave_sum(double x) {
 // sibling follows a refused one, and once for the next token: every wavefront sums one piece of the row, and the piece in which the running sum passes the random number is read once more, a few
 // elements by every thread.
 // What bounds it is latency, and for large vocabularies the one CU that reads a row.
-template <class T, bool DRAFT, int NT>
+//
+// One CU takes in some 40 GB/s of a row and converts as much, so where rows are long and sequences few the first of these sums, which for chains and without drafts is the only one, is
+// shared out: kFirst, `nsplit` workgroups of four wavefronts to a sequence, walk as far as that sum, each for itself, and take a piece of it per wavefront; kRest goes on from there.
+enum { kWhole, kFirst, kRest };
+constexpr int kFirstWaves = 4;
+template <class T, bool DRAFT, int NT, int PART>
 __global__ __launch_bounds__(NT) void tree_verify_kernel(TreeVerifyArgs a) {
     constexpr int NW = NT / 64;
+    static_assert(PART != kFirst || NW == kFirstWaves, "");
     constexpr int U = 64 / (sizeof(Group<T>) / 4 * (DRAFT ? 2 : 1));      // groups of a lane that are in flight: 64 registers of them
     constexpr int kFilter = 1 << 14;      // places that say whether a group of elements may have a refused token
     __shared__ int s_up[HG_MAX_TREE], s_tok[HG_MAX_TREE];
     __shared__ float s_u[HG_MAX_TREE], s_p[HG_MAX_TREE], s_q[DRAFT ? HG_MAX_TREE : 1];
     __shared__ unsigned s_filter[DRAFT ? 1 : kFilter / 32];
     __shared__ double s_sum[NW], s_cut[NW], s_c;
+    __shared__ double s_part[PART == kRest ? kVerifySplits * kFirstWaves : 1];
     __shared__ int s_cur, s_more, s_kept, s_refused;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int b = (int)blockIdx.x;
+    const int b = PART == kFirst ? (int)blockIdx.x / a.nsplit : (int)blockIdx.x, slice = PART == kFirst ? (int)blockIdx.x - b * a.nsplit : 0;
+    const int parts = PART == kWhole ? NW : a.nsplit * kFirstWaves;
     const TreeSeq sq = tree_seq(a.q_off, a.rows, b);
     const int take = min(sq.n, a.max_new), V = a.V;
     if (take == 0) {
-        if (tid == 0) { a.accepted[b] = 0; a.next[b] = -1; }
+        if (PART != kFirst && tid == 0) { a.accepted[b] = 0; a.next[b] = -1; }
         return;
     }
+    TreeVerifyState from_first{0, 1, 1, 1, 0.0};
+    if constexpr (PART == kRest) {
+        from_first = a.state[b];
+        for (int i = tid; i < parts; i += NT) s_part[i] = a.parts[(int64_t)b * parts + i];
+    }
+    const bool walk_on = from_first.more != 0;
     const T* const target = static_cast<const T*>(a.target);
     const T* const draft = static_cast<const T*>(a.draft);
-    for (int t = tid; t < take; t += NT) {
+    for (int t = tid; t < (DRAFT && !walk_on ? 0 : take); t += NT) {
         int up = a.parents[sq.q0 + t];
         const int x = a.tokens[sq.q0 + t];
         if (up < 0 || up >= t) up = -1;
         float p = 0.f, q = 0.f;
-        if (up >= 0 && x >= 0 && x < V) {
+        if (walk_on && up >= 0 && x >= 0 && x < V) {
             p = element(target + (int64_t)(sq.q0 + up) * a.target_stride, x);
             if constexpr (DRAFT) q = element(draft + (int64_t)(sq.q0 + up) * a.draft_stride, x);
         }
@@ -261,12 +275,12 @@ __global__ __launch_bounds__(NT) void tree_verify_kernel(TreeVerifyArgs a) {
     const auto total = [](const double (&x)[kGroup]) -> double { return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7])); };
     const int groups = (V + kGroup - 1) / kGroup, piece = (groups + NW - 1) / NW;
     const int full = V / kGroup;      // groups without an end of the row in them
-    const auto sum_up = [&]() {      // this wavefront's piece
+    const auto sum_up = [&](int which, int piece) -> double {      // of one piece of the row, by a wavefront
         const T* const prow = target + (int64_t)(sq.q0 + cur) * a.target_stride;
         const T* const qrow = DRAFT ? draft + (int64_t)(sq.q0 + cur) * a.draft_stride : nullptr;
-        const int to = min((w + 1) * piece, full);
+        const int to = min((which + 1) * piece, full);
         double all = 0.0;
-        for (int first = w * piece; first < to; first += 64 * U) {
+        for (int first = which * piece; first < to; first += 64 * U) {
             Group<T> p[U], q[U];
             // (every lane loads, those past the end the last group once more: a load under a condition of a lane's own is waited for before the next)
 #pragma unroll
@@ -288,25 +302,37 @@ __global__ __launch_bounds__(NT) void tree_verify_kernel(TreeVerifyArgs a) {
                 all += first + 64 * k + lane < to ? total(x) : 0.0;
             }
         }
-        if (full < groups && full / piece == w && lane == 0) {      // what is left behind them
+        if (full < groups && full / piece == which && lane == 0) {      // what is left behind them
             Group<T> p, q;
             double x[kGroup];
             load(full, p, q);
             weights(full, p, q, x);
             all += total(x);
         }
-        all = wave_sum(all);
-        if (lane == 0) s_sum[w] = all;
+        return wave_sum(all);
+    };
+    // ... of NW or of `parts` pieces
+    const auto sum_whole = [&]() {
+        const double x = sum_up(w, piece);
+        if (lane == 0) s_sum[w] = x;
     };
 
     // ---- the walk ----
-    int t = 1, kept = 1;
+    int t = from_first.t, kept = from_first.kept;
     double S = 1.0;
     bool stale = false;      // S has to be taken before the next test
+    if constexpr (PART == kRest) {
+        cur = from_first.cur;
+        c = from_first.c;
+        S = 0.0;
+        for (int i = lane; i < parts; i += 64) S += s_part[i];
+        S = wave_sum(S);
+    }
+    const double first_sum = S;
     while (true) {
         if (w == 0) {
             bool more = false;
-            while (t < take) {
+            while (walk_on && t < take) {
                 // 64 tokens, those before t among them that no one asks for any more
                 const int t0 = t & ~63, at = min(t0 + lane, take - 1);
                 const int up = t0 + lane < take ? s_up[at] : -1, x = s_tok[at];
@@ -337,7 +363,7 @@ __global__ __launch_bounds__(NT) void tree_verify_kernel(TreeVerifyArgs a) {
                         yes = pt > 0.0 && ut * S < pt;
                     }
                     if (yes) {
-                        if (lane == 0) a.path[sq.q0 + kept] = t;
+                        if (lane == 0 && slice == 0) a.path[sq.q0 + kept] = t;
                         ++kept;
                         cur = t;
                         c = 0.0;
@@ -367,27 +393,35 @@ __global__ __launch_bounds__(NT) void tree_verify_kernel(TreeVerifyArgs a) {
                 if (lane == 0) s_refused = n;
             }
             if (lane == 0) { s_cur = cur; s_c = c; s_more = more; s_kept = kept; }
+            if (PART == kFirst && slice == 0 && lane == 0) a.state[b] = TreeVerifyState{cur, t, kept, more, c};
         }
         __syncthreads();
         cur = __builtin_amdgcn_readfirstlane(s_cur);
         c = s_c;
-        if (!s_more) break;
-        sum_up();
+        if (PART == kFirst || !s_more) break;
+        sum_whole();
         __syncthreads();
         S = 0.0;
         for (int i = 0; i < NW; ++i) S += s_sum[i];
         stale = false;
+    }
+    without = !DRAFT && s_refused > 0;
+    if constexpr (PART == kFirst) {
+        const int which = slice * NW + w;
+        const double x = sum_up(which, (groups + parts - 1) / parts);
+        if (lane == 0) a.parts[(int64_t)b * parts + which] = x;
+        return;
     }
     kept = s_kept;
     for (int i = tid; i < take; i += NT)
         if (i == 0 || i >= kept) a.path[sq.q0 + i] = i == 0 ? 0 : -1;
 
     // ---- the next token ----
-    without = !DRAFT && s_refused > 0;
     bool whole = DRAFT ? c == 0.0 : !without;      // the draw is from p as it is
-    double all;
-    while (true) {
-        sum_up();
+    bool shared_out = PART == kRest && !walk_on && first_sum > 0.0;      // the sums of the row's pieces are there
+    double all = first_sum;
+    while (!shared_out) {
+        sum_whole();
         __syncthreads();
         all = 0.0;
         for (int i = 0; i < NW; ++i) all += s_sum[i];
@@ -415,15 +449,24 @@ __global__ __launch_bounds__(NT) void tree_verify_kernel(TreeVerifyArgs a) {
         const unsigned long long p = __ballot(some && passes), s = __ballot(some);
         return p ? __builtin_ctzll(p) : s ? 63 - __builtin_clzll(s) : -1;
     };
-    const auto cut = [&](const double* sums, double before, double& base) -> int {      // which of the wavefronts' sums, and the sum of those before it
-        const double own = lane < NW ? sums[lane] : 0.0, run = before + scan(own);
-        const int at = max(pick(own > 0.0, run > aim), 0);
-        base = __shfl(run - own, at);
+    const auto cut = [&](const double* sums, int n, double before, double& base) -> int {      // which of n sums, and the sum of those before it
+        int at = 0;
+        base = before;
+        for (int i0 = 0; i0 < n; i0 += 64) {
+            const double own = i0 + lane < n ? sums[i0 + lane] : 0.0, run = before + scan(own);
+            const int i = pick(own > 0.0, run > aim);
+            if (i >= 0) {
+                at = i0 + i;
+                base = __shfl(run - own, i);
+            }
+            if (__any(own > 0.0 && run > aim)) break;
+            before = __shfl(run, 63);
+        }
         return at;
     };
     double before;
-    const int at = cut(s_sum, 0.0, before), first = at * piece, each = (piece + NT - 1) / NT;      // the piece is cut into as many groups to a thread
-    const int from = min(first + tid * each, groups), to = min(min(from + each, first + piece), groups);
+    const int size = shared_out ? (groups + parts - 1) / parts : piece, first = (shared_out ? cut(s_part, parts, 0.0, before) : cut(s_sum, NW, 0.0, before)) * size;
+    const int each = (size + NT - 1) / NT, from = min(first + tid * each, groups), to = min(min(from + each, first + size), groups);      // the piece is cut into as many groups to a thread
     double own = 0.0;
     for (int g = from; g < to; ++g) {
         Group<T> p, q;
@@ -436,7 +479,7 @@ __global__ __launch_bounds__(NT) void tree_verify_kernel(TreeVerifyArgs a) {
     if (lane == 63) s_cut[w] = run;
     __syncthreads();
     double base;
-    if (cut(s_cut, before, base) != w) return;
+    if (cut(s_cut, NW, before, base) != w) return;
     run += base;
     if (lane != max(pick(own > 0.0, run > aim), 0)) return;
     run -= own;
@@ -559,8 +602,16 @@ hipError_t launch_tree_masks(const TreeMaskArgs& a, hipStream_t s) {
 
 template <class T, bool DRAFT>
 static hipError_t launch_verify_t(const TreeVerifyArgs& a, hipStream_t s) {
-    if (a.V <= 8192) tree_verify_kernel<T, DRAFT, 256><<<(unsigned)a.B, 256, 0, s>>>(a);
-    else tree_verify_kernel<T, DRAFT, 1024><<<(unsigned)a.B, 1024, 0, s>>>(a);
+    if (a.nsplit > 1) {
+        tree_verify_kernel<T, DRAFT, 64 * kFirstWaves, kFirst><<<(unsigned)(a.B * a.nsplit), 64 * kFirstWaves, 0, s>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        tree_verify_kernel<T, DRAFT, 1024, kRest><<<(unsigned)a.B, 1024, 0, s>>>(a);
+    } else if (a.V <= 8192) {
+        tree_verify_kernel<T, DRAFT, 256, kWhole><<<(unsigned)a.B, 256, 0, s>>>(a);
+    } else {
+        tree_verify_kernel<T, DRAFT, 1024, kWhole><<<(unsigned)a.B, 1024, 0, s>>>(a);
+    }
     return hipGetLastError();
 }
 

@@ -19,6 +19,14 @@ int check_tree(const hg_ctx* c, const int32_t* q_off, int rows, int max_new, int
     return B > 0 && !q_off ? HG_ERR_INVALID_ARG : HG_OK;
 }
 
+// Workgroups that share a sequence's first sum over the vocabulary: 8192 elements each, as far as all of them run at once.  The second launch costs 2.5 to 3 us, so vocabularies are large that
+// do.  us with / without: 8 sequences, 131072 tokens, chains with drafts in fp32 12.6 / 17.1, trees 29.0 / 31.8, without drafts 11.7 / 12.9; 65536 tokens, 4 trees in bf16 20.0 / 20.4; 50000
+// tokens, 64 trees 24.6 / 22.6; 32000 tokens, 32 chains 12.3 / 9.1.
+int verify_splits(const hg_ctx* c, int B, int V) {
+    const int n = (int)std::min<int64_t>({(V + 8191) / 8192, 1024 / B, kVerifySplits});
+    return V >= 98304 && n > 1 && c->ws && c->ws_bytes >= verify_bytes(B, n) ? n : 1;
+}
+
 bool among(const void* p, std::initializer_list<const void*> others) { return p && std::find(others.begin(), others.end(), p) != others.end(); }
 
 }  // namespace
@@ -55,8 +63,11 @@ int hg_tree_verify(hg_ctx* c, const int32_t* tokens, const int32_t* parents, con
         if (among(out, {tokens, parents, q_off, target, probs ? draft : nullptr, probs ? u : nullptr, probs ? u_next : nullptr})) return HG_ERR_INVALID_ARG;
     if (among(path, {accepted, next_tokens}) || accepted == next_tokens) return HG_ERR_INVALID_ARG;
     if (hipSetDevice(c->device) != hipSuccess) return HG_ERR_HIP;
-    return rc_of(launch_tree_verify(TreeVerifyArgs{tokens, parents, q_off, rows, max_new, B, V, target, probs ? draft : nullptr, target_stride, draft_stride, u, u_next, path, accepted, next_tokens},
-                                    p_dtype, c->stream));
+    TreeVerifyArgs a{tokens, parents, q_off, rows, max_new, B, V, target, probs ? draft : nullptr, target_stride, draft_stride, u, u_next, path, accepted, next_tokens};
+    a.nsplit = probs ? verify_splits(c, B, V) : 1;
+    a.state = reinterpret_cast<TreeVerifyState*>(c->ws);
+    a.parts = reinterpret_cast<double*>(c->ws + (a.nsplit > 1 ? (size_t)B * sizeof(TreeVerifyState) : 0));
+    return rc_of(launch_tree_verify(a, p_dtype, c->stream));
 }
 
 int hg_tree_keep_paged(hg_ctx* c, int n_layers, const hg_paged_kv* kv, const int32_t* q_off, int rows, const int32_t* path, const int32_t* accepted,
