@@ -694,16 +694,16 @@ using namespace rw;
 
 // Packed rows: tiles are all there is.  Paged rows: what remains behind the tiles is in the same launch: they are bound by the matrix pipes, the
 // others by the reads of their cache, and two workgroups of either kind share a CU.  While there are both, 256 workgroups of one kind, one for every CU, come
-// after 256 of the other.
+// after 256 of the other.  Of trees all tiles come first: the few rows' short workgroups, however many there are, then hold up no long one (48 trees, 32/8 heads 150 -> 144 us).
 template <int MODE>
 __global__ __launch_bounds__(64 * NW, 2) void HG_RW_KERNEL(RaggedArgs a) {
     if constexpr (MODE == kDense) {
         tile_workgroup<MODE>(a, blockIdx.x);
     } else {
         const unsigned tiles = TREE ? (unsigned)a.tile_wgs : (unsigned)a.tiles_all * (unsigned)a.Hkv * (unsigned)a.tile_nsplit, rows = a.row_wgs;
-        const unsigned both = min((tiles + 255u) / 256u, (rows + 255u) / 256u), block = blockIdx.x >> 8, in = blockIdx.x & 255u;
-        const bool is_tile = block < 2u * both ? (block & 1u) == 0u : tiles > rows;
-        const unsigned id = (block < 2u * both ? block >> 1 : block - both) * 256u + in;
+        const unsigned both = TREE ? 0u : min((tiles + 255u) / 256u, (rows + 255u) / 256u), block = blockIdx.x >> 8, in = blockIdx.x & 255u;
+        const bool is_tile = TREE ? block < (tiles + 255u) / 256u : block < 2u * both ? (block & 1u) == 0u : tiles > rows;
+        const unsigned id = (TREE ? block - (is_tile ? 0u : (tiles + 255u) / 256u) : block < 2u * both ? block >> 1 : block - both) * 256u + in;
         if (id >= (is_tile ? tiles : rows)) return;
         if (is_tile) tile_workgroup<MODE>(a, id);
         else rr::rows_workgroup<D, MODE == kCodes, true, NW, TREE>(a, id);
