@@ -62,12 +62,13 @@ extern "C" {
  * fills out[3] = { KV head, column of that head, split } and returns 1, or returns 0 if that workgroup has nothing to do or does
  * not exist (there are tiles * splits * Hkv of them, rounded up to a multiple of 8).  Ids equal modulo 8 share an XCD.
  *
- * hg_debug_ragged_plan: how hg_prompt_attn (paged 0; max_new and codes are not looked at) or hg_chunk_attn_paged (paged 1; codes: 8-bit rows) would run with these sizes and
+ * hg_debug_ragged_plan: how hg_prompt_attn (paged 0; max_new and codes are not looked at) hg_chunk_attn_paged (paged 1; codes: 8-bit rows) or hg_tree_attn_paged (paged 2) would run with these sizes and
  * workspace_bytes of workspace.  Returns what the call would return before it enqueues anything, and on HG_OK fills out[14] = { 1 if the launch has 128-row tiles; rows that
  * remain behind tiles and are not one, at most (0: tiles take everything); ... of the largest sequence; key ranges of what remains, and keys of one;
  * key ranges of a tile, and keys of one; where the partial results of what remains begin in the workspace, in floats, and their LSE, the same for tiles (-1: none);
  * workgroups of the launch (0: nothing to do), threads of one; workgroups of the join (0: none) }.  What remains of a sequence has B * Hkv * out[2] rows of parts per range, tiles
- * have rows * Hq.
+ * have rows * Hq.  Trees of up to 64 sequences: the key ranges of a tile are chosen on the device, at most as many and none shorter than said here, and the word in which the choice is left
+ * for the join lies in the 64 floats before the partial results of tiles.
  */
 int hg_debug_wide_plan(int n_blocks, int max_rows, int max_seqs, int Hkv, int rows_per_seq, int max_parts,
                        int slots_per_xcd, int D, int out[9]);

@@ -811,10 +811,11 @@ def hg_debug_fused_plan(levels, B: int, nq: int, Hq: int, Hkv: int, D: int, max_
     return plan
 
 
-def hg_debug_ragged_plan(rows: int, max_len: int, B: int, Hq: int, Hkv: int, D: int, max_new: Optional[int] = None, codes: bool = False, workspace_bytes: int = 0):
-    """dict of how hg_prompt_attn (max_new None) or hg_chunk_attn_paged would run, or the error code it would return (host only)."""
+def hg_debug_ragged_plan(rows: int, max_len: int, B: int, Hq: int, Hkv: int, D: int, max_new: Optional[int] = None, codes: bool = False, workspace_bytes: int = 0,
+                         tree: bool = False):
+    """dict of how hg_prompt_attn (max_new None), hg_chunk_attn_paged or (tree) hg_tree_attn_paged would run, or the error code it would return (host only)."""
     out = (ctypes.c_int64 * 14)()
-    rc = lib().hg_debug_ragged_plan(int(max_new is not None), int(codes), rows, max_new or 0, max_len, B, Hq, Hkv, D, workspace_bytes, out)
+    rc = lib().hg_debug_ragged_plan(int(max_new is not None) + int(tree), int(codes), rows, max_new or 0, max_len, B, Hq, Hkv, D, workspace_bytes, out)
     if rc != HG_OK:
         return rc
     return dict(zip(("tiles", "few_rows", "few_most", "nsplit", "chunk", "tile_nsplit", "tile_chunk", "part_O", "part_L", "tile_part_O", "tile_part_L", "workgroups", "threads",

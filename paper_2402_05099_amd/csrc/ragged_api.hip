@@ -330,6 +330,7 @@ int hg_debug_ragged_plan(int paged, int codes, int rows, int max_new, int max_le
     if (rows == 0 || B == 0 || (paged ? max_new : max_len) == 0) return HG_OK;      // nothing is launched
     RaggedArgs a = ragged_args(nullptr, 0, nullptr, rows, paged ? max_new : max_len, B, Hq, Hkv, D, 0.f, nullptr, HG_F32, nullptr);
     float* const ws = reinterpret_cast<float*>(256);      // (only distances from it are looked at)
+    if (paged == 2) a.masks = reinterpret_cast<const uint32_t*>(ws);      // (not looked at either)
     const Room room{ws, workspace_bytes / sizeof(float)};
     bool tiles = true;
     if (paged) tiles = plan_chunk(a, max_len, D, codes != 0, room);
