@@ -349,7 +349,8 @@ int hg_kv_write_paged(hg_ctx* ctx, const void* Knew, const void* Vnew, int64_t s
  *
  * hg_tree_attn_paged: hg_chunk_attn_paged but for what the n new tokens, the last n of the sequence's lengths[b] rows, see of each other: token t sees all rows [0, lengths[b] - n) and of its sequence's n
  * rows those with a bit in its row of masks (DEVICE, mask_words words to a row, bits as above, from hg_tree_masks or any others: bits from n on count for nothing, tokens without a bit are not
- * seen, and a token without a row to see has O = 0, LSE = -inf).  max_new has no limit here.  Everything else is as there: strides, bounds, the workspace, what rows that are not seen may hold.
+ * seen, and a token without a row to see has O = 0, LSE = -inf).  max_new has no limit here.  Everything else is as there: strides, bounds, the workspace (of which the key ranges of tiles take what
+ * there is, up to 64 ranges of rows * Hq rows, and are chosen on the device), what rows that are not seen may hold.
  *
  * hg_tree_verify: which tokens stand, and the token behind them, so that what comes out is distributed as if the target had been asked token by token (for drafts that are drawn from `draft`, or that are
  * told apart among siblings).  Token 0 stands.  The others are looked at in order, each if its parent is the last one that stands; with x the token (tokens[i]), p and q row

@@ -67,7 +67,7 @@ extern "C" {
  * remain behind tiles and are not one, at most (0: tiles take everything); ... of the largest sequence; key ranges of what remains, and keys of one;
  * key ranges of a tile, and keys of one; where the partial results of what remains begin in the workspace, in floats, and their LSE, the same for tiles (-1: none);
  * workgroups of the launch (0: nothing to do), threads of one; workgroups of the join (0: none) }.  What remains of a sequence has B * Hkv * out[2] rows of parts per range, tiles
- * have rows * Hq.  Trees of up to 64 sequences: the key ranges of a tile are chosen on the device, at most as many and none shorter than said here, and the word in which the choice is left
+ * have rows * Hq.  Trees of up to 256 sequences that do not fill the chip: the key ranges of a tile are chosen on the device, at most as many and none shorter than said here, and the word in which the choice is left
  * for the join lies in the 64 floats before the partial results of tiles.
  */
 int hg_debug_wide_plan(int n_blocks, int max_rows, int max_seqs, int Hkv, int rows_per_seq, int max_parts,

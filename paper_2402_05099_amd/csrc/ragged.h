@@ -57,11 +57,12 @@ struct RaggedArgs {
     const uint32_t* masks;
     int mask_words;           // of a row of the masks
     int tile_wgs, tile_jobs;  // workgroups that take tiles, and how many of them a KV head has
-    int balanced;             // 1 (up to 64 sequences): the workgroups choose the key ranges from the lengths (tree_jobs), at most tile_nsplit to a sequence and none shorter than
+    int balanced;             // 1 (up to kTreeSeqs sequences): the workgroups choose the key ranges from the lengths (tree_jobs), at most tile_nsplit to a sequence and none shorter than
                               // tile_chunk; the first leaves what it has chosen for the join in
     int* tile_choice;
 };
 constexpr int kTile = 128;        // rows of a tile
+constexpr int kTreeSeqs = 256;    // sequences of which the workgroups of a call order the jobs themselves
 constexpr int kFewRows = 32;      // a remainder of more rows is a tile: beside tiles, and wherever a read of the cache for every 32 rows is what costs
 constexpr int kFewRowsAlone = 64; // ... in small calls of no more rows than these, where a launch without tiles is over sooner (plan_few_rows)
 // Of a sequence's n G rows, those that tiles take.  Of a tree: all, or none.
@@ -257,7 +258,7 @@ __device__ __forceinline__ bool tile_of_rank(const RaggedArgs& a, int rank, Ragg
     return tile >= 0 && tile * kTile < rows_in_tiles<TREE>(seq.take * a.G, a.few_rows);      // (tile < 0: offsets out of order)
 }
 
-// ---- trees of up to 64 sequences: which workgroup takes which tile and which keys ----
+// ---- trees of up to kTreeSeqs sequences: which workgroup takes which tile and which keys ----
 // The key ranges of a sequence of `len` keys where none is to be longer than `most`: equal ones, multiples of 64.
 __device__ __forceinline__ int tree_range(int len, int most) {
     if (len <= most) return max(len, 1);
@@ -281,14 +282,29 @@ __device__ __forceinline__ T lane_scan(T x) {
 template <class T>
 __device__ __forceinline__ T last_lane(T x) { return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63)); }
 
-// Every lane of a wavefront must call these; lane i looks after sequence i.
+// Every lane of a wavefront must call these; lane i looks after the sequences i, 64 + i, ..
 struct TreeJobs {
-    RaggedSeq own;
-    int tiles, range, most;      // of this lane's sequence; `most` is the same for all
+    static constexpr int kPer = kTreeSeqs / 64;
+    RaggedSeq own[kPer];
+    int tiles[kPer], range[kPer], jobs[kPer], start[kPer];
+    int most;                    // the longest range; the same for all lanes
+    template <class F>
+    static __device__ __forceinline__ void for_own(int B, F what) {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j)
+            if (64 * j < B) what(j);
+    }
+    __device__ __forceinline__ static int lane_most(int x) {
+#pragma unroll
+        for (int d = 32; d > 0; d /= 2) x = max(x, __shfl_xor(x, d));
+        return x;
+    }
     __device__ __forceinline__ void load(const RaggedArgs& a) {
         const int lane = threadIdx.x & 63;
-        own = ragged_seq(a, min(lane, a.B - 1));
-        tiles = lane < a.B ? (rows_in_tiles<true>(own.take * a.G, a.few_rows) + kTile - 1) / kTile : 0;
+        for_own(a.B, [&](int j) {
+            own[j] = ragged_seq(a, min(64 * j + lane, a.B - 1));
+            tiles[j] = 64 * j + lane < a.B ? (rows_in_tiles<true>(own[j].take * a.G, a.few_rows) + kTile - 1) / kTile : 0;
+        });
     }
     // The longest range: of the longest sequence's halves, thirds, .. those with which the call is estimated to be over first.  us: a stage of 32 keys takes 0.95, 0.6 where a workgroup has
     // its CU to itself, a workgroup 7 beside its stages, 512 run at a time, the longest first; parts are written and read at 4.5 TB/s, their join takes 6.
@@ -297,22 +313,34 @@ struct TreeJobs {
         most = 0x3fffffff;
         if (a.tile_nsplit > 1) {
             const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-            int longest = tiles > 0 ? own.len : 0;
-#pragma unroll
-            for (int d = 32; d > 0; d /= 2) longest = max(longest, __shfl_xor(longest, d));
-            const float per_key = 0.95f / 32.f * (D == 64 ? 0.5f : 1.f), Hkv = (float)a.Hkv, stages = last_lane(lane_scan((float)tiles * (float)own.len)) * Hkv * per_key;
-            const float part = (float)own.take * (float)a.Hq * (float)(D + 1) * (8.f / 4.5e6f);
+            int longest = 0;
+            float keys = 0.f;
+            for_own(a.B, [&](int j) {
+                longest = max(longest, tiles[j] > 0 ? own[j].len : 0);
+                keys += (float)tiles[j] * (float)own[j].len;
+            });
+            longest = lane_most(longest);
+            const float per_key = 0.95f / 32.f * (D == 64 ? 0.5f : 1.f), Hkv = (float)a.Hkv, stages = last_lane(lane_scan(keys)) * Hkv * per_key;
+            const float part = (float)a.Hq * (float)(D + 1) * (8.f / 4.5e6f);      // us, of a token
             float best = 1e30f;
             int last = 0x3fffffff;      // the candidate before
             for (int i = w; i < 18 && last > a.tile_chunk; i += 4) {
                 const int k = i < 12 ? i + 1 : (int)(0x403125'1c1510ull >> (8 * (i - 12)) & 255u);
                 const int c = max(((int)((float)longest * __builtin_amdgcn_rcpf((float)k)) / 64 + 1) * 64, a.tile_chunk);
-                int q = (int)((float)own.len * __builtin_amdgcn_rcpf((float)c)), r = own.len - q * c;      // off by one at most: there are 64 ranges at most
-                if (r < 0) { --q; r += c; }
-                if (r >= c) { ++q; r -= c; }
-                const int p = k == 1 ? 1 : max(q + (r > 0 ? 1 : 0), 1), n = last_lane(lane_scan(tiles * p));
-                const float wgs = (float)n * Hkv, parts = last_lane(lane_scan(tiles > 0 && p > 1 ? (float)p * part : 0.f));
-                const float job = (k == 1 ? (float)longest : (float)c) * per_key;
+                const float inv = __builtin_amdgcn_rcpf((float)c);
+                int n = 0;
+                float parts = 0.f;
+                for_own(a.B, [&](int j) {
+                    int q = (int)((float)own[j].len * inv), r = own[j].len - q * c;      // off by one at most: there are 64 ranges at most
+                    if (r < 0) { --q; r += c; }
+                    if (r >= c) { ++q; r -= c; }
+                    const int p = k == 1 ? 1 : max(q + (r > 0 ? 1 : 0), 1);
+                    n += tiles[j] * p;
+                    parts += tiles[j] > 0 && p > 1 ? (float)p * (float)own[j].take * part : 0.f;
+                });
+                n = last_lane(lane_scan(n));
+                parts = last_lane(lane_scan(parts));
+                const float wgs = (float)n * Hkv, job = (k == 1 ? (float)longest : (float)c) * per_key;
                 float us = wgs <= 512.f ? job * (wgs <= 256.f ? 0.63f : 1.f) + 7.f : fmaxf(job + 7.f, (stages + 7.f * wgs) * (1.f / 512.f) + stages * __builtin_amdgcn_rcpf(wgs));
                 if (parts > 0.f) us += 6.f + parts;
                 if (us < best && (k == 1 || n <= a.tile_jobs)) {
@@ -332,22 +360,44 @@ struct TreeJobs {
                 if (us_of[i] < best) { best = us_of[i]; most = most_of[i]; }
             most = __builtin_amdgcn_readfirstlane(most);
         }
-        range = tree_range(own.len, most);
+        for_own(a.B, [&](int j) {
+            range[j] = tree_range(own[j].len, most);
+            jobs[j] = tiles[j] * ((max(own[j].len, 1) + range[j] - 1) / range[j]);
+        });
     }
-    // First of this lane's sequence's `n` jobs, where those of long ranges come first: by eighths of the longest, sequence after sequence in each.
-    __device__ __forceinline__ int first_of(int n) const {
-        int longest = n > 0 ? range : 0;
-#pragma unroll
-        for (int d = 32; d > 0; d /= 2) longest = max(longest, __shfl_xor(longest, d));
-        const int eighth = n > 0 ? min((int)(8.f * (float)range * __builtin_amdgcn_rcpf((float)longest)), 7) : -1;
-        int start = 0, before = 0;
+    // Numbers for the jobs, those of long ranges first: by eighths of the longest, sequence after sequence in each.
+    __device__ __forceinline__ void order(const RaggedArgs& a) {
+        int longest = 0, eighth[kPer];
+        for_own(a.B, [&](int j) { longest = max(longest, jobs[j] > 0 ? range[j] : 0); });
+        longest = lane_most(longest);
+        for_own(a.B, [&](int j) {
+            eighth[j] = jobs[j] > 0 ? min((int)(8.f * (float)range[j] * __builtin_amdgcn_rcpf((float)longest)), 7) : -1;
+            start[j] = 0;
+        });
+        int before = 0;
 #pragma unroll 1
-        for (int k = 7; k >= 0; --k) {
-            const int mine = eighth == k ? n : 0, run = lane_scan(mine);
-            if (eighth == k) start = before + run - mine;
-            before += last_lane(run);
-        }
-        return start;
+        for (int k = 7; k >= 0; --k)
+            for_own(a.B, [&](int j) {
+                const int mine = eighth[j] == k ? jobs[j] : 0, run = lane_scan(mine);
+                if (eighth[j] == k) start[j] = before + run - mine;
+                before += last_lane(run);
+            });
+    }
+    // Job `job`: its sequence, the length of its range, which of them, and which tile; those that share a range are next to each other.  false: there is none
+    __device__ __forceinline__ bool find(const RaggedArgs& a, int job, RaggedSeq& seq, int& chunk, int& which, int& tile) const {
+        bool found = false;
+        for_own(a.B, [&](int j) {
+            const unsigned long long at = __ballot(job >= start[j] && job < start[j] + jobs[j]);
+            if (at == 0) return;
+            found = true;
+            const int l = __builtin_ctzll(at), t = __builtin_amdgcn_readlane(tiles[j], l), in = job - __builtin_amdgcn_readlane(start[j], l);
+            seq = RaggedSeq{64 * j + l, __builtin_amdgcn_readlane(own[j].q0, l), __builtin_amdgcn_readlane(own[j].n, l), __builtin_amdgcn_readlane(own[j].take, l),
+                            __builtin_amdgcn_readlane(own[j].len, l)};
+            chunk = __builtin_amdgcn_readlane(range[j], l);
+            which = in / t;
+            tile = in - which * t;
+        });
+        return found;
     }
 };
 #endif

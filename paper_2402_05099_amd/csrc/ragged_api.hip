@@ -148,31 +148,30 @@ void plan_tiles(RaggedArgs& a, int D, Room& room) {
     split_keys(best, a.max_len, 1024, 64, (int64_t)a.rows * a.Hq, D, room, a.tile_nsplit, a.tile_chunk, a.tile_part_O, a.tile_part_L);
 }
 
-// Tiles of trees.  Up to 64 sequences: their workgroups choose the key ranges from the lengths (TreeJobs), among as many workgroups as there are here; what is decided here is whether there may be
-// several ranges, and room for their parts.  More sequences: as above.
+// Tiles of trees.  Up to kTreeSeqs sequences the workgroups can order the jobs, and choose the key ranges from the lengths (TreeJobs), which costs each of them 1 to 3 us, 1 to 5 with the
+// ranges.  What is decided here, from the host's bounds, is whether that pays, and where ranges' parts go; else it is as above.
+// Ranges: where the tokens do not fill the chip.  us with the host's ranges / chosen: 70 x 8/1 heads, up to 8000 keys 119 / 95; 45 x 16/2, up to 2000 43 / 32; 4 x 32/8 42 / 26; D = 64, 8 x 32/8 30 / 23;
+// 200 x 16/2, up to 1000 keys, 47 / 53.
+// Order: what starts last is long otherwise, an eighth of the longest job lost or more, against 2.5 us for every 512 jobs.  us without / with: 48 x 32/8, up to 4192 keys 161 / 146; 256 x 8/1, up to 3000
+// 120 / 101; 128 x 32/8, up to 2000 139 / 136, at D = 64 103 / 112; 100 x 32/8, 500 keys of codes 48 / 54; 250 x 40/40, up to 400 328 / 419.
 void plan_tree_tiles(RaggedArgs& a, int D, Room& room) {
-    a.balanced = a.B <= 64;
-    if (!a.balanced) {
-        plan_tiles(a, D, room);
-        a.tile_wgs = a.tiles_all * a.Hkv * a.tile_nsplit;
-        return;
-    }
     const int64_t one = (int64_t)a.tiles_all * a.Hkv;      // (a sequence's last tile may be all but empty: at most B of them)
-    a.tile_wgs = (int)one;
+    const bool here = a.B <= kTreeSeqs, ranges = here && one <= 768 && one - (int64_t)a.B * a.Hkv < 512 && a.max_len >= 1024;
+    a.balanced = here && one > 256 && one <= 2048 && a.max_len * (D / 128.0) >= 1.4 * (double)one;      // (up to 256 each have a CU to themselves)
     a.tile_jobs = a.tiles_all;
-    if (one - (int64_t)a.B * a.Hkv >= 512 || a.max_len < 1024) {
-        a.balanced = one > 256;      // (else each has a CU to itself)
-        return;
+    if (ranges && room.floats >= 64) {
+        Room rest = room;
+        int* const choice = reinterpret_cast<int*>(rest.take(64));
+        split_keys(64, a.max_len, 256, 64, (int64_t)a.rows * a.Hq, D, rest, a.tile_nsplit, a.tile_chunk, a.tile_part_O, a.tile_part_L);
+        if (a.tile_nsplit > 1) {
+            room = rest;
+            a.balanced = 1;
+            a.tile_choice = choice;
+            a.tile_jobs = std::max(a.tiles_all, 512 / a.Hkv);
+        }
     }
-    Room rest = room;
-    int* const choice = reinterpret_cast<int*>(rest.floats >= 64 ? rest.take(64) : nullptr);
-    if (!choice) return;
-    split_keys(64, a.max_len, 256, 64, (int64_t)a.rows * a.Hq, D, rest, a.tile_nsplit, a.tile_chunk, a.tile_part_O, a.tile_part_L);
-    if (a.tile_nsplit == 1) return;
-    room = rest;
-    a.tile_choice = choice;
-    a.tile_jobs = std::max(a.tiles_all, 512 / a.Hkv);
-    a.tile_wgs = a.tile_jobs * a.Hkv;
+    if (!a.balanced && a.B > 64) plan_tiles(a, D, room);
+    a.tile_wgs = a.balanced ? a.tile_jobs * a.Hkv : a.tiles_all * a.Hkv * a.tile_nsplit;
 }
 
 // Choices of a call over packed rows, whose sequences have no more keys than there are tokens, whatever the caller's bound ...

@@ -136,20 +136,13 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
             v = a.by_heads.of(id);
             kvh = (int)(id - v * (unsigned)a.Hkv);
         }
-        if (TREE && a.balanced) {      // longest ranges first; the tiles that share one next to each other
+        if (TREE && a.balanced) {
             TreeJobs jobs;
             jobs.load(a);
             jobs.choose(a, D, smem + lds_bytes(MODE) + 16);
             if (id == 0 && a.tile_choice && threadIdx.x == 0) *a.tile_choice = jobs.most;
-            const int parts = (max(jobs.own.len, 1) + jobs.range - 1) / jobs.range, n = jobs.tiles * parts, start = jobs.first_of(n);
-            const unsigned long long at = __ballot((int)v >= start && (int)v < start + n);
-            if (at == 0) return;
-            const int b = __builtin_ctzll(at), t = __builtin_amdgcn_readlane(jobs.tiles, b), in = (int)v - __builtin_amdgcn_readlane(start, b);
-            sq = RaggedSeq{b, __builtin_amdgcn_readlane(jobs.own.q0, b), __builtin_amdgcn_readlane(jobs.own.n, b), __builtin_amdgcn_readlane(jobs.own.take, b),
-                           __builtin_amdgcn_readlane(jobs.own.len, b)};
-            chunk = __builtin_amdgcn_readlane(jobs.range, b);
-            sp = in / t;
-            tile = in - sp * t;
+            jobs.order(a);
+            if (!jobs.find(a, (int)v, sq, chunk, sp, tile)) return;
         } else {
             const int rank = (int)(v / (unsigned)a.tile_nsplit);
             sp = (int)(v - (unsigned)rank * (unsigned)a.tile_nsplit);

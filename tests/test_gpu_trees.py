@@ -171,7 +171,7 @@ def test_tokens_and_rows_behind_the_bounds(D, codes):
 
 @pytest.mark.parametrize("codes", [False, True])
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("B", [1, 2, 63, 64, 65, 130])
+@pytest.mark.parametrize("B", [1, 2, 63, 64, 65, 130, 256, 257])
 def test_key_ranges_of_many_sequences(B, D, codes):
     """Up to 64 sequences the workgroups choose the ranges from the lengths; long ones among short and empty ones, trees that are tiles among those that are few rows."""
     pairs = [(max(n, (1500 if b % 7 == 0 else 40) + 13 * b % 300), n) for b in range(B) for n in [(40, 3, 0, 17, 64, 9, 33)[b % 7]]]
@@ -188,6 +188,19 @@ def test_tiles_of_sequences_without_enough_rows(D, codes):
         run_attn([(0, 64), (5, 64), (64, 64), (33, 100), (70, 64)], (8, 2), D, codes=codes, kind=kind)
     run_attn([(0, 64), (5, 64), (1500, 64), (33, 100)], (8, 2), D, codes=codes, mib=64)
     run_attn([(40, 9), (70, 64), (0, 3)], (8, 2), D, codes=codes, max_len=0)
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_key_ranges_of_more_sequences_than_are_ordered(D, codes):
+    """Two large trees behind long contexts among 64 and more others: the ranges are the host's."""
+    run_attn([(3000, 40), (2500, 33)] + [(20 + b, b % 3) for b in range(64)], (8, 2), D, codes=codes, mib=64)
+    run_attn([(20 + b, b % 3) for b in range(70)] + [(3000, 40), (0, 40)], (8, 2), D, codes=codes, mib=64, kind="any")
+
+
+def test_many_heads_to_a_kv_head():
+    run_attn([(50, 7), (300, 3), (33, 33), (9, 1)], (80, 1), 128, mib=64)
+    run_attn([(50, 7), (300, 3), (33, 33), (9, 1)], (66, 2), 64, codes=True)
 
 
 def test_bounds_that_are_a_capacity():
@@ -240,12 +253,12 @@ def test_chains_are_chunks(heads, D, codes):
 
 @pytest.mark.parametrize("codes", [False, True])
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("n", [9, 90])
+@pytest.mark.parametrize("n,context_rows", [(9, 150), (90, 150), (9, 1500), (90, 1500)])      # (behind 1500 rows in several ranges of keys)
 @pytest.mark.parametrize("what", ["k", "v", "inf"])
-def test_values_that_are_not_finite_reach_only_those_that_see_them(what, n, D, codes):
+def test_values_that_are_not_finite_reach_only_those_that_see_them(what, n, context_rows, D, codes):
     if what == "inf" and codes:
         return      # (the codes have no infinities)
-    heads, lens = (8, 2), [n + 150, n + 3]
+    heads, lens = (8, 2), [n + context_rows, n + 3]
     Q, Qd, off, T, lens, counts, sees, masks, kv, keys, values = tree_case([(x, n) for x in lens], *heads, D, codes=codes)
     bad = n // 2      # a token of the tree whose row is spoiled: it and those that follow from it have NaN or infinity
     for b in range(2):
@@ -297,16 +310,18 @@ def test_tree_attention_in_a_graph_and_on_a_stream():
     ctx.close()
 
 
-def test_a_whole_step_in_a_graph():
+@pytest.mark.parametrize("V", [3000, 98500])
+def test_a_whole_step_in_a_graph(V):
     """Masks, attention, verification and the move captured on a stream of their own, replayed with eager work and other lengths between: the results of eager calls."""
     g, r = torch.Generator().manual_seed(5), np.random.default_rng(5)
-    Hq, Hkv, D, ps, V, B, n = 8, 2, 128, 16, 3000, 6, 70
+    Hq, Hkv, D, ps, B, n = 8, 2, 128, 16, 6, 70
     T = B * n
     Kp, Vp, table, _, _ = make_cache(g, [1300] * B, Hkv, D, ps, False)
     first = [(Kp.clone(), Vp.clone()) for _ in range(2)]
     Q = rand(g, T, Hq, D).to(DEV)
     parents, off = i32(sum([random_parents(r, n, 4) for _ in range(B)], [])), i32(list(range(0, T + 1, n)))
-    target, draft = torch.softmax(4 * torch.randn(T, V, generator=g), 1).to(DEV), torch.softmax(4 * torch.randn(T, V, generator=g), 1).to(DEV)
+    z = torch.randn(T, V, generator=g) * 4
+    target, draft = torch.softmax(z, 1).to(DEV), torch.softmax(z + torch.randn(T, V, generator=g), 1).to(DEV)
     tokens, u, un = torch.multinomial(draft, 1)[:, 0].to(torch.int32), torch.rand(T, generator=g).to(DEV), torch.rand(B, generator=g).to(DEV)
     lens = [i32([n + int(x) for x in r.integers(0, 1230, B)]) for _ in range(4)]
     ctx = context(64)
@@ -429,6 +444,11 @@ def test_verification_over_large_vocabularies(V, drafts, dtype):
 def test_verification_where_few_tokens_have_nearly_all(V, drafts, dtype):
     kept = run_verify([1, 7, 0, 30, 12, 64, 33, 20], V, drafts=drafts, dtype=dtype, seed=V, width=3, near=0.9, peaked=True)
     assert max(kept) > 1
+
+
+@pytest.mark.parametrize("drafts", [True, False])
+def test_verification_over_more_groups_than_the_filter_tells_apart(drafts):
+    run_verify([6, 1, 9], 300001, drafts=drafts, near=0.9, peaked=True)
 
 
 @pytest.mark.parametrize("drafts", [True, False])
@@ -604,3 +624,48 @@ def test_paths_and_tables_with_holes():
     run_keep(KEEP, wild=0.3)
     run_keep(KEEP, holes=True)
     run_keep(KEEP, max_new=16)
+
+
+# ---- calls with nothing in them, offsets that leave the tensors ----------------------------------------------------------------
+
+def test_calls_without_tokens_and_without_sequences():
+    ctx = context(1)
+    e = lambda *shape, dtype=torch.int32: torch.full(shape, 7, dtype=dtype, device=DEV)  # noqa: E731
+    bf, f32 = torch.bfloat16, torch.float32
+    for B in (0, 3):
+        off, len_, table, kept, nxt, grown = i32([0] * (B + 1)), i32([5] * B), torch.zeros(B, 4, dtype=torch.int32, device=DEV), e(B), e(B), e(B)
+        kv = hb.PagedKV(e(64, 2, 64, dtype=bf), e(64, 2, 64, dtype=bf), table, 16)
+        hb.hg_tree_masks(ctx, e(0), off, 8, e(0, 1), e(0))
+        hb.hg_tree_attn_paged(ctx, e(0, 4, 64, dtype=bf), off, e(0, 1), kv, len_, 8, 16, e(0, 4, 64, dtype=bf), e(0, 4, dtype=f32))
+        hb.hg_tree_verify(ctx, e(0), e(0), off, 8, e(0, 100, dtype=f32), e(0, 100, dtype=f32), e(0, dtype=f32), e(B, dtype=f32), e(0), kept, nxt)
+        assert kept.tolist() == [0] * B and nxt.tolist() == [-1] * B
+        hb.hg_tree_keep_paged(ctx, [kv], off, e(0), kept, len_, 8, grown)
+        assert grown.tolist() == [5] * B and torch.all(kv.K == 7)
+    ctx.close()
+
+
+def test_offsets_behind_the_tensors_end_with_them():
+    """q_off says more tokens than there are rows: those that are there are a smaller tree's."""
+    r, g, T, V = np.random.default_rng(3), torch.Generator().manual_seed(3), 30, 50
+    off, clamped = [0, 12, 45, 90], [0, 12, 30, 30]
+    ups = [random_parents(r, n, 3) for n in (12, 18)]
+    parents, tokens, says = i32(sum(ups, [])), i32(r.integers(0, 2, T).tolist()), i32(r.integers(0, 2, T).tolist())
+    lens = [40, 60, 33]
+    Kp, Vp, table, keys, values = make_cache(g, lens, 2, 64, 16, False)
+    kv, Q = hb.PagedKV(Kp, Vp, table, 16), rand(g, T, 4, 64)
+    got = []
+    for o in (off, clamped):
+        ctx = context()
+        m, d, O, L = torch.zeros(T, 2, dtype=torch.int32, device=DEV), i32([0] * T), torch.zeros(T, 4, 64, device=DEV), torch.zeros(T, 4, device=DEV)
+        path, kept, nxt, grown = i32([7] * T), i32([7] * 3), i32([7] * 3), i32([7] * 3)
+        pool = kv.K.clone()
+        hb.hg_tree_masks(ctx, parents, i32(o), 64, m, d)
+        hb.hg_tree_attn_paged(ctx, Q.to(DEV), i32(o), m, kv, i32(lens), 64, 60, O, L)
+        hb.hg_tree_verify(ctx, tokens, parents, i32(o), 64, says, None, None, None, path, kept, nxt)
+        hb.hg_tree_keep_paged(ctx, [hb.PagedKV(pool, Vp.clone(), table, 16)], i32(o), path, kept, i32(lens), 64, grown)
+        torch.cuda.synchronize()
+        got.append((m, d, O, L, path, kept, nxt, grown, pool.view(torch.int16)))
+        ctx.close()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    assert torch.isfinite(got[0][2]).all()

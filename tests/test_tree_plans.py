@@ -24,7 +24,9 @@ def look(rows, max_len, B, Hq, Hkv, D, max_new, codes, ws):
             continue
         assert chunk % 64 == 0 and O % 4 == 0, what
         used += [(O, O + n * part_rows * D), (L, L + n * part_rows)]
-    if p["tile_nsplit"] > 1 and B <= 64:
+    one = (rows * G // 128 + B) * Hkv      # workgroups with a range each
+    chosen = p["tile_nsplit"] > 1 and B <= 256 and one <= 768 and max_len >= 1024      # ... or more of them, as the device chooses
+    if chosen:
         assert p["tile_nsplit"] <= 64, f"{what}: the device looks at 64 ranges at most"
         used.append((p["tile_part_O"] - 64, p["tile_part_O"]))      # the choice that it leaves for the join
     used.sort()
@@ -32,7 +34,7 @@ def look(rows, max_len, B, Hq, Hkv, D, max_new, codes, ws):
     assert all(z <= a for (_, z), (a, _) in zip(used, used[1:])), f"{what}: parts {used} overlap"
     assert p["workgroups"] > 0 and p["workgroups"] * p["threads"] < 2**32, what
     if p["tiles"]:
-        assert p["workgroups"] >= (rows * G // 128 + B) * Hkv * (p["tile_nsplit"] if B > 64 else 1), f"{what}: a tile has no workgroup"
+        assert p["workgroups"] >= one * (1 if chosen else p["tile_nsplit"]), f"{what}: a tile has no workgroup"
     assert (p["join"] > 0) == (p["nsplit"] > 1 or p["tile_nsplit"] > 1) and p["join"] * 256 < 2**32, what
     return p
 
@@ -45,7 +47,7 @@ def test_trees_under_any_bound(D, heads, ws, codes):
     for rows in (1, 45, 256, 3000, 20000):
         for max_new in (1, 8, 33, 64, 1024, 2**31 - 1):
             for max_len in (0, 1, 515, 1023, 1024, 4096, 65536 + 33, (1 << 30) - 2):
-                for B in (1, 3, 64, 65, 512):
+                for B in (1, 3, 64, 65, 256, 512):
                     look(rows, max_len, B, *heads, D, max_new, codes, ws)
 
 
