@@ -1,6 +1,7 @@
 // Attention of packed tokens of several sequences, each with its own number of new tokens and of keys: whole prompts
 // (hg_prompt_attn) and chunks behind a paged cache (hg_chunk_attn_paged).  Arguments and what the kernels share (gfx950 only).
 #pragma once
+#include <algorithm>
 #include <type_traits>
 
 #include "hg_internal.h"
@@ -57,12 +58,14 @@ struct RaggedArgs {
     const uint32_t* masks;
     int mask_words;           // of a row of the masks
     int tile_wgs, tile_jobs;  // workgroups that take tiles, and how many of them a KV head has
-    int balanced;             // 1 (up to kTreeSeqs sequences): the workgroups choose the key ranges from the lengths (tree_jobs), at most tile_nsplit to a sequence and none shorter than
-                              // tile_chunk; the first leaves what it has chosen for the join in
+    int balanced;             // 1 (up to kTreeSeqs sequences): the workgroups order the jobs, and with tile_nsplit > 1 choose the key ranges from the lengths (TreeJobs).  The longest is never
+                              // set below tile_chunk, so a sequence has at most tile_nsplit; one that is longer than that is cut into equal ranges, which may be little more than half as long.
+                              // The first workgroup leaves what it has chosen for the join in
     int* tile_choice;
 };
 constexpr int kTile = 128;        // rows of a tile
 constexpr int kTreeSeqs = 256;    // sequences of which the workgroups of a call order the jobs themselves
+constexpr int kFewTiles = 768;    // with more workgroups than these, by what the host knows, there are key ranges only where they save much
 constexpr int kFewRows = 32;      // a remainder of more rows is a tile: beside tiles, and wherever a read of the cache for every 32 rows is what costs
 constexpr int kFewRowsAlone = 64; // ... in small calls of no more rows than these, where a launch without tiles is over sooner (plan_few_rows)
 // Of a sequence's n G rows, those that tiles take.  Of a tree: all, or none.
@@ -80,8 +83,13 @@ inline int64_t rows_grid(const RaggedArgs& a) {
 
 // Workgroups that take tiles
 inline int64_t tiles_grid(const RaggedArgs& a) { return a.masks ? a.tile_wgs : (int64_t)a.tiles_all * a.Hkv * a.tile_nsplit; }
-// ... and of a launch that has tiles: over a paged cache both kinds by turns, 256 of each
-inline int64_t ragged_grid(const RaggedArgs& a) { return a.few_rows == 0 ? tiles_grid(a) : ((tiles_grid(a) + 255) / 256 + (rows_grid(a) + 255) / 256) * 256; }
+// ... and of a launch that has tiles: over a paged cache both kinds by turns, 256 of each.  Of trees, where ranges are chosen among more than kFewTiles: as many as plan_tiles' ranges would have; those
+// that can have nothing to do come last and end at once.
+inline int64_t ragged_grid(const RaggedArgs& a) {
+    if (a.few_rows == 0) return tiles_grid(a);
+    const int64_t one = (int64_t)a.tiles_all * a.Hkv, both = ((tiles_grid(a) + 255) / 256 + (rows_grid(a) + 255) / 256) * 256;
+    return a.balanced && one > kFewTiles ? std::max(both, one * a.tile_nsplit) : both;
+}
 // Workgroups of the join of parts: groups of D / 8 lanes to a row, and of a token's heads
 inline int join_groups(const RaggedArgs& a) { return a.nsplit > 8 || a.tile_nsplit > 8 ? 8 : 1; }
 inline int join_per_token(const RaggedArgs& a, int D) { const int rows = 2048 / D / join_groups(a); return a.tile_nsplit > 1 ? (a.Hq + rows - 1) / rows : 0; }
@@ -287,7 +295,9 @@ struct TreeJobs {
     static constexpr int kPer = kTreeSeqs / 64;
     RaggedSeq own[kPer];
     int tiles[kPer], range[kPer], jobs[kPer], start[kPer];
-    int most;                    // the longest range; the same for all lanes
+    int most;                    // the longest range (kNoRange: no sequence is cut); the same for all lanes
+    static constexpr int kNoRange = 0x3fffffff;      // longer than any sequence
+    static __device__ __forceinline__ bool crowded(const RaggedArgs& a) { return a.tile_nsplit > 1 && a.tiles_all * a.Hkv > kFewTiles; }
     template <class F>
     static __device__ __forceinline__ void for_own(int B, F what) {
 #pragma unroll
@@ -306,11 +316,13 @@ struct TreeJobs {
             tiles[j] = 64 * j + lane < a.B ? (rows_in_tiles<true>(own[j].take * a.G, a.few_rows) + kTile - 1) / kTile : 0;
         });
     }
-    // The longest range: of the longest sequence's halves, thirds, .. those with which the call is estimated to be over first.  us: a stage of 32 keys takes 0.95, 0.6 where a workgroup has
+    // The longest range: of the longest sequence's halves, thirds, .. those with which the call is estimated to be over first (if there may be many workgroups: in three fifths of the time
+    // or less, and none is looked at where all places, or the reads of all sequences, take longer anyway; with whichever is best 20 x 40/40 heads, 40 tokens, 500 to 8000 keys 250 us for 233, and one of
+    // 64 tokens behind 2000 keys among 100 x 32/8 of 2 tokens 70 for 63).  us: a stage of 32 keys takes 0.95, 0.6 where a workgroup has
     // its CU to itself, a workgroup 7 beside its stages, 512 run at a time, the longest first; parts are written and read at 4.5 TB/s, their join takes 6.
     // Of a workgroup of four wavefronts, each of which looks at every fourth candidate (0.4 us each); `meet`: 32 bytes of LDS.
     __device__ __forceinline__ void choose(const RaggedArgs& a, int D, unsigned char* meet) {
-        most = 0x3fffffff;
+        most = kNoRange;
         if (a.tile_nsplit > 1) {
             const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
             int longest = 0;
@@ -323,8 +335,20 @@ struct TreeJobs {
             const float per_key = 0.95f / 32.f * (D == 64 ? 0.5f : 1.f), Hkv = (float)a.Hkv, stages = last_lane(lane_scan(keys)) * Hkv * per_key;
             const float part = (float)a.Hq * (float)(D + 1) * (8.f / 4.5e6f);      // us, of a token
             float best = 1e30f;
-            int last = 0x3fffffff;      // the candidate before
-            for (int i = w; i < 18 && last > a.tile_chunk; i += 4) {
+            int last = kNoRange;      // the candidate before
+            bool look = true;
+            if (crowded(a)) {      // what ranges have to save: two fifths, and the rows of all sequences, tiles or not, are read within the call (5 TB/s; the join takes 10 with what it waits for)
+                float n = 0.f, all = 0.f;
+                for_own(a.B, [&](int j) {
+                    n += (float)tiles[j];
+                    all += 64 * j + (int)(threadIdx.x & 63) < a.B ? (float)own[j].len : 0.f;
+                });
+                const float wgs = last_lane(lane_scan(n)) * Hkv, job = (float)longest * per_key, least = (stages + 7.f * wgs) * (1.f / 512.f);
+                const float us = wgs <= 512.f ? job * (wgs <= 256.f ? 0.63f : 1.f) + 7.f : fmaxf(job + 7.f, least + stages * __builtin_amdgcn_rcpf(wgs));
+                best = 0.6f * us;
+                look = best > least + 6.f && us > last_lane(lane_scan(all)) * (float)a.kv_stride * (2.f / 5e6f) + 10.f;      // (else there is none that does)
+            }
+            for (int i = crowded(a) && w == 0 ? 4 : w; look && i < 18 && last > a.tile_chunk; i += 4) {
                 const int k = i < 12 ? i + 1 : (int)(0x403125'1c1510ull >> (8 * (i - 12)) & 255u);
                 const int c = max(((int)((float)longest * __builtin_amdgcn_rcpf((float)k)) / 64 + 1) * 64, a.tile_chunk);
                 const float inv = __builtin_amdgcn_rcpf((float)c);
@@ -345,25 +369,33 @@ struct TreeJobs {
                 if (parts > 0.f) us += 6.f + parts;
                 if (us < best && (k == 1 || n <= a.tile_jobs)) {
                     best = us;
-                    most = k == 1 ? 0x3fffffff : c;
+                    most = k == 1 ? kNoRange : c;
                 }
                 last = k == 1 ? last : c;
             }
-            float* const us_of = reinterpret_cast<float*>(meet);
-            int* const most_of = reinterpret_cast<int*>(meet + 16);
-            if ((threadIdx.x & 63) == 0) { us_of[w] = best; most_of[w] = most; }
-            __syncthreads();
-            best = us_of[0];
-            most = most_of[0];
+            if (look) {
+                float* const us_of = reinterpret_cast<float*>(meet);
+                int* const most_of = reinterpret_cast<int*>(meet + 16);
+                if ((threadIdx.x & 63) == 0) { us_of[w] = best; most_of[w] = most; }
+                __syncthreads();
+                best = us_of[0];
+                most = most_of[0];
 #pragma unroll
-            for (int i = 1; i < 4; ++i)
-                if (us_of[i] < best) { best = us_of[i]; most = most_of[i]; }
+                for (int i = 1; i < 4; ++i)
+                    if (us_of[i] < best) { best = us_of[i]; most = most_of[i]; }
+            }
             most = __builtin_amdgcn_readfirstlane(most);
         }
         for_own(a.B, [&](int j) {
             range[j] = tree_range(own[j].len, most);
             jobs[j] = tiles[j] * ((max(own[j].len, 1) + range[j] - 1) / range[j]);
         });
+    }
+    // all there are
+    __device__ __forceinline__ int count(const RaggedArgs& a) const {
+        int n = 0;
+        for_own(a.B, [&](int j) { n += jobs[j]; });
+        return last_lane(lane_scan(n));
     }
     // Numbers for the jobs, those of long ranges first: by eighths of the longest, sequence after sequence in each.
     __device__ __forceinline__ void order(const RaggedArgs& a) {

@@ -149,29 +149,47 @@ void plan_tiles(RaggedArgs& a, int D, Room& room) {
 }
 
 // Tiles of trees.  Up to kTreeSeqs sequences the workgroups can order the jobs, and choose the key ranges from the lengths (TreeJobs), which costs each of them 1 to 3 us, 1 to 5 with the
-// ranges.  What is decided here, from the host's bounds, is whether that pays, and where ranges' parts go; else it is as above.
+// ranges.  What is decided here, from the host's bounds, is whether that pays, how many ranges there may be, and where their parts go.  More sequences: as above.
 // Ranges: where the tokens do not fill the chip.  us with the host's ranges / chosen: 70 x 8/1 heads, up to 8000 keys 119 / 95; 45 x 16/2, up to 2000 43 / 32; 4 x 32/8 42 / 26; D = 64, 8 x 32/8 30 / 23;
 // 200 x 16/2, up to 1000 keys, 47 / 53.
+// How many tiles there are the host does not know: `one` counts a last tile, all but empty, for every sequence, also for those that are few rows.  Beyond kFewTiles of them there may be as many
+// ranges as plan_tiles would take, or as make 8192 workgroups, and the workgroups split where that saves much (TreeJobs::choose).  us without ranges / chosen: 64 tokens behind 65536 keys among requests
+// of 2 tokens behind 300 to 1000: 20 x 40/40 heads 977 / 316, 64 x 40/40 1027 / 367, 32 x 32/32 971 / 270, 60 x 64/16 1018 / 223, 100 x 32/8 1010 / 160, its codes 1233 / 170, D = 64, 20 x 40/40 635 / 188;
+// 60 x 32/8, 33 tokens each, up to 1500 keys and one of 65536 1005 / 173.  Where there is nothing to split: 128 x 32/8, 9 tokens, up to 2000 keys 132.8 / 134.2, under a bound of 65536 132.7 / 134.7;
+// 20 x 40/40, 40 tokens, up to 2000 keys under that bound 100.8 / 102.3 (plan_tiles' ranges there: 119, and 60 x 32/8, 33 tokens, up to 4000 keys 170 / 439).
 // Order: what starts last is long otherwise, an eighth of the longest job lost or more, against 2.5 us for every 512 jobs.  us without / with: 48 x 32/8, up to 4192 keys 161 / 146; 256 x 8/1, up to 3000
 // 120 / 101; 128 x 32/8, up to 2000 139 / 136, at D = 64 103 / 112; 100 x 32/8, 500 keys of codes 48 / 54; 250 x 40/40, up to 400 328 / 419.
 void plan_tree_tiles(RaggedArgs& a, int D, Room& room) {
-    const int64_t one = (int64_t)a.tiles_all * a.Hkv;      // (a sequence's last tile may be all but empty: at most B of them)
-    const bool here = a.B <= kTreeSeqs, ranges = here && one <= 768 && one - (int64_t)a.B * a.Hkv < 512 && a.max_len >= 1024;
-    a.balanced = here && one > 256 && one <= 2048 && a.max_len * (D / 128.0) >= 1.4 * (double)one;      // (up to 256 each have a CU to themselves)
+    const int64_t one = (int64_t)a.tiles_all * a.Hkv;
+    if (a.B > kTreeSeqs) {
+        plan_tiles(a, D, room);
+        a.tile_wgs = a.tiles_all * a.Hkv * a.tile_nsplit;
+        return;
+    }
+    a.balanced = one > 256 && one <= 2048 && a.max_len * (D / 128.0) >= 1.4 * (double)one;      // (up to 256 each have a CU to themselves)
     a.tile_jobs = a.tiles_all;
-    if (ranges && room.floats >= 64) {
+    if (one - (int64_t)a.B * a.Hkv < 512 && a.max_len >= 1024 && room.floats >= 64) {
+        int64_t want = 64;
+        if (one > kFewTiles) {
+            RaggedArgs host = a;
+            Room all = room;
+            plan_tiles(host, D, all);
+            want = std::max<int64_t>(host.tile_nsplit, 8192 / one);
+        }
         Room rest = room;
         int* const choice = reinterpret_cast<int*>(rest.take(64));
-        split_keys(64, a.max_len, 256, 64, (int64_t)a.rows * a.Hq, D, rest, a.tile_nsplit, a.tile_chunk, a.tile_part_O, a.tile_part_L);
+        split_keys(want, a.max_len, 256, 64, (int64_t)a.rows * a.Hq, D, rest, a.tile_nsplit, a.tile_chunk, a.tile_part_O, a.tile_part_L);
         if (a.tile_nsplit > 1) {
             room = rest;
             a.balanced = 1;
             a.tile_choice = choice;
-            a.tile_jobs = std::max(a.tiles_all, 512 / a.Hkv);
+            // tiles that there can be: a sequence has its first with more than few_rows rows, the second with 128 and one, ..
+            const int64_t nrows = (int64_t)a.rows * a.G, least = a.few_rows + 1, seqs = std::min<int64_t>(a.B, nrows / least);
+            const int tiles = (int)(seqs + std::min((nrows - seqs * least) / (kTile - a.few_rows), nrows / kTile));
+            a.tile_jobs = one > kFewTiles ? tiles + 512 / a.Hkv : std::max(a.tiles_all, 512 / a.Hkv);
         }
     }
-    if (!a.balanced && a.B > 64) plan_tiles(a, D, room);
-    a.tile_wgs = a.balanced ? a.tile_jobs * a.Hkv : a.tiles_all * a.Hkv * a.tile_nsplit;
+    a.tile_wgs = a.tile_jobs * a.Hkv;
 }
 
 // Choices of a call over packed rows, whose sequences have no more keys than there are tokens, whatever the caller's bound ...

@@ -141,6 +141,7 @@ __device__ __forceinline__ void tile_workgroup(const RaggedArgs& a, unsigned id)
             jobs.load(a);
             jobs.choose(a, D, smem + lds_bytes(MODE) + 16);
             if (id == 0 && a.tile_choice && threadIdx.x == 0) *a.tile_choice = jobs.most;
+            if (jobs.crowded(a) && (int)v >= jobs.count(a)) return;
             jobs.order(a);
             if (!jobs.find(a, (int)v, sq, chunk, sp, tile)) return;
         } else {
