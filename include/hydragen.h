@@ -357,10 +357,11 @@ int hg_kv_write_paged(hg_ctx* ctx, const void* Knew, const void* Vnew, int64_t s
  * `parent` of target and draft (DEVICE [rows, V] of p_dtype, HG_F32 or HG_BF16, row distances in elements: row i has the probabilities of what comes behind token i, the target's, and
  * those that its children were drawn with), u[i] a random number from [0, 1):
  *   with draft: p_0 = p; x stands if u q(x) < p_k(x), k being the siblings refused before; a refusal leaves p_k+1 = max(0, p_k - q) / its sum.
- *   draft NULL (each drafted token counts as certain): x stands if u < p_k(x); a refusal leaves p_k+1 = p_k without x, / its sum.
- * next_tokens[b] is drawn from the p_k that is left at the last token that stands: the smallest y with p_k(0) + .. + p_k(y) > u_next[b] (times the sum as it is: rows need not sum to one exactly).
+ *   draft NULL (each drafted token counts as certain): x stands if u S_k < p(x), S_0 = 1; a refusal leaves S_k+1 = S_k - p(x), and p(x) counts as 0 from then on.  (p_k = p without the refused tokens, / S_k: where a
+ *   row does not sum to one, every sibling keeps its own p, and S_k is not what is left of the row.)
+ * next_tokens[b] is drawn from the p_k that is left at the last token that stands: the smallest y with p_k(0) + .. + p_k(y) > u_next[b] (times the sum of p_k as it is: rows need not sum to one).
  * Sums are taken in 64 bits; the first over a vocabulary of 98304 tokens or more by several workgroups, if the workspace has room for it (at most 2072 bytes a sequence; else it
- * is not used).  The kernels use p_k = max(0, p - c_k q) / S_k, c_0 = 0, S_0 = 1, c_k+1 = c_k + S_k, S_k+1 = sum of max(0, p - c_k+1 q), which is the same.  Entries that are not positive finite
+ * is not used).  With draft the kernels use p_k = max(0, p - c_k q) / S_k, c_0 = 0, S_0 = 1, c_k+1 = c_k + S_k, S_k+1 = sum of max(0, p - c_k+1 q), which is the same.  Entries that are not positive finite
  * numbers count as 0, so do tokens outside [0, V).  Where nothing is left (rounding), the draw is from p; where p has nothing either, next_tokens[b] is -1.
  *   p_dtype = HG_TOKENS (greedy decoding): target is int32 [rows], what the target says behind each token; a token stands if it is what its parent's row says, next_tokens[b] is what the last
  * one's says.  V, draft, u and u_next are not looked at.
