@@ -596,8 +596,16 @@ hipError_t launch_tree_masks(const TreeMaskArgs& a, hipStream_t s) {
         tree_masks_kernel<<<(unsigned)((a.B + 3) / 4), 256, 0, s>>>(a);
         return hipGetLastError();
     }
-    tree_masks_long_kernel<<<dim3((unsigned)a.B, (unsigned)((a.max_new + 63) / 64)), kMaskThreads, 0, s>>>(a);
-    return hipGetLastError();
+    const int blocks = (a.max_new + 63) / 64, most = (int)(0xffffffffu / (unsigned)(kMaskThreads * blocks));      // sequences of a launch, which has fewer than 2^32 threads
+    for (int first = 0; first < a.B; first += most) {
+        TreeMaskArgs some = a;
+        some.q_off += first;
+        some.B = std::min(most, a.B - first);
+        tree_masks_long_kernel<<<dim3((unsigned)some.B, (unsigned)blocks), kMaskThreads, 0, s>>>(some);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <class T, bool DRAFT>
