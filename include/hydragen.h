@@ -350,7 +350,7 @@ int hg_kv_write_paged(hg_ctx* ctx, const void* Knew, const void* Vnew, int64_t s
  * hg_tree_attn_paged: hg_chunk_attn_paged but for what the n new tokens, the last n of the sequence's lengths[b] rows, see of each other: token t sees all rows [0, lengths[b] - n) and of its sequence's n
  * rows those with a bit in its row of masks (DEVICE, mask_words words to a row, bits as above, from hg_tree_masks or any others: bits from n on count for nothing, tokens without a bit are not
  * seen, and a token without a row to see has O = 0, LSE = -inf).  max_new has no limit here.  Everything else is as there: strides, bounds, the workspace (of which the key ranges of tiles take what
- * there is, up to 64 ranges of rows * Hq rows, and are chosen on the device), what rows that are not seen may hold.
+ * there is, up to 64 ranges of rows * Hq rows; with up to 256 sequences they are chosen on the device from the lengths, with more on the host from max_len), what rows that are not seen may hold.
  *
  * hg_tree_verify: which tokens stand, and the token behind them, so that what comes out is distributed as if the target had been asked token by token (for drafts that are drawn from `draft`, or that are
  * told apart among siblings).  Token 0 stands.  The others are looked at in order, each if its parent is the last one that stands; with x the token (tokens[i]), p and q row
@@ -369,7 +369,7 @@ int hg_kv_write_paged(hg_ctx* ctx, const void* Knew, const void* Vnew, int64_t s
  * -1 behind them.  max_new at most HG_MAX_TREE; tokens from max_new on are not looked at, their places in path are left as they are.  Outputs must not be inputs.
  *
  * hg_tree_keep_paged: the tokens that stand become part of the context: row lengths[b] - n + i = row lengths[b] - n + path[q_off[b] + i] for i < accepted[b], K and V, in the pages of n_layers (at most
- * HG_MAX_LAYERS) caches that differ in K and V only, and new_lengths[b] = max(lengths[b] - n + accepted[b], 0).  accepted above n counts as n; a path that is not ascending gives wrong rows; rows that the table has no place
+ * HG_MAX_LAYERS) caches that differ in K and V only, and new_lengths[b] = max(lengths[b] - n + accepted[b], 0).  accepted above n or max_new counts as that; a path that is not ascending gives wrong rows; rows that the table has no place
  * for, or whose page is not in the pool, are not moved, nor is anything from or to a place outside the sequence's n rows.  new_lengths must not be any of the inputs; no pool may be there twice.
  */
 int hg_tree_masks(hg_ctx* ctx, const int32_t* parents, const int32_t* q_off, int rows, int max_new, int B, uint32_t* masks, int mask_words, int32_t* depth);

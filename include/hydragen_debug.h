@@ -62,13 +62,14 @@ extern "C" {
  * fills out[3] = { KV head, column of that head, split } and returns 1, or returns 0 if that workgroup has nothing to do or does
  * not exist (there are tiles * splits * Hkv of them, rounded up to a multiple of 8).  Ids equal modulo 8 share an XCD.
  *
- * hg_debug_ragged_plan: how hg_prompt_attn (paged 0; max_new and codes are not looked at) hg_chunk_attn_paged (paged 1; codes: 8-bit rows) or hg_tree_attn_paged (paged 2) would run with these sizes and
+ * hg_debug_ragged_plan: how hg_prompt_attn (paged 0; max_new and codes are not looked at), hg_chunk_attn_paged (paged 1; codes: 8-bit rows) or hg_tree_attn_paged (paged 2) would run with these sizes and
  * workspace_bytes of workspace.  Returns what the call would return before it enqueues anything, and on HG_OK fills out[14] = { 1 if the launch has 128-row tiles; rows that
  * remain behind tiles and are not one, at most (0: tiles take everything); ... of the largest sequence; key ranges of what remains, and keys of one;
  * key ranges of a tile, and keys of one; where the partial results of what remains begin in the workspace, in floats, and their LSE, the same for tiles (-1: none);
  * workgroups of the launch (0: nothing to do), threads of one; workgroups of the join (0: none) }.  What remains of a sequence has B * Hkv * out[2] rows of parts per range, tiles
- * have rows * Hq.  Trees of up to 256 sequences that do not fill the chip: the key ranges of a tile are chosen on the device, at most as many and none shorter than said here, and the word in which the choice is left
- * for the join lies in the 64 floats before the partial results of tiles.
+ * have rows * Hq.  Trees of up to 256 sequences whose tokens do not fill the chip: the key ranges of a tile are chosen on the device.  A sequence has at most as many as said here.  The longest range that is
+ * chosen is at least as long as said here, or no sequence is cut; longer sequences are cut into equal ranges, multiples of 64 keys, which may be little more than half as long.  The word in which the choice is left for
+ * the join lies in the 64 floats before the partial results of tiles.  Where they are chosen among more than 768 workgroups of one range each, the launch's workgroups include those that end at once.
  */
 int hg_debug_wide_plan(int n_blocks, int max_rows, int max_seqs, int Hkv, int rows_per_seq, int max_parts,
                        int slots_per_xcd, int D, int out[9]);

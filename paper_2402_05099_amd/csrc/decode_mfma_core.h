@@ -266,7 +266,8 @@ struct MfmaTile {
         }
     }
 
-    // online softmax: scores -> weights as B operand of the value product (k-slot order), row sums, lazy rescaling
+    // online softmax: scores -> weights as B operand of the value product (k-slot order), row sums, lazy rescaling.  The weights are rounded to bf16, the product's type (fp32 products have 1/16 of its
+    // rate): by 2^-8 of each at most, so O is off by as much of the largest value; the sum, and with it LSE, is that of the unrounded ones.
     __device__ __forceinline__ void softmax(const Scores& r, uintx4 (&pb)[2]) {
         float tmax;
         if constexpr (TR == 16) {

@@ -6,7 +6,7 @@
 // A workgroup of NW wavefronts takes one tile and one range of its keys; its 32-key stages go to the wavefronts in turn, each with a K and a V slot
 // in LDS that is filled again by global_load_lds_dwordx4 as soon as its rows have been multiplied.  The wavefronts never wait for each other until their
 // (m, l, O) meet in LDS.  So a call of short contexts is one launch that needs no workspace, and one of long contexts splits the
-// keys over workgroups as well: partial results by Eq. 5, joined by ragged_join_kernel (ragged_rows.hip).
+// keys over workgroups as well: partial results by Eq. 5, joined by the kernel of ragged_rows_kernels.h.
 //
 // Single tokens, all of one length: 32 x 64/8 heads, 8192 keys 179 us, 6.0 TB/s, codes 106 us, 5.1 (at D = 64 102 and 69 us); 32 x 40/40, 2048 keys 213 us, 6.3 TB/s, codes 132, 5.1;
 // 32 rows instead of 8 cost 14 % more, over codes 22.  45 x 16/2 heads, up to 515 keys 8.8 us, a chain of loads: lengths, table, rows, the join.

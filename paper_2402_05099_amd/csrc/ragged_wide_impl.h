@@ -14,7 +14,7 @@
 //   * Codes of K are copied to a staging ring of the wavefront's own, and become bf16 on the way from there into the K ring, once per workgroup; those of V stay
 //     codes in LDS and become bf16 behind the transposing read, in every wavefront.  The LDS is what codes press on (K and V both expanded into rings: 1767 cycles a
 //     stage where bf16 rows take 1417, of which the LDS needs some 770 for each of a CU's two workgroups), and this way the vector ALU carries half of it.
-//   * The output is divided by the sum of the rounded weights (LSE has the sum of the unrounded ones): where one key has nearly all the weight its rounding
+//   * Weights are rounded to bf16, the second product's type, by 2^-8 of each at most.  The output is divided by the sum of the rounded weights (LSE has the sum of the unrounded ones): where one key has nearly all the weight its rounding
 //     would otherwise show in O as a whole, since the largest weight is anywhere up to kMostWeight and not a power of two.
 //
 // What bounds it: the matrix pipes, and in calls of a millisecond the board's power.  One prompt of 8192 tokens, 64/8 heads: 0.95-1.01 ms, 1.10-1.16 PFLOP/s of what the mask leaves, at

@@ -85,6 +85,18 @@ def test_contexts_that_are_not_worth_a_split(D, codes):
     assert one > 768 and p["tile_nsplit"] > 1 and choice > 8192
 
 
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_sequences_about_as_long_as_the_longest_range(D, codes):
+    """A key more than the longest range makes two that are little more than half as long."""
+    at = 0
+    for _ in range(2):      # the range that is chosen for the first lengths, and then lengths about it (it may be chosen anew, so what is chosen is looked at again)
+        near = [at + d for d in (-1, 0, 1, 2)] + [2 * at + d for d in (-1, 0, 1)] if at else [300, 700]
+        p, one, choice = run([(2000, 40)] + [(x, 40) for x in near], (8, 2), D, codes=codes, kind="any")
+        assert one <= 768 and p["tile_nsplit"] > 1 and p["tile_chunk"] <= choice < 2000
+        at = choice
+
+
 def test_a_captured_call_follows_its_lengths():
     """Replays with lengths for which the workgroups split, and with such that they don't: what eager calls give."""
     B, n, heads, D, cap = 110, 33, (8, 8), 128, 4096

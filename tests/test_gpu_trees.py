@@ -169,6 +169,7 @@ def test_tokens_and_rows_behind_the_bounds(D, codes):
     run_attn([(300, 40), (20, 7), (90, 64)], (8, 2), D, codes=codes, max_len=100)
 
 
+# (It is up to 256 sequences, not 64, that the workgroups choose for.)
 @pytest.mark.parametrize("codes", [False, True])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("B", [1, 2, 63, 64, 65, 130, 256, 257])
@@ -190,6 +191,7 @@ def test_tiles_of_sequences_without_enough_rows(D, codes):
     run_attn([(40, 9), (70, 64), (0, 3)], (8, 2), D, codes=codes, max_len=0)
 
 
+# (66 and 72 sequences: here too the workgroups choose.  Ranges by the host, for more than 256, are in test_gpu_tree_ranges.py.)
 @pytest.mark.parametrize("codes", [False, True])
 @pytest.mark.parametrize("D", [64, 128])
 def test_key_ranges_of_more_sequences_than_are_ordered(D, codes):
