@@ -85,6 +85,12 @@ def test_contexts_that_are_not_worth_a_split(D, codes):
     assert one > 768 and p["tile_nsplit"] > 1 and choice > 8192
 
 
+def test_as_many_jobs_as_there_can_be_tiles():
+    """520 KV heads leave no job beside those that the tokens can make: two sequences of 33 rows and one of few."""
+    p, one, choice = run([(1030, 33), (33, 33), (50, 3)], (520, 520), 64)
+    assert one > 768 and p["tile_nsplit"] > 1 and choice > 1030
+
+
 @pytest.mark.parametrize("codes", [False, True])
 @pytest.mark.parametrize("D", [64, 128])
 def test_sequences_about_as_long_as_the_longest_range(D, codes):
